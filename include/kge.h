@@ -273,9 +273,85 @@ typedef struct {
 int kge_sample_steps(const kge_sampler* sampler, int64_t first_step, int64_t n_steps, int64_t* h, int64_t* r,
                      int64_t* t, int64_t* neg, int32_t* sides, void* stream);
 
+/*
+ * Rows of scores as distributions over candidates.  scores: [rows] of n values, `ld` >= n values from one row's start to the
+ * next, of the type `dtype`; as kge_score writes them, or a caller's own.  Rows may start at any multiple of a value's size.
+ * The calls below need no context; they enqueue on `stream` of the current device, on which all pointers must lie, and
+ * keep intermediate results of rows of more than 32,768 values in `workspace`, memory of the caller (16-byte aligned) of at least
+ * the bytes that the ..._workspace function of the same arguments returns; it may be NULL where that is 0.  A workspace
+ * serves one call at a time: calls that may overlap, graphs that may run side by side among them, need one each.  All
+ * of them can be captured into HIP graphs.  rows may be 0; n is in [1, 2^32).  Errors: kge_last_error(NULL) has the text.
+ *
+ * Order of the candidates of a row: higher score first, equal scores by their position.
+ * (Knowledge distillation and decoding have no passage in the paper.)
+ */
+typedef enum { KGE_F32 = 0, KGE_BF16 = 1, KGE_F16 = 2 } kge_dtype;
+
+/*
+ * The best m candidates of every row, 1 <= m <= 1024: ids_out [rows x m] receives their positions in the row, scores_out [rows x m]
+ * their scores (fp32), best first.  -inf and NaN mark candidates that are masked and never returned; where a row has fewer
+ * than m others, the list ends with id -1 and score -inf.
+ * lse_out: device float [rows] or NULL, receives log sum_j exp(s_j / temperature) over the candidates that are not masked
+ * (-inf without any).  temperature > 0; it has no other effect.
+ */
+int64_t kge_top_scores_workspace(int64_t rows, int64_t n, int32_t m);
+int kge_top_scores(const void* scores, int32_t dtype, int64_t rows, int64_t n, int64_t ld, int32_t m, float temperature,
+                   int64_t* ids_out, float* scores_out, float* lse_out,
+                   void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Draws from every row by given random numbers.  With w_j = exp((s_j - best) / temperature) (masked candidates, -inf and NaN: 0) the
+ * candidates kept are the first K in order, K the least of
+ *     top_k (0, or n and more: all; else at most 1024),
+ *     the fewest whose w sum to top_p times the sum over those first top_k or more (1: all; at least one), and
+ *     the number with w_j >= min_p (0: all);
+ * the number u in [0, 1) falls on the first position j at which the sum of the kept w over positions up to j exceeds u times their
+ * whole sum.  temperature 0: the best candidate.  All sums are in 64 bits; the draw depends on the row and on u alone.
+ * u [rows x draws] (fp64: a row of millions of candidates needs more than 24 bits).  ids_out [rows x draws] receives the positions,
+ * logp_out (float, same shape, or NULL) the logarithm of the candidate's share of the kept w.  A row without a candidate: id
+ * -1, logarithm -inf.  Numbers outside [0, 1) count as the nearest inside, NaN as 0.
+ */
+int64_t kge_sample_scores_workspace(int64_t rows, int64_t n, int32_t draws, int32_t top_k, float top_p);
+int kge_sample_scores(const void* scores, int32_t dtype, int64_t rows, int64_t n, int64_t ld,
+                      const double* u, int32_t draws, float temperature, int32_t top_k, float top_p, float min_p,
+                      int64_t* ids_out, float* logp_out, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Divergence of rows of a student's scores s from a teacher's lists of best candidates, and its gradient.
+ * teacher_ids, teacher_scores [rows x m], 1 <= m <= 1024, as kge_top_scores writes them; entries with an id outside [0, n) or the
+ * score -inf are unused.  With q = softmax(s / T), T = temperature > 0, and p_e over the entries of a row
+ *     teacher_lse NULL:     p = softmax of their scores / T
+ *     teacher_lse [rows]:   p_e = exp(score_e / T - teacher_lse), the lse_out of kge_top_scores at the same temperature; the rest,
+ *                           p_r = max(0, 1 - sum p), belongs to the candidates that are not listed, of which the student gives q_r
+ *     loss   = T^2 [ sum_e p_e log(p_e / q_(id_e)) + p_r log(p_r / q_r) ]                      -> loss_out [rows], may be NULL
+ *     grad_j = grad_scale * d loss / d s_j                                                     -> grad_out, may be NULL
+ * Entries of the same id add their p.  grad_out [rows] of n values of the type `dtype`, ld_grad >= n apart; it may be `scores` itself
+ * (with the same pitch) and must not overlap it otherwise.  -inf marks a candidate that is masked: q = 0, gradient 0 unless it is
+ * listed.  A row with no candidate, or with no entry in use, has loss 0 and gradient 0; so has a rest without a candidate it could
+ * belong to.  NaN and +inf make the row's loss and gradient NaN.
+ */
+int64_t kge_distill_loss_workspace(int64_t rows, int64_t n);
+int kge_distill_loss(const void* scores, int32_t dtype, int64_t rows, int64_t n, int64_t ld,
+                     const int64_t* teacher_ids, const float* teacher_scores, const float* teacher_lse, int32_t m,
+                     float temperature, float grad_scale, float* loss_out, void* grad_out, int64_t ld_grad,
+                     void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * kge_train_step with that divergence for its loss: positive i's row is its scores of the k corrupting entities of its chunk, teacher
+ * entries are positions in 0 .. k - 1 among them, L = (1/b) sum_i loss_i.  The third entity of a positive (its tail, or its head) takes
+ * part only where it is among the corrupting entities; cfg.loss and cfg.adv_temperature are not used.  Everything else, the
+ * update among it, as in kge_train_step (rows of the positives count as touched, with the gradient they get).
+ * TransE-L2, DistMult, ComplEx and RESCAL; k <= 32768.  teacher_lse may be NULL.
+ */
+int kge_distill_step(kge_ctx* ctx, float* ent, float* ent_state, float* rel, float* rel_state,
+                     const int64_t* h, const int64_t* r, const int64_t* t, int64_t b,
+                     const int64_t* neg, int64_t k, int64_t chunk, int32_t neg_side, float gamma, float lr,
+                     const int64_t* teacher_ids, const float* teacher_scores, const float* teacher_lse, int32_t m,
+                     float temperature, void* hip_stream, float* loss_out);
+
 /* (host) Text of the last error on this context ("" if none); valid until the next call on the context.
  * kge_last_error(NULL) returns the text of the last failed context-free call (kge_create, kge_sample_steps,
- * kge_rank_metrics, kge_score_noalloc) on this thread.  (Error reporting, no passage.) */
+ * kge_rank_metrics, kge_score_noalloc, kge_top_scores, kge_sample_scores, kge_distill_loss) on this thread.  (Error reporting, no passage.) */
 const char* kge_last_error(const kge_ctx* ctx);
 
 /* Bytes of device workspace the context holds.  (No passage of the paper: library bookkeeping.) */

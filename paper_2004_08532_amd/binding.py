@@ -26,7 +26,9 @@ MODEL_IDS = {"transe_l2": KGE_TRANSE_L2, "transe_l1": KGE_TRANSE_L1, "distmult":
 
 EXPORTS = ("kge_create", "kge_destroy", "kge_train_step", "kge_train_steps", "kge_score", "kge_get_dedup",
            "kge_check_indices", "kge_last_error", "kge_workspace_bytes", "kge_profile", "kge_profile_read",
-           "kge_profile_slot_name", "kge_sample_steps", "kge_rank", "kge_rank_metrics", "kge_graph_captures", "kge_score_noalloc")
+           "kge_profile_slot_name", "kge_sample_steps", "kge_rank", "kge_rank_metrics", "kge_graph_captures", "kge_score_noalloc",
+           "kge_top_scores", "kge_top_scores_workspace", "kge_sample_scores", "kge_sample_scores_workspace",
+           "kge_distill_loss", "kge_distill_loss_workspace", "kge_distill_step")
 KGE_PROF_SLOTS = 9
 
 
@@ -93,6 +95,20 @@ def _load() -> ctypes.CDLL:
     lib.kge_rank.argtypes = [vp, vp, vp, vp, vp, vp, i64, vp, i64, i64, i32, f32, vp, vp]
     lib.kge_rank_metrics.restype = ctypes.c_int
     lib.kge_rank_metrics.argtypes = [vp, i64, vp, vp]
+    lib.kge_top_scores_workspace.restype = i64
+    lib.kge_top_scores_workspace.argtypes = [i64, i64, i32]
+    lib.kge_top_scores.restype = ctypes.c_int
+    lib.kge_top_scores.argtypes = [vp, i32, i64, i64, i64, i32, f32, vp, vp, vp, vp, i64, vp]
+    lib.kge_sample_scores_workspace.restype = i64
+    lib.kge_sample_scores_workspace.argtypes = [i64, i64, i32, i32, f32]
+    lib.kge_sample_scores.restype = ctypes.c_int
+    lib.kge_sample_scores.argtypes = [vp, i32, i64, i64, i64, vp, i32, f32, i32, f32, f32, vp, vp, vp, i64, vp]
+    lib.kge_distill_loss_workspace.restype = i64
+    lib.kge_distill_loss_workspace.argtypes = [i64, i64]
+    lib.kge_distill_loss.restype = ctypes.c_int
+    lib.kge_distill_loss.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, i32, f32, f32, vp, vp, i64, vp, i64, vp]
+    lib.kge_distill_step.restype = ctypes.c_int
+    lib.kge_distill_step.argtypes = [vp] * 5 + [vp] * 3 + [i64, vp, i64, i64, i32, f32, f32, vp, vp, vp, i32, f32, vp, vp]
     lib.kge_sample_steps.restype = ctypes.c_int
     lib.kge_sample_steps.argtypes = [vp, i64, i64, vp, vp, vp, vp, vp, vp]
     return lib
@@ -161,6 +177,139 @@ def kge_sample_steps(seed, triples, num_entities, batch, n_chunks, neg_per_chunk
                                _dev_ptr(r, i, "r"), _dev_ptr(t, i, "t"), _dev_ptr(neg, i, "neg"),
                                _dev_ptr(sides, torch.int32, "sides"), _stream(hip_stream))
     _check(None, rc)
+
+
+# ---- rows of scores: two-dimensional tensors [rows, n] whose rows are contiguous, any distance apart
+KGE_F32, KGE_BF16, KGE_F16 = 0, 1, 2
+_DTYPES = {torch.float32: KGE_F32, torch.bfloat16: KGE_BF16, torch.float16: KGE_F16}
+
+
+def _rows(x: torch.Tensor, name: str):
+    """Address, dtype, rows, n and distance of the rows of a tensor of scores."""
+    if not isinstance(x, _Tensor) or not x.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {x.dtype}")
+    if x.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    rows, n = x.shape
+    ld = x.stride(0) if rows > 1 else n
+    if (n > 1 and x.stride(1) != 1) or ld < n:
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    return x.data_ptr(), dtype, rows, n, ld
+
+
+def _shaped(x, dtype, shape, like, name: str):
+    """Address of a contiguous tensor of this shape on the device of `like`, or None."""
+    if x is None:
+        return None
+    p = _dev_ptr(x, dtype, name)
+    if tuple(x.shape) != shape:
+        raise ValueError(f"{name} must have the shape {shape}, got {tuple(x.shape)}")
+    if x.device != like.device:
+        raise ValueError(f"{name} must be on the device of the scores")
+    return p
+
+
+def _on_device(call, like, hip_stream):
+    """call(stream) with the device of `like` current, as calls without a context need it."""
+    device = like.device.index
+    if device == torch.cuda.current_device():
+        return call(_stream(hip_stream))
+    with torch.cuda.device(device):
+        return call(_stream(hip_stream))
+
+
+def _workspace(given, needed: int, like, hip_stream):
+    """The caller's workspace, or one that lives until the work that has been enqueued on the stream is over."""
+    if given is not None:
+        if given.device != like.device:
+            raise ValueError("workspace must be on the device of the scores")
+        return given
+    if needed == 0:
+        return None
+    ws = torch.empty(needed, dtype=torch.uint8, device=like.device)
+    if hip_stream is not None:
+        ws.record_stream(hip_stream)
+    return ws
+
+
+def kge_top_scores_workspace(rows, n, m) -> int:
+    return int(_lib.kge_top_scores_workspace(int(rows), int(n), int(m)))
+
+
+def kge_top_scores(scores, m, temperature, ids_out, scores_out, lse_out=None, workspace=None, hip_stream=None) -> None:
+    """scores [rows, n] float32, bfloat16 or float16; ids_out int64 and scores_out float32 [rows, m], lse_out float32 [rows] or None."""
+    p, dtype, rows, n, ld = _rows(scores, "scores")
+    m, f = int(m), torch.float32
+    ids, tops = _shaped(ids_out, torch.int64, (rows, m), scores, "ids_out"), _shaped(scores_out, f, (rows, m), scores, "scores_out")
+    lse = _shaped(lse_out, f, (rows,), scores, "lse_out")
+    ws = _workspace(workspace, kge_top_scores_workspace(rows, n, m), scores, hip_stream)
+    at, size = _dev_ptr(ws, torch.uint8, "workspace"), 0 if ws is None else ws.numel()
+    _check(None, _on_device(lambda st: _lib.kge_top_scores(p, dtype, rows, n, ld, m, float(temperature), ids, tops, lse, at, size, st),
+                            scores, hip_stream))
+
+
+def kge_sample_scores_workspace(rows, n, draws, top_k=0, top_p=1.0) -> int:
+    return int(_lib.kge_sample_scores_workspace(int(rows), int(n), int(draws), int(top_k), float(top_p)))
+
+
+def kge_sample_scores(scores, u, temperature, top_k, top_p, min_p, ids_out, logp_out=None, workspace=None, hip_stream=None) -> None:
+    """scores [rows, n]; u float64 [rows, draws] in [0, 1); ids_out int64 and logp_out float32 (or None) of u's shape."""
+    p, dtype, rows, n, ld = _rows(scores, "scores")
+    if not isinstance(u, _Tensor) or u.dim() != 2 or u.shape[0] != rows:
+        raise ValueError("u must be a tensor [rows, draws]")
+    draws = u.shape[1]
+    un = _shaped(u, torch.float64, (rows, draws), scores, "u")
+    ids = _shaped(ids_out, torch.int64, (rows, draws), scores, "ids_out")
+    logp = _shaped(logp_out, torch.float32, (rows, draws), scores, "logp_out")
+    ws = _workspace(workspace, kge_sample_scores_workspace(rows, n, draws, top_k, top_p), scores, hip_stream)
+    at, size = _dev_ptr(ws, torch.uint8, "workspace"), 0 if ws is None else ws.numel()
+    _check(None, _on_device(lambda st: _lib.kge_sample_scores(p, dtype, rows, n, ld, un, draws, float(temperature), int(top_k),
+                                                              float(top_p), float(min_p), ids, logp, at, size, st), scores, hip_stream))
+
+
+def kge_distill_loss_workspace(rows, n) -> int:
+    return int(_lib.kge_distill_loss_workspace(int(rows), int(n)))
+
+
+def _teacher(ids, scores, lse, rows, like):
+    if not isinstance(ids, _Tensor) or ids.dim() != 2:
+        raise ValueError("teacher_ids must be a tensor [rows, m]")
+    m, f = ids.shape[1], torch.float32
+    return (_shaped(ids, torch.int64, (rows, m), like, "teacher_ids"), _shaped(scores, f, (rows, m), like, "teacher_scores"),
+            _shaped(lse, f, (rows,), like, "teacher_lse"), m)
+
+
+def kge_distill_loss(scores, teacher_ids, teacher_scores, teacher_lse, temperature, grad_scale, loss_out=None, grad_out=None,
+                     workspace=None, hip_stream=None) -> None:
+    """scores [rows, n]; teacher_ids int64 and teacher_scores float32 [rows, m], teacher_lse float32 [rows] or None; loss_out
+    float32 [rows] or None; grad_out [rows, n] of the scores' dtype, or the scores themselves, or None."""
+    p, dtype, rows, n, ld = _rows(scores, "scores")
+    grad, ld_grad = None, n
+    if grad_out is not None:
+        grad, g_dtype, g_rows, g_n, ld_grad = _rows(grad_out, "grad_out")
+        if (g_dtype, g_rows, g_n, grad_out.device) != (dtype, rows, n, scores.device):
+            raise ValueError("grad_out must have the shape, dtype and device of the scores")
+    ids, tops, lse, m = _teacher(teacher_ids, teacher_scores, teacher_lse, rows, scores)
+    loss = _shaped(loss_out, torch.float32, (rows,), scores, "loss_out")
+    ws = _workspace(workspace, kge_distill_loss_workspace(rows, n), scores, hip_stream)
+    at, size = _dev_ptr(ws, torch.uint8, "workspace"), 0 if ws is None else ws.numel()
+    _check(None, _on_device(lambda st: _lib.kge_distill_loss(p, dtype, rows, n, ld, ids, tops, lse, m, float(temperature), float(grad_scale),
+                                                             loss, grad, ld_grad, at, size, st), scores, hip_stream))
+
+
+def kge_distill_step(ctx, ent, ent_state, rel, rel_state, h, r, t, b, neg, k, chunk, neg_side, gamma, lr, teacher_ids, teacher_scores,
+                     teacher_lse, temperature, hip_stream=None, loss_out=None) -> None:
+    f, i = torch.float32, torch.int64
+    ids, tops, lse, m = _teacher(teacher_ids, teacher_scores, teacher_lse, int(b), ent)
+    rc = _lib.kge_distill_step(ctx, _dev_ptr(ent, f, "ent"), _dev_ptr(ent_state, f, "ent_state"),
+                               _dev_ptr(rel, f, "rel"), _dev_ptr(rel_state, f, "rel_state"),
+                               _dev_ptr(h, i, "h"), _dev_ptr(r, i, "r"), _dev_ptr(t, i, "t"), int(b),
+                               _dev_ptr(neg, i, "neg"), int(k), int(chunk), int(neg_side), float(gamma), float(lr),
+                               ids, tops, lse, m, float(temperature), _stream(hip_stream), _dev_ptr(loss_out, f, "loss_out"))
+    _check(ctx, rc)
 
 
 def kge_create(cfg: kge_config) -> ctypes.c_void_p:
@@ -293,6 +442,11 @@ class KgeContext:
                     stream=None):
         kge_train_steps(self.ctx, ent, ent_state, rel, rel_state, h, r, t, h.shape[1], neg, k, chunk, neg_sides,
                         h.shape[0], gamma, lr, stream, loss_out)
+
+    def distill_step(self, ent, ent_state, rel, rel_state, h, r, t, neg, k, chunk, neg_side, gamma, lr, teacher_ids, teacher_scores,
+                     teacher_lse=None, temperature=1.0, loss_out=None, stream=None):
+        kge_distill_step(self.ctx, ent, ent_state, rel, rel_state, h, r, t, h.numel(), neg, k, chunk, neg_side, gamma, lr,
+                         teacher_ids, teacher_scores, teacher_lse, temperature, stream, loss_out)
 
     def profile(self, enable):
         kge_profile(self.ctx, enable)

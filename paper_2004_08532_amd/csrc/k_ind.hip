@@ -527,7 +527,7 @@ void launch(kge_ctx* c, const float* E, const float* R, const StepIds& ids, int 
 // uniform weights only.)
 bool kge_ind_step_fits(const kge_ctx* c, int g) {
     const bool rows = c->cfg.model != KGE_RESCAL && c->cfg.model != KGE_TRANSR;
-    return g == 1 && rows && (c->cfg.gemm_input == 0 || kge_gemm_backward_forms_w(c));
+    return g == 1 && rows && !c->teacher && (c->cfg.gemm_input == 0 || kge_gemm_backward_forms_w(c));
 }
 bool kge_ind_score_fits(const kge_ctx* c, int g) {
     return g == 1 && c->cfg.model != KGE_RESCAL && c->cfg.model != KGE_TRANSR && c->cfg.gemm_input == 0;

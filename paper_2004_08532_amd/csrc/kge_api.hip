@@ -8,6 +8,7 @@
 #include <new>
 
 #include "kge_common.h"
+#include "k_rows.h"
 #include "k_weights.h"
 
 // Scratch memory of kge_score_noalloc, the one entry point that allocates nothing: a fixed array in the library's
@@ -88,6 +89,40 @@ int check_batch(kge_ctx* c, const void* ent, const void* rel, const int64_t* h, 
     if (side != KGE_NEG_TAIL && side != KGE_NEG_HEAD) return fail(c, KGE_ERR_INVALID_ARG, "neg_side must be 0 or 1%s");
     if (b > c->cfg.max_batch || k > c->cfg.max_neg_per_chunk || b / chunk > c->cfg.max_chunks)
         return fail(c, KGE_ERR_WORKSPACE, "b, k or b/chunk exceed the sizes given to kge_create%s");
+    return KGE_OK;
+}
+
+// ---- rows of scores
+int check_rows(const void* scores, int32_t dtype, int64_t rows, int64_t n, int64_t ld) {
+    if (dtype != KGE_F32 && dtype != KGE_BF16 && dtype != KGE_F16) return fail(nullptr, KGE_ERR_INVALID_ARG, "dtype must be a kge_dtype%s");
+    if (rows < 0 || rows > 0x7FFFFFFF || n <= 0 || n >= (1ll << 32) || ld < n)
+        return fail(nullptr, KGE_ERR_INVALID_ARG, "rows, n or ld out of range%s");
+    if (rows * pieces(n, KGE_ROW_SEGMENT) > (1ll << 35)) return fail(nullptr, KGE_ERR_INVALID_ARG, "rows * n out of range%s");
+    if (rows == 0) return KGE_OK;
+    if (!scores) return fail(nullptr, KGE_ERR_INVALID_ARG, "scores is null%s");
+    if ((uintptr_t)scores % (dtype == KGE_F32 ? 4 : 2)) return fail(nullptr, KGE_ERR_INVALID_ARG, "scores is not aligned to its type%s");
+    return KGE_OK;
+}
+
+int check_workspace(const void* workspace, int64_t bytes, int64_t needed) {
+    if (needed == 0) return KGE_OK;
+    if (!workspace || bytes < needed) return fail(nullptr, KGE_ERR_WORKSPACE, "the workspace is smaller than the size asked for%s");
+    if ((uintptr_t)workspace % 16) return fail(nullptr, KGE_ERR_INVALID_ARG, "the workspace is not aligned to 16 bytes%s");
+    return KGE_OK;
+}
+
+bool positive_finite(float x) { return x > 0.f && x <= 3.402823466e38f; }
+
+int check_teacher(kge_ctx* c, const int64_t* ids, const float* scores, int32_t m, float temperature) {
+    if (!ids || !scores) return fail(c, KGE_ERR_INVALID_ARG, "null teacher list%s");
+    if (m < 1 || m > KGE_TOP_MAX) return fail(c, KGE_ERR_INVALID_ARG, "m must be in 1 .. 1024%s");
+    if (!positive_finite(temperature)) return fail(c, KGE_ERR_INVALID_ARG, "temperature must be positive and finite%s");
+    return KGE_OK;
+}
+
+int launched(const char* what) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(nullptr, KGE_ERR_DEVICE, what, hipGetErrorString(e));
     return KGE_OK;
 }
 
@@ -213,6 +248,13 @@ int enqueue_ind_rest(kge_ctx* c, float* ent, float* ent_state, float* rel, float
     return end_of_step(c, st);
 }
 
+// The loss of kge_distill_step in the place of k_loss: scores (distances) in S -> W, loss terms of the rows.
+void launch_distill_loss(kge_ctx* c, int b, int k, float gamma, hipStream_t st) {
+    const RowScores rows = {c->S, KGE_F32, b, k, c->ld_s};
+    const StepRows step = {c, gamma, c->cfg.model == KGE_TRANSE_L2, c->cfg.gemm_input, c->cpos};
+    kge_launch_distill(rows, *c->teacher, 1.f / (float)b, 1.f / (float)b, c->row_loss, c->S, c->ld_s, &step, nullptr, st);
+}
+
 int enqueue_step(kge_ctx* c, float* ent, float* ent_state, float* rel, float* rel_state, const StepIds& ids, int K,
                  int G, float gamma, float lr, hipStream_t st) {
     const int B = ids.b;
@@ -280,7 +322,8 @@ int enqueue_step(kge_ctx* c, float* ent, float* ent_state, float* rel, float* re
     int n_loss_parts = gemm ? kge_gemm_loss_parts(c, B, K, G) : 0;
     if (run_loss) {
         ProfScope p(c, KGE_PROF_LOSS);
-        kge_launch_loss(c, B, K, gamma, st);
+        if (c->teacher) launch_distill_loss(c, B, K, gamma, st);
+        else kge_launch_loss(c, B, K, gamma, st);
     }
     {
         ProfScope p(c, KGE_PROF_BACKWARD);
@@ -649,6 +692,30 @@ int kge_train_steps(kge_ctx* c, float* ent, float* ent_state, float* rel, float*
     return plain(done, n_steps);
 }
 
+int kge_distill_step(kge_ctx* c, float* ent, float* ent_state, float* rel, float* rel_state,
+                     const int64_t* h, const int64_t* r, const int64_t* t, int64_t b,
+                     const int64_t* neg, int64_t k, int64_t chunk, int32_t neg_side, float gamma, float lr,
+                     const int64_t* teacher_ids, const float* teacher_scores, const float* teacher_lse, int32_t m,
+                     float temperature, void* hip_stream, float* loss_out) {
+    if (!c) return KGE_ERR_INVALID_ARG;
+    c->err[0] = 0;
+    if (!is_gemm_model(c->cfg.model))
+        return fail(c, KGE_ERR_UNSUPPORTED, "kge_distill_step serves TransE-L2, DistMult, ComplEx and RESCAL%s");
+    if (!ent_state || !rel_state) return fail(c, KGE_ERR_INVALID_ARG, "null optimizer state%s");
+    int rc = check_batch(c, ent, rel, h, r, t, b, neg, k, chunk, neg_side, true);
+    if (rc != KGE_OK) return rc;
+    rc = check_teacher(c, teacher_ids, teacher_scores, m, temperature);
+    if (rc != KGE_OK) return rc;
+    if (k > KGE_ROW_RESIDENT) return fail(c, KGE_ERR_UNSUPPORTED, "kge_distill_step takes at most 32768 candidates per chunk%s");
+    KGE_HIP(c, hipSetDevice(c->cfg.device));
+    const StepIds ids = direct_ids(h, r, t, (int)b, neg, (int)((b / chunk) * k), neg_side, loss_out);
+    const TeacherLists lists = {teacher_ids, teacher_scores, teacher_lse, m, temperature};
+    c->teacher = &lists;
+    rc = enqueue_step(c, ent, ent_state, rel, rel_state, ids, (int)k, (int)chunk, gamma, lr, (hipStream_t)hip_stream);
+    c->teacher = nullptr;
+    return rc;
+}
+
 int kge_score(kge_ctx* c, const float* ent, const float* rel,
               const int64_t* h, const int64_t* r, const int64_t* t, int64_t b,
               const int64_t* neg, int64_t k, int64_t chunk, int32_t neg_side, float gamma,
@@ -827,6 +894,76 @@ int kge_sample_steps(const kge_sampler* sp, int64_t first_step, int64_t n_steps,
     if (kge_sample_launch(sp, first_step, n_steps, h, r, t, neg, sides, (hipStream_t)stream) != KGE_OK)
         return fail(nullptr, KGE_ERR_DEVICE, "launch of the sampling kernel failed%s");
     return KGE_OK;
+}
+
+int64_t kge_top_scores_workspace(int64_t rows, int64_t n, int32_t m) {
+    return rows > 0 && n > 0 && m > 0 ? kge_top_workspace(rows, n, m < KGE_TOP_MAX ? m : KGE_TOP_MAX) : 0;
+}
+
+int kge_top_scores(const void* scores, int32_t dtype, int64_t rows, int64_t n, int64_t ld, int32_t m, float temperature,
+                   int64_t* ids_out, float* scores_out, float* lse_out, void* workspace, int64_t workspace_bytes, void* stream) {
+    int rc = check_rows(scores, dtype, rows, n, ld);
+    if (rc != KGE_OK) return rc;
+    if (m < 1 || m > KGE_TOP_MAX) return fail(nullptr, KGE_ERR_INVALID_ARG, "m must be in 1 .. 1024%s");
+    if (!positive_finite(temperature)) return fail(nullptr, KGE_ERR_INVALID_ARG, "temperature must be positive and finite%s");
+    if (rows == 0) return KGE_OK;
+    if (!ids_out || !scores_out) return fail(nullptr, KGE_ERR_INVALID_ARG, "null output%s");
+    rc = check_workspace(workspace, workspace_bytes, kge_top_workspace(rows, n, m));
+    if (rc != KGE_OK) return rc;
+    kge_launch_top({scores, dtype, rows, n, ld}, m, temperature, ids_out, scores_out, nullptr, lse_out, workspace, (hipStream_t)stream);
+    return launched("kge_top_scores: %s");
+}
+
+int64_t kge_sample_scores_workspace(int64_t rows, int64_t n, int32_t draws, int32_t top_k, float top_p) {
+    if (rows <= 0 || n <= 0 || draws <= 0) return 0;
+    return kge_draw_workspace(rows, n, top_k <= 0 || top_k >= n ? 0 : top_k < KGE_TOP_MAX ? top_k : KGE_TOP_MAX, top_p);
+}
+
+int kge_sample_scores(const void* scores, int32_t dtype, int64_t rows, int64_t n, int64_t ld, const double* u, int32_t draws,
+                      float temperature, int32_t top_k, float top_p, float min_p, int64_t* ids_out, float* logp_out, void* workspace,
+                      int64_t workspace_bytes, void* stream) {
+    int rc = check_rows(scores, dtype, rows, n, ld);
+    if (rc != KGE_OK) return rc;
+    if (draws < 1 || draws > (1 << 20)) return fail(nullptr, KGE_ERR_INVALID_ARG, "draws must be in 1 .. 2^20%s");
+    if (temperature != 0.f && !positive_finite(temperature))
+        return fail(nullptr, KGE_ERR_INVALID_ARG, "temperature must be finite and not negative%s");
+    if (top_k < 0 || (top_k > KGE_TOP_MAX && top_k < n))
+        return fail(nullptr, KGE_ERR_INVALID_ARG, "top_k must be in 1 .. 1024, or 0 or at least n for all%s");
+    if (!(top_p >= 0.f && top_p <= 1.f) || !(min_p >= 0.f && min_p <= 1.f))
+        return fail(nullptr, KGE_ERR_INVALID_ARG, "top_p and min_p must be in [0, 1]%s");
+    if (rows == 0) return KGE_OK;
+    if (!u || !ids_out) return fail(nullptr, KGE_ERR_INVALID_ARG, "null random numbers or output%s");
+    if (top_k >= n) top_k = 0;
+    if (temperature == 0.f) { top_k = 1; temperature = 1.f; }  // the best candidate
+    rc = check_workspace(workspace, workspace_bytes, kge_draw_workspace(rows, n, top_k, top_p));
+    if (rc != KGE_OK) return rc;
+    kge_launch_draw({scores, dtype, rows, n, ld}, u, draws, temperature, top_k, top_p, min_p, ids_out, logp_out, workspace, (hipStream_t)stream);
+    return launched("kge_sample_scores: %s");
+}
+
+int64_t kge_distill_loss_workspace(int64_t rows, int64_t n) { return rows > 0 && n > 0 ? kge_distill_workspace(rows, n) : 0; }
+
+int kge_distill_loss(const void* scores, int32_t dtype, int64_t rows, int64_t n, int64_t ld, const int64_t* teacher_ids,
+                     const float* teacher_scores, const float* teacher_lse, int32_t m, float temperature, float grad_scale, float* loss_out,
+                     void* grad_out, int64_t ld_grad, void* workspace, int64_t workspace_bytes, void* stream) {
+    int rc = check_rows(scores, dtype, rows, n, ld);
+    if (rc != KGE_OK) return rc;
+    if (grad_out && ld_grad < n) return fail(nullptr, KGE_ERR_INVALID_ARG, "ld_grad is less than n%s");
+    if (grad_out && (uintptr_t)grad_out % (dtype == KGE_F32 ? 4 : 2))
+        return fail(nullptr, KGE_ERR_INVALID_ARG, "grad_out is not aligned to its type%s");
+    if (grad_out && grad_out == scores && ld_grad != ld)
+        return fail(nullptr, KGE_ERR_INVALID_ARG, "gradients in the place of the scores need the same pitch%s");
+    if (!(grad_scale >= -3.402823466e38f && grad_scale <= 3.402823466e38f))
+        return fail(nullptr, KGE_ERR_INVALID_ARG, "grad_scale must be finite%s");
+    if (rows == 0) return KGE_OK;
+    rc = check_teacher(nullptr, teacher_ids, teacher_scores, m, temperature);
+    if (rc != KGE_OK) return rc;
+    if (!loss_out && !grad_out) return fail(nullptr, KGE_ERR_INVALID_ARG, "null outputs%s");
+    rc = check_workspace(workspace, workspace_bytes, kge_distill_workspace(rows, n));
+    if (rc != KGE_OK) return rc;
+    kge_launch_distill({scores, dtype, rows, n, ld}, {teacher_ids, teacher_scores, teacher_lse, m, temperature}, grad_scale, 1.f, loss_out,
+                       grad_out, ld_grad, nullptr, workspace, (hipStream_t)stream);
+    return launched("kge_distill_loss: %s");
 }
 
 const char* kge_last_error(const kge_ctx* c) { return c ? c->err : g_create_err; }

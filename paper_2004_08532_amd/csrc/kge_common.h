@@ -54,6 +54,7 @@ struct TransrGroups {
 };
 
 struct StepBlock;
+struct TeacherLists;  // (k_rows.h)
 
 struct kge_ctx {
     kge_config cfg;
@@ -101,6 +102,8 @@ struct kge_ctx {
     int* flags;         // [0]: an id was out of range
     int32_t* rank_out;  // kge_rank: where the running call wants the ranks (the gather launch sets them to 1, the
                         // forward launch counts); null otherwise
+
+    const TeacherLists* teacher;  // kge_distill_step: the running step's loss; null otherwise
 
     int ebuf, rbuf;                 // which ping-pong half holds the sorted result
     uint32_t* sort_counts;          // radix sort: digit counts per slice of both lists, digit bases
