@@ -61,10 +61,10 @@ __device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, 
     if (a.t.lse) {
         l.shift = (double)a.t.lse[row];
     } else {
-        uint32_t best = 0;
-        for (int e = threadIdx.x; e < a.t.m; e += WAVES * 64) if (used(e)) best = max(best, order_key(ts[e]));
-        best = block_max_u32<WAVES>(best, reinterpret_cast<uint32_t*>(slot));
-        l.shift = best ? (double)key_score(best) * a.inv_t : 0.0;
+        float best = -INFINITY;
+        for (int e = threadIdx.x; e < a.t.m; e += WAVES * 64) if (used(e)) best = fmaxf(best, ts[e]);
+        best = block_max<WAVES>(best, reinterpret_cast<float*>(slot));
+        l.shift = best > -INFINITY ? (double)best * a.inv_t : 0.0;
         double z = 0.0;
         for (int e = threadIdx.x; e < a.t.m; e += WAVES * 64) if (used(e)) z += exp((double)ts[e] * a.inv_t - l.shift);
         z = block_sum64<WAVES>(z, slot);
@@ -176,8 +176,9 @@ __global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
     RowSums s = {};
     if constexpr (PASS == SEGMENT_GRAD) {
         const double* p = a.parts + 3 * row * a.segments;
-        double top = -INFINITY;
-        for (int g = 0; g < a.segments; ++g) top = fmax(top, p[3 * g]);
+        float best = -INFINITY;
+        for (int g = threadIdx.x; g < a.segments; g += THREADS) best = fmaxf(best, (float)p[3 * g]);
+        const double top = (double)block_max<WAVES>(best, reinterpret_cast<float*>(slot));
         for (int g = threadIdx.x; g < a.segments; g += THREADS) {
             if (p[3 * g + 1] == 0.0) continue;
             const double w = p[3 * g] == top ? 1.0 : exp((p[3 * g] - top) * a.inv_t);
@@ -188,15 +189,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
         const double* q = a.lists + 4 * row;
         l.mass = q[0]; l.rest = q[1]; l.cross = q[2]; l.shift = q[3];
     } else {
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor(best, o, 64));
-        __syncthreads();
-        if (lane == 0) slot[wave] = (double)best;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) best = fmaxf(best, (float)slot[w]);
-        __syncthreads();
-        s.best = (double)best;
+        s.best = (double)block_max<WAVES>(best, reinterpret_cast<float*>(slot));
     }
 #pragma unroll
     for (int i = 0; i < TPW; ++i) {

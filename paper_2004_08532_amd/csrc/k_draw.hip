@@ -28,34 +28,34 @@ template <int THREADS> __device__ __forceinline__ void write_empty(const DrawArg
     }
 }
 
-// What is kept: keys above t, and the first `ties` of those equal to it, with a weight of at least min_p.
+// What is kept, of scores with a weight of at least min_p: those above t, and of those equal to it the ones whose inverted position is
+// at least `least`, or the first `ties` of the row.
 struct Kept {
-    uint32_t t, ties;
-    float best;
-    double inv_t, min_p;
+    float t;
+    uint32_t least, ties;
 };
 
 // Position in a tile (256 scores from `first` on) at which the sum passes `target`, `base` of it in front of the tile; the tile's
-// last kept position where rounding leaves none.  `ties_before`: equal keys in front of the tile.
-template <int DT>
-__device__ __forceinline__ void draw_in_tile(const typename Score<DT>::type* s, int64_t first, int64_t n, const Kept& k, uint32_t ties_before,
-                                             double base, double target, int lane, int64_t& id, double& weight) {
+// last kept position where rounding leaves none.  COUNTED: equal scores are kept by `ties`, `ties_before` of them lie in front of the tile.
+template <int DT, bool COUNTED>
+__device__ __forceinline__ void draw_in_tile(const typename Score<DT>::type* s, int64_t first, int64_t n, const Kept& k, const Weights& weights, double min_p,
+                                             uint32_t ties_before, double base, double target, int lane, int64_t& id, double& weight) {
     float v[4];
     load4<DT>(s, first + lane * 4, n, v);
     double w[4], sum = 0.0;
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    uint32_t rank = ties_before, key[4];
+    uint32_t rank = ties_before;
+    if constexpr (COUNTED) {
+        const uint64_t below = ((uint64_t)1 << lane) - 1;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        key[q] = order_key(v[q]);
-        rank += __popcll(__ballot(key[q] == k.t) & below);
+        for (int q = 0; q < 4; ++q) rank += __popcll(__ballot(v[q] == k.t) & below);
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        w[q] = 0.0;
-        if (key[q] > k.t || (key[q] == k.t && rank < k.ties)) w[q] = weight64(key_score(key[q]), k.best, k.inv_t);
-        rank += key[q] == k.t;
-        if (!(w[q] >= k.min_p)) w[q] = 0.0;
+        v[q] = fmaxf(v[q], -INFINITY);
+        const bool equal = v[q] == k.t, in = v[q] > k.t || (equal && (COUNTED ? rank < k.ties : ~(uint32_t)(first + lane * 4 + q) >= k.least));
+        w[q] = in ? weights.of(v[q]) : 0.0;
+        rank += equal;
+        if (!(w[q] >= min_p)) w[q] = 0.0;
         sum += w[q];
     }
     const double incl = base + wave_scan64(sum, lane);
@@ -84,7 +84,7 @@ template <int THREADS>
 __device__ __forceinline__ void draw_from_list(const DrawArgs& a, int64_t row, uint64_t* list, int count, double* sums, int* kept) {
     if (count == 0) { write_empty<THREADS>(a, row); return; }
     const int lane = threadIdx.x & 63;
-    const float best = key_score((uint32_t)(list[0] >> 32));
+    const Weights weights(key_score((uint32_t)(list[0] >> 32)), a.inv_t);
     auto scan = [&](int n) {  // sums of weights -> running sums, by the first wave
         __syncthreads();
         if (threadIdx.x < 64) {
@@ -97,12 +97,12 @@ __device__ __forceinline__ void draw_from_list(const DrawArgs& a, int64_t row, u
         }
         __syncthreads();
     };
-    for (int e = threadIdx.x; e < count; e += THREADS) sums[e] = weight64(key_score((uint32_t)(list[e] >> 32)), best, a.inv_t);
+    for (int e = threadIdx.x; e < count; e += THREADS) sums[e] = weights.of(key_score((uint32_t)(list[e] >> 32)));
     if (threadIdx.x == 0) *kept = 0;
     scan(count);
     const double target = a.top_p < 1.0 ? a.top_p * sums[count - 1] : INFINITY;
     for (int e = threadIdx.x; e < count; e += THREADS) {
-        const bool in = e == 0 || (sums[e - 1] < target && weight64(key_score((uint32_t)(list[e] >> 32)), best, a.inv_t) >= a.min_p);
+        const bool in = e == 0 || (sums[e - 1] < target && weights.of(key_score((uint32_t)(list[e] >> 32))) >= a.min_p);
         if (in) atomicMax(kept, e + 1);
     }
     __syncthreads();
@@ -111,7 +111,7 @@ __device__ __forceinline__ void draw_from_list(const DrawArgs& a, int64_t row, u
     // into the order of positions; the key goes below the inverted position
     for (int e = threadIdx.x; e < size; e += THREADS) list[e] = e < count ? list[e] << 32 | list[e] >> 32 : 0;
     sort_descending<THREADS>(list, size);
-    for (int e = threadIdx.x; e < count; e += THREADS) sums[e] = weight64(key_score((uint32_t)list[e]), best, a.inv_t);
+    for (int e = threadIdx.x; e < count; e += THREADS) sums[e] = weights.of(key_score((uint32_t)list[e]));
     scan(count);
     const double total = sums[count - 1];
     for (int d = threadIdx.x; d < a.draws; d += THREADS) {
@@ -123,7 +123,7 @@ __device__ __forceinline__ void draw_from_list(const DrawArgs& a, int64_t row, u
         }
         while (lo > 0 && !(sums[lo] > sums[lo - 1])) --lo;  // (an entry without weight is never drawn)
         a.ids[row * a.draws + d] = (int64_t)(uint32_t)~(uint32_t)(list[lo] >> 32);
-        if (a.logp) a.logp[row * a.draws + d] = (float)log(weight64(key_score((uint32_t)list[lo]), best, a.inv_t) / total);
+        if (a.logp) a.logp[row * a.draws + d] = (float)log(weights.of(key_score((uint32_t)list[lo])) / total);
     }
 }
 
@@ -131,66 +131,40 @@ enum { CUT_NONE, CUT_WEIGHT, CUT_LIST };  // whole row or min-p; top-p; top-k (a
 
 template <int DT, int WAVES, int TPW, int CUT>
 __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
-    constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64, N = TPW * 4;
-    constexpr int LIST = CUT == CUT_LIST ? (CAP < KGE_TOP_MAX ? CAP : KGE_TOP_MAX) : 1;
-    constexpr int SUMS = CUT == CUT_LIST ? LIST : WAVES * TPW;
-    __shared__ uint64_t list[LIST];
-    __shared__ double sums[SUMS], part[2 * WAVES];
-    __shared__ uint32_t slots[2 * WAVES], ties[WAVES * TPW + 1], filled;
-    __shared__ int kept_entries;
+    constexpr int THREADS = WAVES * 64, N = TPW * 4, TILES = WAVES * TPW;
+    __shared__ float maxima[WAVES];
     const int64_t row = flat_block();
     if (row >= a.in.rows) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const auto* s = static_cast<const typename Score<DT>::type*>(a.in.p) + row * a.in.ld;
+    auto low = [&](int q) { return ~(uint32_t)tile_position<WAVES>(q); };
 
-    uint32_t key[N];
-    load_keys<DT, WAVES, TPW>(s, 0, a.in.n, key);
-    uint32_t best = 0;
-#pragma unroll
-    for (int q = 0; q < N; ++q) best = max(best, key[q]);
-    best = block_max_u32<WAVES>(best, slots);
-    if (best == 0) { write_empty<THREADS>(a, row); return; }
-
-    auto how_many_above = [&](uint32_t t) {
-        int c = 0;
-#pragma unroll
-        for (int q = 0; q < N; ++q) c += __popcll(__ballot(key[q] > t));
-        __syncthreads();
-        if (lane == 0) slots[wave] = c;
-        __syncthreads();
-        c = 0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) c += slots[w];
-        return c;
-    };
+    float v[N];
+    const float mine = load_tiles<DT, WAVES, TPW>(s, 0, a.in.n, v), best = block_max<WAVES>(mine, maxima);
+    if (!(best > -INFINITY)) { write_empty<THREADS>(a, row); return; }
 
     if constexpr (CUT == CUT_LIST) {
-        const int m = min(a.top_k, LIST), size = power_of_two(m);
-        for (int e = threadIdx.x; e < size; e += THREADS) list[e] = 0;
-        if (threadIdx.x == 0) filled = 0;
-        int reach, last = CAP;
-        const uint32_t t = select_threshold<WAVES, N, uint32_t>(key, best, m, slots, reach);
-        if (reach > m) last = nth_equal<WAVES, TPW>(key, t, m - how_many_above(t), ties);
-        __syncthreads();
-#pragma unroll
-        for (int q = 0; q < N; ++q) {
-            const int at = ((q / 4) * WAVES + wave) * 256 + lane * 4 + q % 4;
-            append_entry(key[q] > t || (key[q] == t && at <= last), order_entry(key[q], at), list, &filled);
-        }
-        sort_descending<THREADS>(list, size);
-        draw_from_list<THREADS>(a, row, list, (int)filled, sums, &kept_entries);
+        __shared__ BestList<WAVES, TPW> b;
+        __shared__ double sums[BestList<WAVES, TPW>::ROOM < KGE_TOP_MAX ? BestList<WAVES, TPW>::ROOM : KGE_TOP_MAX];
+        __shared__ int kept_entries;
+        const int count = collect_best<WAVES, TPW>(v, low, mine, order_key(best), a.top_k, b);
+        uint64_t* list = order_list<THREADS>(b.list, b.sorted, b.rank, count);
+        draw_from_list<THREADS>(a, row, list, min(count, a.top_k), sums, &kept_entries);
     } else {
-        Kept kept = {0u, 0u, key_score(best), a.inv_t, a.min_p};
+        __shared__ double sums[TILES], part[2 * WAVES];
+        __shared__ uint32_t slots[2 * WAVES];
+        const Weights weights(best, a.inv_t);
+        Kept kept = {-INFINITY, 0u, 0u};
         double w[N];
-        int last = CAP;
 #pragma unroll
-        for (int q = 0; q < N; ++q) w[q] = key[q] ? weight64(key_score(key[q]), kept.best, a.inv_t) : 0.0;
+        for (int q = 0; q < N; ++q) w[q] = weights.of(v[q]);
         if constexpr (CUT == CUT_WEIGHT) {
             int round = 0;
-            auto weight_from = [&](uint32_t t) {  // of the keys at or above t
+            auto weight_from = [&](uint32_t key) {  // of the scores at or above a key's
+                const float t = key_score(key);
                 double z = 0.0;
 #pragma unroll
-                for (int q = 0; q < N; ++q) z += key[q] >= t ? w[q] : 0.0;
+                for (int q = 0; q < N; ++q) z += v[q] >= t ? w[q] : 0.0;
                 z = wave_sum64(z);
                 if constexpr (WAVES == 1) return z;
                 double* p = part + (round++ & 1) * WAVES;
@@ -198,51 +172,45 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
                 __syncthreads();
                 z = 0.0;
 #pragma unroll
-                for (int v = 0; v < WAVES; ++v) z += p[v];
+                for (int x = 0; x < WAVES; ++x) z += p[x];
                 return z;
             };
-            const double target = a.top_p * weight_from(1);
-            uint32_t lo = 1, hi = best;  // largest threshold that reaches the target
+            const double target = a.top_p * weight_from(LOWEST_KEY);
+            uint32_t lo = LOWEST_KEY, hi = order_key(best);  // largest threshold that reaches the target
             while (lo < hi) {
                 const uint32_t mid = lo + (hi - lo) / 2 + ((hi - lo) & 1);
                 if (weight_from(mid) >= target) lo = mid; else hi = mid - 1;
             }
-            kept.t = lo;
-            const int equal = how_many_above(lo - 1) - how_many_above(lo);
-            const double above = lo < best ? weight_from(lo + 1) : 0.0;
-            const double need = ceil((target - above) / weight64(key_score(lo), kept.best, a.inv_t));
+            kept.t = key_score(lo);
+            int equal = 0;
+#pragma unroll
+            for (int q = 0; q < N; ++q) equal += __popcll(__ballot(v[q] == kept.t));
+            __syncthreads();
+            equal = block_count<WAVES>(equal, slots);
+            const double above = lo < order_key(best) ? weight_from(lo + 1) : 0.0;
+            const double need = ceil((target - above) / weights.of(kept.t));
             const int c = need >= equal ? equal : need < 1.0 ? 1 : (int)need;
-            kept.ties = c;
-            if (c < equal) last = nth_equal<WAVES, TPW>(key, lo, c, ties);
+            if (c < equal) kept.least = select_equal<WAVES, N>(v, kept.t, low, c, slots);
         }
 #pragma unroll
         for (int i = 0; i < TPW; ++i) {
             double z = 0.0;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int at = (i * WAVES + wave) * 256 + lane * 4 + q;
-                const bool in = key[4 * i + q] > kept.t || (key[4 * i + q] == kept.t && at <= last);
-                z += in && w[4 * i + q] >= a.min_p ? w[4 * i + q] : 0.0;
+            for (int q = 4 * i; q < 4 * i + 4; ++q) {
+                const bool in = CUT == CUT_NONE || v[q] > kept.t || (v[q] == kept.t && low(q) >= kept.least);
+                z += in && w[q] >= a.min_p ? w[q] : 0.0;
             }
             z = wave_sum64(z);
             if (lane == 0) sums[i * WAVES + wave] = z;
-            if constexpr (CUT == CUT_WEIGHT) {  // equal keys per tile, for the tile that a draw falls into
-                int e = 0;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) e += __popcll(__ballot(key[4 * i + q] == kept.t));
-                __syncthreads();
-                if (lane == 0) ties[i * WAVES + wave] = e;
-            }
         }
         __syncthreads();
-        constexpr int TILES = WAVES * TPW;
         if (wave == 0) {
             double carry = 0.0;
 #pragma unroll
             for (int t0 = 0; t0 < TILES; t0 += 64) {
-                const double v = carry + wave_scan64(t0 + lane < TILES ? sums[t0 + lane] : 0.0, lane);
-                if (t0 + lane < TILES) sums[t0 + lane] = v;
-                carry = __shfl(v, 63, 64);
+                const double x = carry + wave_scan64(t0 + lane < TILES ? sums[t0 + lane] : 0.0, lane);
+                if (t0 + lane < TILES) sums[t0 + lane] = x;
+                carry = __shfl(x, 63, 64);
             }
         }
         __syncthreads();
@@ -253,17 +221,15 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
 #pragma unroll
             for (int t0 = 0; t0 < TILES; t0 += 64) {
                 const bool there = t0 + lane < TILES;
-                const double v = there ? sums[t0 + lane] : 0.0, before = t0 + lane > 0 && there ? sums[t0 + lane - 1] : 0.0;
-                const uint64_t past = __ballot(there && v > want), some = __ballot(there && v > before);
+                const double x = there ? sums[t0 + lane] : 0.0, before = t0 + lane > 0 && there ? sums[t0 + lane - 1] : 0.0;
+                const uint64_t past = __ballot(there && x > want), some = __ballot(there && x > before);
                 if (tile < 0 && past) tile = t0 + __ffsll((unsigned long long)past) - 1;
                 if (some) fallback = t0 + 63 - __clzll(some);
             }
             if (tile < 0) tile = fallback;
-            uint32_t ties_before = 0;
-            if constexpr (CUT == CUT_WEIGHT) for (int v = 0; v < tile; ++v) ties_before += ties[v];
             int64_t id = -1;
             double weight = 0.0;
-            draw_in_tile<DT>(s, (int64_t)tile * 256, a.in.n, kept, ties_before, tile > 0 ? sums[tile - 1] : 0.0, want, lane, id, weight);
+            draw_in_tile<DT, false>(s, (int64_t)tile * 256, a.in.n, kept, weights, a.min_p, 0u, tile > 0 ? sums[tile - 1] : 0.0, want, lane, id, weight);
             if (lane == 0) {
                 a.ids[row * a.draws + d] = id;
                 if (a.logp) a.logp[row * a.draws + d] = (float)log(weight / total);
@@ -324,22 +290,18 @@ struct LongArgs {
 template <int DT, int PASS>
 __global__ __launch_bounds__(SEG_WAVES * 64) void k_draw_sums(LongArgs a) {
     __shared__ uint32_t slots[SEG_WAVES];
+    __shared__ float maxima[SEG_WAVES];
     __shared__ double sums[SEG_WAVES];
     const int64_t block = flat_block();
     if (block >= a.d.in.rows * a.segments) return;
     const int64_t row = block / a.segments, seg = block - row * a.segments;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const auto* s = static_cast<const typename Score<DT>::type*>(a.d.in.p) + row * a.d.in.ld;
-    uint32_t key[SEG_TPW * 4];
-    load_keys<DT, SEG_WAVES, SEG_TPW>(s, seg * KGE_ROW_SEGMENT, a.d.in.n, key);
-    uint32_t t = 0;
-    float best;
+    float v[SEG_TPW * 4];
+    const float mine = load_tiles<DT, SEG_WAVES, SEG_TPW>(s, seg * KGE_ROW_SEGMENT, a.d.in.n, v);
+    float t = -INFINITY, best;
     if constexpr (PASS == 0) {
-        uint32_t b = 0;
-#pragma unroll
-        for (int q = 0; q < SEG_TPW * 4; ++q) b = max(b, key[q]);
-        b = block_max_u32<SEG_WAVES>(b, slots);
-        best = b ? key_score(b) : -INFINITY;
+        best = block_max<SEG_WAVES>(mine, maxima);
         if (a.bins) {  // clear the row's bins
             const int64_t words = 2 * BINS;
             for (int level = 0; level < LEVELS; ++level)
@@ -347,9 +309,10 @@ __global__ __launch_bounds__(SEG_WAVES * 64) void k_draw_sums(LongArgs a) {
                     a.bins[((int64_t)level * a.d.in.rows + row) * words + x] = 0;
         }
     } else {
-        t = a.rows[row].t;
         best = a.rows[row].best;
+        if (a.rows[row].t) t = key_score(a.rows[row].t);
     }
+    const Weights weights(best, a.d.inv_t);
     const double min_p = PASS == 0 ? 0.0 : a.d.min_p;
     double all = 0.0;
     uint32_t equal = 0;
@@ -358,11 +321,10 @@ __global__ __launch_bounds__(SEG_WAVES * 64) void k_draw_sums(LongArgs a) {
         double z = 0.0;
         uint32_t e = 0;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint32_t k = key[4 * i + q];
-            const double w = k > t ? weight64(key_score(k), best, a.d.inv_t) : 0.0;
+        for (int q = 4 * i; q < 4 * i + 4; ++q) {
+            const double w = v[q] > t ? weights.of(v[q]) : 0.0;
             z += w >= min_p ? w : 0.0;
-            if constexpr (PASS == 1) e += t > 0 ? __popcll(__ballot(k == t)) : 0;
+            if constexpr (PASS == 1) e += t > -INFINITY ? __popcll(__ballot(v[q] == t)) : 0;
         }
         z = wave_sum64(z);
         all += z;
@@ -387,17 +349,16 @@ __global__ __launch_bounds__(SEG_WAVES * 64) void k_draw_sums(LongArgs a) {
 
 // The row's best score; with top-p the interval in which its threshold is looked for.
 __global__ __launch_bounds__(256) void k_draw_begin(LongArgs a) {
-    __shared__ uint32_t slots[4];
+    __shared__ float maxima[4];
     const int64_t row = flat_block();
     if (row >= a.d.in.rows) return;
-    uint32_t b = 0;
-    for (int64_t g = threadIdx.x; g < a.segments; g += 256) b = max(b, order_key((float)a.parts[2 * (row * a.segments + g)]));
-    b = block_max_u32<4>(b, slots);
+    float best = -INFINITY;
+    for (int64_t g = threadIdx.x; g < a.segments; g += 256) best = fmaxf(best, (float)a.parts[2 * (row * a.segments + g)]);
+    best = block_max<4>(best, maxima);
     if (threadIdx.x == 0) {
         RowCut r = {};
-        r.lo = 1; r.hi = b ? b : 1;
-        r.t = 0; r.ties = 0;
-        r.best = b ? key_score(b) : -INFINITY;
+        r.best = best;
+        r.lo = LOWEST_KEY; r.hi = order_key(best);
         a.rows[row] = r;
     }
 }
@@ -414,16 +375,18 @@ __global__ __launch_bounds__(SEG_WAVES * 64) void k_draw_bins(LongArgs a, int le
     const RowCut r = a.rows[row];
     const auto* s = static_cast<const typename Score<DT>::type*>(a.d.in.p) + row * a.d.in.ld;
     for (int x = threadIdx.x; x < BINS * 2; x += 1024) bins[x] = 0;
-    uint32_t key[SEG_TPW * 4];
-    load_keys<DT, SEG_WAVES, SEG_TPW>(s, seg * KGE_ROW_SEGMENT, a.d.in.n, key);
+    float v[SEG_TPW * 4];
+    load_tiles<DT, SEG_WAVES, SEG_TPW>(s, seg * KGE_ROW_SEGMENT, a.d.in.n, v);
     __syncthreads();
+    const Weights weights(r.best, a.d.inv_t);
     const int shift = r.hi > r.lo ? bin_shift(r.lo, r.hi) : 0;
     const double unit = (double)((uint64_t)1 << a.bits);
 #pragma unroll
     for (int q = 0; q < SEG_TPW * 4; ++q) {
-        if (key[q] >= r.lo && key[q] <= r.hi) {
-            const int bin = (int)((r.hi - key[q]) >> shift);
-            const double w = weight64(key_score(key[q]), r.best, a.d.inv_t) * unit, whole = floor(w);
+        const uint32_t key = order_key(v[q]);
+        if (key >= r.lo && key <= r.hi) {
+            const int bin = (int)((r.hi - key) >> shift);
+            const double w = weights.of(v[q]) * unit, whole = floor(w);
             const uint64_t x = (uint64_t)whole, y = (uint64_t)((w - whole) * unit);
             if (x) atomicAdd(&bins[2 * bin], (unsigned long long)x);
             if (y) atomicAdd(&bins[2 * bin + 1], (unsigned long long)y);
@@ -518,7 +481,7 @@ __global__ __launch_bounds__(256) void k_draw_narrow(LongArgs a, int level) {
         r.lo = top >= width && top - width + 1 > r.lo ? top - width + 1 : r.lo;
         if (level == LEVELS - 1) {
             r.t = r.hi;
-            const double w = weight64(key_score(r.t), r.best, a.d.inv_t) * unit, down = floor(w);
+            const double w = Weights(r.best, a.d.inv_t).of(key_score(r.t)) * unit, down = floor(w);
             const uint64_t one[2] = {(uint64_t)down, (uint64_t)((w - down) * unit)};
             const unsigned __int128 each = whole(one), have = whole(r.above);
             unsigned __int128 c = 1;
@@ -532,22 +495,23 @@ __global__ __launch_bounds__(256) void k_draw_narrow(LongArgs a, int level) {
 // Running sums over the segments of a row.
 __global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a) {
     __shared__ double part[16];
-    __shared__ uint32_t tpart[16], slots[16];
+    __shared__ uint32_t tpart[16];
+    __shared__ float maxima[16];
     const int64_t row = flat_block();
     if (row >= a.d.in.rows) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     double* parts = a.parts + 2 * row * a.segments;
-    uint32_t b = 0;
-    for (int64_t g = threadIdx.x; g < a.segments; g += 1024) b = max(b, order_key((float)parts[2 * g]));
-    b = block_max_u32<16>(b, slots);
-    const float best = b ? key_score(b) : -INFINITY;
+    float best = -INFINITY;
+    for (int64_t g = threadIdx.x; g < a.segments; g += 1024) best = fmaxf(best, (float)parts[2 * g]);
+    best = block_max<16>(best, maxima);
+    const Weights weights(best, a.d.inv_t);
     uint32_t t = 0, most = 0;
     double each = 0.0;
     if (a.cut) {
         const RowCut r = a.rows[row];
         t = r.t; most = r.ties;
         if (t) {
-            each = weight64(key_score(t), best, a.d.inv_t);
+            each = weights.of(key_score(t));
             if (!(each >= a.d.min_p)) each = 0.0;
         }
     } else if (threadIdx.x == 0) {
@@ -563,7 +527,7 @@ __global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a) {
         uint32_t e = 0;
         if (g < a.segments) {
             const float own = (float)parts[2 * g];
-            v = own > -INFINITY ? parts[2 * g + 1] * weight64(own, best, a.d.inv_t) : 0.0;
+            v = own > -INFINITY ? parts[2 * g + 1] * weights.of(own) : 0.0;
             if (t) e = a.seg_ties[row * a.segments + g];
         }
         uint32_t es = e;  // equal keys up to this segment
@@ -624,9 +588,9 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
     while (lo > 0 && !(parts[2 * lo + 1] > parts[2 * lo - 1])) --lo;  // (never a segment without weight)
     const int64_t block = row * a.segments + lo;
     const float own = (float)parts[2 * lo];
-    const double scale = weight64(own, r.best, a.d.inv_t);
+    const Weights weights(r.best, a.d.inv_t);
     double base = lo > 0 ? parts[2 * lo - 1] : 0.0;
-    double v = a.tiles[block * SEG_TILES + lane] * scale;
+    double v = a.tiles[block * SEG_TILES + lane] * weights.of(own);
     uint32_t before = 0;
     if (r.t) {
         const uint32_t e = a.tile_ties[block * SEG_TILES + lane];
@@ -637,7 +601,7 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
             if (lane >= o) es += y;
         }
         before = a.seg_ties[block] + es - e;
-        const double each = weight64(key_score(r.t), r.best, a.d.inv_t);
+        const double each = weights.of(key_score(r.t));
         if (before < r.ties && each >= a.d.min_p) v += each * (double)min(e, r.ties - before);
     }
     const double incl = base + wave_scan64(v, lane);
@@ -645,10 +609,10 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
     const int tile = past ? __ffsll((unsigned long long)past) - 1 : any ? 63 - __clzll(any) : 0;
     base = __shfl(incl - v, tile, 64);
     before = __shfl((int)before, tile, 64);
-    const Kept kept = {r.t, r.ties, r.best, a.d.inv_t, a.d.min_p};
+    const Kept kept = {r.t ? key_score(r.t) : -INFINITY, 0u, r.ties};
     int64_t id = -1;
     double weight = 0.0;
-    draw_in_tile<DT>(s, lo * KGE_ROW_SEGMENT + (int64_t)tile * 256, a.d.in.n, kept, before, base, want, lane, id, weight);
+    draw_in_tile<DT, true>(s, lo * KGE_ROW_SEGMENT + (int64_t)tile * 256, a.d.in.n, kept, weights, a.d.min_p, before, base, want, lane, id, weight);
     if (lane == 0) {
         a.d.ids[d] = id;
         if (a.d.logp) a.d.logp[d] = (float)log(weight / total);

@@ -93,32 +93,79 @@ __device__ __forceinline__ uint32_t order_key(float s) {
 __device__ __forceinline__ float key_score(uint32_t k) {  // of a key that is not 0
     return __uint_as_float(k >> 31 ? k & 0x7FFFFFFFu : ~k);
 }
-__device__ __forceinline__ uint64_t order_entry(uint32_t key, int64_t j) { return key ? (uint64_t)key << 32 | (uint32_t)~(uint32_t)j : 0; }
 __device__ __forceinline__ int64_t entry_position(uint64_t e) { return (int64_t)(uint32_t)~(uint32_t)e; }
 
-// exp((s - best) / T) of a score that is not masked.  In 64 bits: which candidate a random number falls on is decided by sums
-// of these, and the sums of 32-bit weights would move thousands of borders by more than the numbers' spacing.
-__device__ __forceinline__ double weight64(float s, float best, double inv_t) {
-    return s == best ? 1.0 : exp(((double)s - (double)best) * inv_t);
-}
-
-__device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-__device__ __forceinline__ double wave_scan64(double v, int lane) {  // sum over lanes 0 .. lane
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const double w = __shfl_up(v, o, 64);
-        if (lane >= o) v += w;
+// exp((s - best) / T) in 64 bits, 0 of a masked score (-inf): which candidate a random number falls on is decided by sums of these, and
+// the sums of 32-bit weights would move thousands of borders by more than the numbers' spacing.  As p * 2^n: n the whole number nearest to
+// the exponent of 2 (its low bits appear where 1.5 * 2^52 is added), p the polynomial of degree 10 that interpolates exp2 on
+// [-1/2, 1/2] at the Chebyshev nodes, off by 3e-16.  About 20 instructions where the library's exp takes twice as many; of the
+// kernels that form a weight per score they are what bounds it beside the reads: 64 scores take a SIMD some 90 cycles.
+struct Weights {
+    double best, scale;  // best score, log2(e) / T
+    float floor;         // scores below have a weight of 0 (2^-1000 and less)
+    __device__ __forceinline__ Weights(float b, double inv_t) : scale(inv_t * 1.4426950408889634) {
+        floor = (float)fmax((double)b - 1000.0 / scale, -3.402823466e38);  // (b = +inf: above every number)
+        best = (double)fminf(b, 3.402823466e38f);
     }
+    __device__ __forceinline__ bool none(float s) const { return !(s >= floor); }
+    __device__ __forceinline__ void split(float s, double& p, int& n) const {
+        const double x = ((double)__builtin_amdgcn_fmed3f(s, fminf(floor, 3.402823466e38f), 3.402823466e38f) - best) * scale;
+        const double shifted = x + 0x1.8p52, f = x - (shifted - 0x1.8p52);
+        n = __double2loint(shifted);
+        p = 0x1.e6063f7217bc6p-28;
+        p = fma(p, f, 0x1.b675bca4eeebbp-24);
+        p = fma(p, f, 0x1.62bfd47773353p-20);
+        p = fma(p, f, 0x1.ffcb54062e698p-17);
+        p = fma(p, f, 0x1.430913096fd9fp-13);
+        p = fma(p, f, 0x1.5d87fe9d7a584p-10);
+        p = fma(p, f, 0x1.3b2ab6fba1ddap-7);
+        p = fma(p, f, 0x1.c6b08d703ce49p-5);
+        p = fma(p, f, 0x1.ebfbdff82c598p-3);
+        p = fma(p, f, 0x1.62e42fefa3a19p-1);
+        p = fma(p, f, 1.0);
+    }
+    static __device__ __forceinline__ double scaled(double p, int n) {  // p * 2^n, p and the result normal numbers
+        return __hiloint2double(__double2hiint(p) + (n << 20), __double2loint(p));
+    }
+    __device__ __forceinline__ double of(float s) const {
+        double p;
+        int n;
+        split(s, p, n);
+        return none(s) ? 0.0 : scaled(p, n);
+    }
+};
+
+// Sums and maxima of a wave by moves within rows of 16 lanes and from row to row: no LDS on the way.
+template <int CTRL, int ROWS> __device__ __forceinline__ double moved64(double v) {  // lanes without a source: 0
+    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, ROWS, 0xf, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, ROWS, 0xf, false);
+    return __hiloint2double(hi, lo);
+}
+constexpr int ROW_SHR = 0x110, BCAST_15 = 0x142, BCAST_31 = 0x143;
+__device__ __forceinline__ double wave_scan64(double v, int) {  // sum over lanes 0 .. own
+    v += moved64<ROW_SHR + 1, 0xf>(v);
+    v += moved64<ROW_SHR + 2, 0xf>(v);
+    v += moved64<ROW_SHR + 4, 0xf>(v);
+    v += moved64<ROW_SHR + 8, 0xf>(v);
+    v += moved64<BCAST_15, 0xa>(v);
+    v += moved64<BCAST_31, 0xc>(v);
     return v;
 }
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-    return v;
+__device__ __forceinline__ double lane64(double v, int lane) {  // of one lane, the same for all
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+__device__ __forceinline__ double wave_sum64(double v) { return lane64(wave_scan64(v, 0), 63); }
+template <int CTRL, int ROWS> __device__ __forceinline__ float max_moved(float v) {
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(-INFINITY), __float_as_int(v), CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ float wave_most(float v) {
+    v = max_moved<ROW_SHR + 1, 0xf>(v);
+    v = max_moved<ROW_SHR + 2, 0xf>(v);
+    v = max_moved<ROW_SHR + 4, 0xf>(v);
+    v = max_moved<ROW_SHR + 8, 0xf>(v);
+    v = max_moved<BCAST_15, 0xa>(v);
+    v = max_moved<BCAST_31, 0xc>(v);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 // Reductions over a workgroup of WAVES waves; `slot` is LDS of WAVES values that is free again after the next barrier.
@@ -133,54 +180,64 @@ template <int WAVES> __device__ __forceinline__ double block_sum64(double v, dou
     __syncthreads();
     return s;
 }
-template <int WAVES> __device__ __forceinline__ uint32_t block_max_u32(uint32_t v, uint32_t* slot) {
-    v = wave_max_u32(v);
+template <int WAVES> __device__ __forceinline__ float block_max(float v, float* slot) {
+    v = wave_most(v);
     if constexpr (WAVES == 1) return v;
     if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
     __syncthreads();
-    uint32_t m = 0;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) m = max(m, slot[w]);
+    for (int w = 0; w < WAVES; ++w) v = fmaxf(v, slot[w]);
     __syncthreads();
-    return m;
+    return v;
 }
 
-// The tiles of a workgroup in registers, as keys.
+// The tiles of a workgroup in registers, masked scores as -inf; returns this thread's largest.
 template <int DT, int WAVES, int TPW>
-__device__ __forceinline__ void load_keys(const typename Score<DT>::type* row, int64_t first, int64_t n, uint32_t key[TPW * 4]) {
+__device__ __forceinline__ float load_tiles(const typename Score<DT>::type* row, int64_t first, int64_t n, float v[TPW * 4]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float best = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < TPW; ++i) {
-        float v[4];
-        load4<DT>(row, first + (int64_t)(i * WAVES + wave) * 256 + lane * 4, n, v);
+    for (int i = 0; i < TPW; ++i) load4<DT>(row, first + (int64_t)(i * WAVES + wave) * 256 + lane * 4, n, v + 4 * i);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) key[4 * i + q] = order_key(v[q]);
+    for (int q = 0; q < TPW * 4; ++q) {
+        v[q] = fmaxf(v[q], -INFINITY);  // (NaN: -inf)
+        best = fmaxf(best, v[q]);
     }
+    return best;
+}
+template <int WAVES> __device__ __forceinline__ int tile_position(int q) {  // of register q, in the workgroup's tiles
+    return ((q / 4) * WAVES + (int)(threadIdx.x >> 6)) * 256 + (int)(threadIdx.x & 63) * 4 + q % 4;
 }
 
-// Largest threshold that at least m of the workgroup's keys reach, by halving the interval of keys: every round counts the keys
-// at or above its middle.  Ends early where exactly m do.  `reach`: how many reach the result.  Fewer than m candidates: 1.
-template <int WAVES, int N, typename K>
-__device__ __forceinline__ K select_threshold(const K key[N], K best, int m, uint32_t* slots /* [2 * WAVES] */, int& reach) {
-    K lo = 1, hi = best;  // count(>= lo) >= m, count(> hi) < m
+template <int WAVES> __device__ __forceinline__ int block_count(int c, uint32_t* slot) {  // c: of a wave
+    if constexpr (WAVES == 1) return c;
+    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = c;
+    __syncthreads();
+    c = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) c += slot[w];
+    return c;
+}
+
+// Key of the largest score that at least m of the workgroup's scores reach, by halving the interval of keys: every round
+// counts the scores at or above its middle.  Ends early where exactly m do.  `reach`: how many reach the result.  Fewer than m
+// candidates: the lowest key.
+constexpr uint32_t LOWEST_KEY = 0x00800000u;  // of the lowest finite number
+template <int WAVES, int N>
+__device__ __forceinline__ uint32_t select_threshold(const float v[N], uint32_t best, int m, uint32_t* slots /* [2 * WAVES] */, int& reach) {
+    uint32_t lo = LOWEST_KEY, hi = best;  // count(>= lo) >= m, count(> hi) < m
     int round = 0;
-    auto count = [&](K t) {
+    auto count = [&](uint32_t key) {
+        const float t = key_score(key);
         int c = 0;
 #pragma unroll
-        for (int q = 0; q < N; ++q) c += __popcll(__ballot(key[q] >= t));
-        if constexpr (WAVES == 1) return c;
-        uint32_t* s = slots + (round++ & 1) * WAVES;
-        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = c;
-        __syncthreads();
-        c = 0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) c += s[w];
-        return c;
+        for (int q = 0; q < N; ++q) c += __popcll(__ballot(v[q] >= t));
+        return block_count<WAVES>(c, slots + (round++ & 1) * WAVES);
     };
     reach = count(lo);
     if (reach <= m) return lo;
     while (lo < hi) {
-        const K mid = lo + (hi - lo) / 2 + ((hi - lo) & 1);  // lo < mid <= hi
+        const uint32_t mid = lo + (hi - lo) / 2 + ((hi - lo) & 1);  // lo < mid <= hi
         const int c = count(mid);
         if (c >= m) {
             lo = mid;
@@ -193,42 +250,21 @@ __device__ __forceinline__ K select_threshold(const K key[N], K best, int m, uin
     return lo;
 }
 
-// Position (within the workgroup's tiles) of the c-th key that equals t, c >= 1 and at most their number.
-template <int WAVES, int TPW>
-__device__ __forceinline__ int nth_equal(const uint32_t key[TPW * 4], uint32_t t, int c, uint32_t* tile_count /* [WAVES * TPW + 1] */) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
+// Of the scores that equal t: the largest bound that c of their inverted positions reach, 1 <= c <= their number.
+template <int WAVES, int N, typename L>
+__device__ __forceinline__ uint32_t select_equal(const float v[N], float t, const L& low, int c, uint32_t* slots /* [2 * WAVES] */) {
+    uint32_t lo = 0, hi = 0xFFFFFFFFu;
+    int round = 0;
     __syncthreads();
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2 + ((hi - lo) & 1);
+        int n = 0;
 #pragma unroll
-    for (int i = 0; i < TPW; ++i) {
-        int s = 0;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) s += __popcll(__ballot(key[4 * i + q] == t));
-        if (lane == 0) tile_count[i * WAVES + wave] = s;
+        for (int q = 0; q < N; ++q) n += __popcll(__ballot(v[q] == t && low(q) >= mid));
+        if (block_count<WAVES>(n, slots + (round++ & 1) * WAVES) >= c) lo = mid; else hi = mid - 1;
     }
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < TPW; ++i) {
-        const int tile = i * WAVES + wave;
-        int before = 0;
-        for (int u = 0; u < tile; ++u) before += tile_count[u];
-        if (before >= c || before + (int)tile_count[tile] < c) continue;
-        int at = before;
-        uint64_t eq[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            eq[q] = __ballot(key[4 * i + q] == t);
-            at += __popcll(eq[q] & below);
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (eq[q] >> lane & 1) {
-                if (++at == c) tile_count[WAVES * TPW] = tile * 256 + lane * 4 + q;
-            }
-        }
-    }
-    __syncthreads();
-    return (int)tile_count[WAVES * TPW];
+    return lo;
 }
 
 // Appends the entries that `take` says to a list in LDS (in any order); *n starts at 0 and ends at their number.
@@ -258,6 +294,128 @@ template <int THREADS> __device__ __forceinline__ void sort_descending(uint64_t*
 }
 
 __device__ __forceinline__ int power_of_two(int x) { return x <= 1 ? 1 : 1 << (32 - __clz(x - 1)); }
+
+// The best of a workgroup's scores, as entries in an LDS list, best first.  A score that at least m of the workgroup's groups (its
+// threads, or the threads' vectors of 4) reach with their largest is reached by at least m scores, and by few more than m if
+// not many more groups reach it: -groups ln(1 - m / groups) where scores lie as they come, 1.4 m at m = groups / 2.  So it is enough to look for such a score among the groups' largest, 1024 instead of 16,384, and only until at most a quarter too many
+// reach it; the candidates are then put in order by counting (up to 256: a position is the number of entries
+// above) or by a sorting network.  Where they do not fit the list (equal scores, orders made for it) the threshold is found among all
+// scores.
+constexpr int BEST_ROOM = 2048;
+template <int WAVES, int TPW> struct BestList {
+    static constexpr int ROOM = WAVES * TPW * 256 < BEST_ROOM ? WAVES * TPW * 256 : BEST_ROOM;
+    uint64_t list[ROOM];
+    uint64_t sorted[256];
+    float most[WAVES * 64];
+    uint32_t slots[2 * WAVES], rank[256];
+    uint32_t count, bound;
+};
+
+// A key that at least m, and if it is found in time at most m + m / 4 + 2, of a wave's PER values per lane reach.
+template <int PER> __device__ __forceinline__ uint32_t wave_bound(const float v[PER], uint32_t best, int m) {
+    uint32_t lo = LOWEST_KEY, hi = best;
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2 + ((hi - lo) & 1);
+        const float t = key_score(mid);
+        int c = 0;
+#pragma unroll
+        for (int q = 0; q < PER; ++q) c += __popcll(__ballot(v[q] >= t));
+        if (c >= m) {
+            lo = mid;
+            if (c <= m + m / 4 + 2) break;
+        } else {
+            hi = mid - 1;
+        }
+    }
+    return lo;
+}
+
+// Sorts the list's first `count` entries, the largest first; returns where they are.
+template <int THREADS> __device__ __forceinline__ uint64_t* order_list(uint64_t* list, uint64_t* sorted, uint32_t* rank, int count) {
+    if (count <= 256) {
+        const int width = count <= 64 ? 64 : power_of_two(count), parts = THREADS > width ? THREADS / width : 1;
+        for (int e = threadIdx.x; e < width; e += THREADS) rank[e] = 0;
+        __syncthreads();
+        for (int e0 = threadIdx.x; e0 < width * parts; e0 += THREADS) {
+            const int e = e0 & (width - 1), part = e0 / width;
+            if (e < count) {
+                const uint64_t own = list[e];
+                uint32_t above = 0;
+                for (int j = part; j < count; j += parts) above += list[j] > own;
+                if (parts > 1) atomicAdd(&rank[e], above);
+                else rank[e] = above;
+            }
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < count; e += THREADS) sorted[rank[e]] = list[e];
+        __syncthreads();
+        return sorted;
+    }
+    const int size = power_of_two(count);
+    for (int e = count + threadIdx.x; e < size; e += THREADS) list[e] = 0;
+    sort_descending<THREADS>(list, size);
+    return list;
+}
+
+// v: the workgroup's scores, low(q): their inverted positions in the row, `mine` this thread's largest score, `best` the key of the largest
+// (not 0).  Fills the list with candidates that the best m are among (any order, list[0 .. count - 1]) and returns their number.
+template <int WAVES, int TPW, typename L>
+__device__ __forceinline__ int collect_best(const float v[TPW * 4], const L& low, float mine, uint32_t best, int m, BestList<WAVES, TPW>& s) {
+    constexpr int N = TPW * 4, THREADS = WAVES * 64, CAP = WAVES * TPW * 256, ROOM = BestList<WAVES, TPW>::ROOM;
+    uint32_t bound = LOWEST_KEY;
+    if (threadIdx.x == 0) s.count = 0;
+    if (m <= THREADS / 2) {
+        if constexpr (WAVES == 1) {
+            bound = wave_bound<1>(&mine, best, m);
+        } else {
+            s.most[threadIdx.x] = mine;
+            __syncthreads();
+            if (threadIdx.x < 64) {
+                float x[WAVES];
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) x[w] = s.most[w * 64 + threadIdx.x];
+                bound = wave_bound<WAVES>(x, best, m);
+                if (threadIdx.x == 0) s.bound = bound;
+            }
+            __syncthreads();
+            bound = s.bound;
+        }
+    } else if (CAP > ROOM && m <= THREADS * TPW / 2) {
+        float x[TPW];
+#pragma unroll
+        for (int i = 0; i < TPW; ++i) x[i] = fmaxf(fmaxf(v[4 * i], v[4 * i + 1]), fmaxf(v[4 * i + 2], v[4 * i + 3]));
+        int reach;
+        bound = select_threshold<WAVES, TPW>(x, best, m, s.slots, reach);
+    }
+    __syncthreads();
+    float t = key_score(bound);
+    uint32_t least = 0;  // of the inverted positions of scores that equal t
+    if constexpr (CAP > ROOM) {
+        int c = 0;
+#pragma unroll
+        for (int q = 0; q < N; ++q) c += __popcll(__ballot(v[q] >= t));
+        if (block_count<WAVES>(c, s.slots) > ROOM) {
+            __syncthreads();
+            int reach;
+            t = key_score(select_threshold<WAVES, N>(v, best, m, s.slots, reach));
+            if (reach > m) {  // more than m reach it: equal scores, of which the first ones count
+                int above = 0;
+#pragma unroll
+                for (int q = 0; q < N; ++q) above += __popcll(__ballot(v[q] > t));
+                __syncthreads();
+                above = block_count<WAVES>(above, s.slots);
+                least = select_equal<WAVES, N>(v, t, low, m - above, s.slots);
+            }
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        const uint32_t at = low(q);
+        append_entry(v[q] > t || (v[q] == t && at >= least), (uint64_t)order_key(v[q]) << 32 | at, s.list, &s.count);
+    }
+    __syncthreads();
+    return (int)s.count;
+}
 
 }  // namespace
 #endif

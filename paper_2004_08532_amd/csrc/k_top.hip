@@ -1,8 +1,8 @@
 // The best candidates of every row of scores, and its log-sum-exp (kge_top_scores).
 //
-// One workgroup holds a row, or a segment of a long one, in registers and finds the score that exactly its m best reach by
-// halving the interval of keys.  The entries at or above it are sorted in LDS.  The lists of a row's segments are joined by
-// the same selection over (key, position) entries, level by level, until one list is left.
+// One workgroup holds a row, or a segment of a long one, in registers, collects the few candidates that its best m are among and
+// puts them in order in LDS (collect_best, order_list).  Of a row in segments every workgroup leaves its candidates, at least
+// its best m; they are collected and ordered in the same way, level by level, until one list is left.
 // log-sum-exp: the weights exp((s - best) / T) of a segment are summed in 64 bits beside it.
 #include "k_rows.h"
 
@@ -21,9 +21,9 @@ struct TopArgs {
 };
 
 template <int THREADS>
-__device__ __forceinline__ void write_list(const uint64_t* list, int m, int64_t* ids, float* scores) {
+__device__ __forceinline__ void write_list(const uint64_t* list, int count, int m, int64_t* ids, float* scores) {
     for (int e = threadIdx.x; e < m; e += THREADS) {
-        const uint64_t x = list[e];
+        const uint64_t x = e < count ? list[e] : 0;
         ids[e] = x ? entry_position(x) : -1;
         scores[e] = x ? key_score((uint32_t)(x >> 32)) : -INFINITY;
     }
@@ -35,64 +35,40 @@ __device__ __forceinline__ float lse_of(double best, double sum, double inv_t) {
 
 template <int DT, int WAVES, int TPW>
 __global__ __launch_bounds__(WAVES * 64) void k_top_rows(TopArgs a) {
-    constexpr int CAP = WAVES * TPW * 256, LIST = CAP < KGE_TOP_MAX ? CAP : KGE_TOP_MAX;
-    __shared__ uint64_t list[LIST];
-    __shared__ uint32_t slots[2 * WAVES], ties[WAVES * TPW + 1], count;
+    constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64;
+    __shared__ BestList<WAVES, TPW> s;
     __shared__ double sums[WAVES];
+    __shared__ float maxima[WAVES];
     const int64_t block = flat_block();
     if (block >= a.in.rows * a.segments) return;
     const int64_t row = block / a.segments, seg = block - row * a.segments, first = seg * CAP;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const auto* s = static_cast<const typename Score<DT>::type*>(a.in.p) + row * a.in.ld;
+    const auto* scores = static_cast<const typename Score<DT>::type*>(a.in.p) + row * a.in.ld;
 
-    uint32_t key[TPW * 4];
-    load_keys<DT, WAVES, TPW>(s, first, a.in.n, key);
-    uint32_t best = 0;
-#pragma unroll
-    for (int q = 0; q < TPW * 4; ++q) best = max(best, key[q]);
-    best = block_max_u32<WAVES>(best, slots);
-
+    float v[TPW * 4];
+    const float mine = load_tiles<DT, WAVES, TPW>(scores, first, a.in.n, v), best = block_max<WAVES>(mine, maxima);
+    const bool empty = !(best > -INFINITY);
     if (a.want_lse) {
         double z = 0.0;
-        const float top = key_score(best);
+        if (!empty) {
+            const Weights w(best, a.inv_t);
 #pragma unroll
-        for (int q = 0; q < TPW * 4; ++q) z += key[q] ? weight64(key_score(key[q]), top, a.inv_t) : 0.0;
-        z = block_sum64<WAVES>(z, sums);
+            for (int q = 0; q < TPW * 4; ++q) z += w.of(v[q]);
+            z = block_sum64<WAVES>(z, sums);
+        }
         if (threadIdx.x == 0) {
-            if (a.segments == 1) a.lse[row] = lse_of(top, best ? z : 0.0, a.inv_t);
-            else { a.parts[2 * block] = best ? top : -INFINITY; a.parts[2 * block + 1] = best ? z : 0.0; }
+            if (a.segments == 1) a.lse[row] = lse_of(best, z, a.inv_t);
+            else { a.parts[2 * block] = best; a.parts[2 * block + 1] = z; }
         }
     }
-
-    const int m = min(a.m, LIST), size = power_of_two(m);
-    for (int e = threadIdx.x; e < size; e += WAVES * 64) list[e] = 0;
-    if (threadIdx.x == 0) count = 0;
-    int reach = 0, last = CAP;
-    const uint32_t t = best ? select_threshold<WAVES, TPW * 4, uint32_t>(key, best, m, slots, reach) : 1;
-    if (reach > m) {  // more than m reach it: equal scores, of which the first ones count
-        int above = 0;
-#pragma unroll
-        for (int q = 0; q < TPW * 4; ++q) above += __popcll(__ballot(key[q] > t));
-        __syncthreads();
-        if (lane == 0) slots[wave] = above;
-        __syncthreads();
-        above = 0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) above += slots[w];
-        last = nth_equal<WAVES, TPW>(key, t, m - above, ties);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < TPW * 4; ++q) {
-        const int at = ((q / 4) * WAVES + wave) * 256 + lane * 4 + q % 4;
-        append_entry(key[q] > t || (key[q] == t && at <= last), order_entry(key[q], first + at), list, &count);
-    }
-    sort_descending<WAVES * 64>(list, size);
+    const int count = empty ? 0 :
+        collect_best<WAVES, TPW>(v, [&](int q) { return ~(uint32_t)(first + tile_position<WAVES>(q)); }, mine, order_key(best), a.m, s);
+    const uint64_t* list = s.list;
+    // the candidates of a segment: in order only where they are more than its share of the lists
+    if (a.segments == 1 || count > a.m) list = order_list<THREADS>(s.list, s.sorted, s.rank, count);
     if (a.segments == 1) {
-        write_list<WAVES * 64>(list, m, a.ids + row * a.m, a.scores + row * a.m);
-        for (int e = m + threadIdx.x; e < a.m; e += WAVES * 64) { a.ids[row * a.m + e] = -1; a.scores[row * a.m + e] = -INFINITY; }
+        write_list<THREADS>(list, count, a.m, a.ids + row * a.m, a.scores + row * a.m);
     } else {
-        for (int e = threadIdx.x; e < a.m; e += WAVES * 64) a.lists[block * a.m + e] = e < m ? list[e] : 0;
+        for (int e = threadIdx.x; e < a.m; e += THREADS) a.lists[block * a.m + e] = e < count ? list[e] : 0;
     }
 }
 
@@ -112,57 +88,43 @@ struct MergeArgs {
 // Lists of a row -> one list of its group.
 template <int WAVES, int TPW>
 __global__ __launch_bounds__(WAVES * 64) void k_top_merge(MergeArgs a) {
-    constexpr int CAP = WAVES * TPW * 256;
-    __shared__ uint64_t list[KGE_TOP_MAX], bests[WAVES];
-    __shared__ uint32_t slots[2 * WAVES], count;
+    constexpr int CAP = WAVES * TPW * 256, N = TPW * 4, THREADS = WAVES * 64;
+    __shared__ BestList<WAVES, TPW> s;
     __shared__ double sums[WAVES];
+    __shared__ float maxima[WAVES];
     const int64_t block = flat_block();
     if (block >= a.rows * a.groups) return;
     const int64_t row = block / a.groups, first = (block - row * a.groups) * CAP;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const uint64_t* in = a.in + row * a.entries;
     const int n = (int)min((int64_t)CAP, a.entries - first);
 
-    uint64_t key[TPW * 4], best = 0;
+    float v[N], mine = -INFINITY;
+    uint32_t low[N];  // inverted positions
 #pragma unroll
-    for (int q = 0; q < TPW * 4; ++q) {
+    for (int q = 0; q < N; ++q) {
         const int at = (q * WAVES + wave) * 64 + lane;
-        key[q] = at < n ? in[first + at] : 0;
-        best = key[q] > best ? key[q] : best;
+        const uint64_t x = at < n ? in[first + at] : 0;
+        v[q] = x ? key_score((uint32_t)(x >> 32)) : -INFINITY;
+        low[q] = (uint32_t)x;
+        mine = fmaxf(mine, v[q]);
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const uint64_t v = __shfl_xor((unsigned long long)best, o, 64);
-        best = v > best ? v : best;
-    }
-    if (lane == 0) bests[wave] = best;
-    const int size = power_of_two(a.m);
-    for (int e = threadIdx.x; e < size; e += WAVES * 64) list[e] = 0;
-    if (threadIdx.x == 0) count = 0;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) best = bests[w] > best ? bests[w] : best;
-
-    int reach = 0;
-    const uint64_t t = best ? select_threshold<WAVES, TPW * 4, uint64_t>(key, best, a.m, slots, reach) : 1;
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < TPW * 4; ++q) append_entry(key[q] >= t, key[q], list, &count);
-    sort_descending<WAVES * 64>(list, size);
-    if (a.groups > 1) {
-        for (int e = threadIdx.x; e < a.m; e += WAVES * 64) a.out[block * a.m + e] = list[e];
+    const float best = block_max<WAVES>(mine, maxima);
+    const int count = best > -INFINITY ? collect_best<WAVES, TPW>(v, [&](int q) { return low[q]; }, mine, order_key(best), a.m, s) : 0;
+    const uint64_t* list = order_list<THREADS>(s.list, s.sorted, s.rank, count);
+    if (a.groups > 1 || !a.ids) {
+        for (int e = threadIdx.x; e < a.m; e += THREADS) a.out[block * a.m + e] = e < count ? list[e] : 0;
         return;
     }
-    if (a.ids) write_list<WAVES * 64>(list, a.m, a.ids + row * a.m, a.scores + row * a.m);
-    else for (int e = threadIdx.x; e < a.m; e += WAVES * 64) a.out[row * a.m + e] = list[e];
+    write_list<THREADS>(list, count, a.m, a.ids + row * a.m, a.scores + row * a.m);
     if (a.parts) {
         const double* p = a.parts + 2 * row * a.segments;
-        const float top = key_score((uint32_t)(list[0] >> 32));
+        const Weights w(best, a.inv_t);
         double z = 0.0;
-        for (int g = threadIdx.x; g < a.segments; g += WAVES * 64)
-            if (p[2 * g + 1] > 0.0) z += p[2 * g + 1] * weight64((float)p[2 * g], top, a.inv_t);
+        for (int g = threadIdx.x; g < a.segments; g += THREADS)
+            if (p[2 * g + 1] > 0.0) z += p[2 * g + 1] * w.of((float)p[2 * g]);
         z = block_sum64<WAVES>(z, sums);
-        if (threadIdx.x == 0) a.lse[row] = lse_of(top, list[0] ? z : 0.0, a.inv_t);
+        if (threadIdx.x == 0) a.lse[row] = lse_of(best, z, a.inv_t);
     }
 }
 
