@@ -127,7 +127,286 @@ __device__ __forceinline__ void draw_from_list(const DrawArgs& a, int64_t row, u
     }
 }
 
-enum { CUT_NONE, CUT_WEIGHT, CUT_LIST };  // whole row or min-p; top-p; top-k (and what follows it)
+// The draws of a row whose tile sums a workgroup has in LDS.  sums[t]: of tile t, relative to best[t] (a row's best where that is null).
+template <int DT, int WAVES, int TILES>
+__device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, const typename Score<DT>::type* s, int tiles, double* sums,
+                                                const float* tile_best, const Kept& kept, const Weights& weights, double min_p) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __syncthreads();
+    if (wave == 0) {  // running sums
+        double carry = 0.0;
+#pragma unroll
+        for (int t0 = 0; t0 < TILES; t0 += 64) {
+            const int t = t0 + lane;
+            double x = t < tiles ? sums[t] : 0.0;
+            if (tile_best && t < tiles) x = tile_best[t] > -INFINITY ? x * weights.of(tile_best[t]) : 0.0;
+            x = carry + wave_scan64(x, lane);
+            if (t < tiles) sums[t] = x;
+            carry = lane64(x, 63);
+        }
+    }
+    __syncthreads();
+    const double total = sums[tiles - 1];
+    for (int d = wave; d < a.draws; d += WAVES) {
+        const double want = unit_number(a.u[row * a.draws + d]) * total;
+        int tile = -1, fallback = 0;
+#pragma unroll
+        for (int t0 = 0; t0 < TILES; t0 += 64) {
+            const bool there = t0 + lane < tiles;
+            const double x = there ? sums[t0 + lane] : 0.0, before = t0 + lane > 0 && there ? sums[t0 + lane - 1] : 0.0;
+            const uint64_t past = __ballot(there && x > want), some = __ballot(there && x > before);
+            if (tile < 0 && past) tile = t0 + __ffsll((unsigned long long)past) - 1;
+            if (some) fallback = t0 + 63 - __clzll(some);
+        }
+        if (tile < 0) tile = fallback;
+        int64_t id = -1;
+        double weight = 0.0;
+        draw_in_tile<DT, false>(s, (int64_t)tile * 256, a.in.n, kept, weights, min_p, 0u, tile > 0 ? sums[tile - 1] : 0.0, want, lane, id, weight);
+        if (lane == 0) {
+            a.ids[row * a.draws + d] = id;
+            if (a.logp) a.logp[row * a.draws + d] = (float)log(weight / total);
+        }
+    }
+}
+
+// Rows of which nothing is left out: a wave works through its tiles, each relative to its own best score.
+template <int DT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void k_draw_whole(DrawArgs a) {
+    constexpr int TILES = KGE_ROW_RESIDENT / 256;
+    __shared__ double sums[TILES];
+    __shared__ float bests[TILES], maxima[WAVES];
+    const int64_t row = flat_block();
+    if (row >= a.in.rows) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tiles = (int)((a.in.n + 255) / 256);
+    const auto* s = static_cast<const typename Score<DT>::type*>(a.in.p) + row * a.in.ld;
+    float most = -INFINITY;
+    for (int t0 = wave; t0 < tiles; t0 += 4 * WAVES) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load4<DT>(s, (int64_t)(t0 + i * WAVES) * 256 + lane * 4, a.in.n, v + 4 * i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int q = 4 * i; q < 4 * i + 4; ++q) v[q] = fmaxf(v[q], -INFINITY);
+            const float best = wave_most(fmaxf(fmaxf(v[4 * i], v[4 * i + 1]), fmaxf(v[4 * i + 2], v[4 * i + 3])));
+            const Weights w(best, a.inv_t);
+            const double z = wave_sum64((w.of(v[4 * i]) + w.of(v[4 * i + 1])) + (w.of(v[4 * i + 2]) + w.of(v[4 * i + 3])));
+            if (t0 + i * WAVES < tiles && lane == 0) { sums[t0 + i * WAVES] = z; bests[t0 + i * WAVES] = best; }
+            most = fmaxf(most, best);
+        }
+    }
+    most = block_max<WAVES>(most, maxima);
+    if (!(most > -INFINITY)) { write_empty<WAVES * 64>(a, row); return; }
+    const Kept kept = {-INFINITY, 0u, 0u};
+    draw_from_tiles<DT, WAVES, TILES>(a, row, s, tiles, sums, bests, kept, Weights(most, a.inv_t), 0.0);
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Where the weights of a row reach top-p.  The scores are counted into bins by what their weights sum to; the bin in which the running
+// sum, from the best score down, reaches the target becomes the interval for the next round, until its scores are few enough
+// to be put in order one by one or are all equal.  First round: bins of equal width between the best score and the lowest that matters
+// (40 T below it, or the lowest there is); then of equal numbers of keys.
+// Sums in bins are whole numbers (any order of the additions gives the same): p * 2^(n + bits - e) of a weight p * 2^n, with e the exponent at the
+// bin's (in later rounds: the interval's) upper end, so that a sum is as exact in the far bins as in the first.
+// ---------------------------------------------------------------------------------------------------------
+template <int LOG_BINS> struct BinRule {
+    static constexpr int BINS = 1 << LOG_BINS;
+    uint32_t lo, hi;   // interval of keys
+    int shift;         // keys per bin: 2^shift; negative: bins of equal width
+    float best, per;   // bins per unit of the score
+    double drop;       // exponents per bin
+    int top;           // exponent at the interval's upper end
+    __device__ __forceinline__ int bin(float s) const {
+        if (shift < 0) {
+            const float x = s < best ? (best - s) * per : 0.f;
+            return x < (float)(BINS - 1) ? (int)x : BINS - 1;
+        }
+        return (int)((hi - order_key(s)) >> shift);
+    }
+    __device__ __forceinline__ bool in(float s) const { return s >= key_score(lo) && s <= key_score(hi); }
+    __device__ __forceinline__ int exponent(int b) const { return shift < 0 ? (int)floor(-(double)b * drop) : top; }
+};
+
+// Rule of the first round.
+template <int LOG_BINS> __device__ __forceinline__ BinRule<LOG_BINS> first_bins(float best, float worst, double inv_t) {
+    constexpr int BINS = 1 << LOG_BINS;
+    BinRule<LOG_BINS> r;
+    r.lo = LOWEST_KEY; r.hi = order_key(best);
+    r.shift = -1; r.best = best;
+    const float range = fminf(best - worst, (float)fmin(40.0 / inv_t, 3e38));
+    r.per = range > 0.f ? (float)BINS / range : 0.f;
+    r.drop = r.per > 0.f ? inv_t * 1.4426950408889634 / (double)r.per : 0.0;
+    r.top = 0;
+    return r;
+}
+// Rule of the round that follows, for bin b.
+template <int LOG_BINS> __device__ __forceinline__ BinRule<LOG_BINS> next_bins(const BinRule<LOG_BINS>& r, int b, const Weights& w) {
+    BinRule<LOG_BINS> x = r;
+    if (r.shift < 0) {  // the keys whose bin is b: a larger key never has a larger bin
+        uint32_t lo = r.lo, hi = r.hi;
+        while (lo < hi) {  // the lowest key whose bin is at most b
+            const uint32_t mid = lo + (hi - lo) / 2;
+            if (r.bin(key_score(mid)) <= b) hi = mid; else lo = mid + 1;
+        }
+        x.lo = lo;
+        hi = r.hi;
+        while (lo < hi) {  // the highest whose bin is at least b
+            const uint32_t mid = lo + (hi - lo) / 2 + ((hi - lo) & 1);
+            if (r.bin(key_score(mid)) >= b) lo = mid; else hi = mid - 1;
+        }
+        x.hi = lo;
+    } else {
+        x.hi = r.hi - ((uint32_t)b << r.shift);
+        const uint32_t last = ((uint32_t)1 << r.shift) - 1;
+        x.lo = x.hi >= last && x.hi - last > r.lo ? x.hi - last : r.lo;
+    }
+    x.shift = x.hi > x.lo ? max(0, 32 - __clz(x.hi - x.lo) - LOG_BINS) : 0;
+    double p;
+    w.split(key_score(x.hi), p, x.top);
+    return x;
+}
+
+__device__ __forceinline__ uint64_t whole_weight(const Weights& w, float s, int exponent, int bits) {
+    double p;
+    int n;
+    w.split(s, p, n);
+    const int up = n - exponent + bits;
+    if (w.none(s) || up < -2) return 0;
+    return (uint64_t)__double_as_longlong(Weights::scaled(p, up) + 0x1p52) & (((uint64_t)1 << 52) - 1);
+}
+
+// Running sums of the bins' weights, from the best down, by THREADS threads of BINS / THREADS neighbours each: the first bin at which `above` plus
+// the sum reaches the target (first: target = top_p times the whole sum, which is returned in it).  The last bin with
+// anything in it where rounding leaves none.  `above` becomes the sum in front of the bin.
+template <int THREADS, int LOG_BINS>
+__device__ __forceinline__ int find_bin(const uint64_t* bins, const BinRule<LOG_BINS>& r, int bits, bool first, double top_p, double& target, double& above,
+                                        double* part /* [THREADS / 64 + 1] */, uint32_t* found /* [2] */) {
+    constexpr int BINS = 1 << LOG_BINS, PER = BINS / THREADS, WAVES = THREADS / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (threadIdx.x < 2) found[threadIdx.x] = threadIdx.x ? 0 : BINS;
+    double x[PER], sum = 0.0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        const int b = threadIdx.x * PER + q;
+        x[q] = ldexp((double)bins[b], r.exponent(b) - bits);
+        sum += x[q];
+    }
+    const double incl = wave_scan64(sum, lane);
+    if (lane == 63) part[wave] = incl;
+    __syncthreads();
+    double before = 0.0, all = 0.0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) before += part[w];
+        all += part[w];
+    }
+    if (first) target = top_p * all;
+    double run = above + (before + (incl - sum)), front[PER];
+    int mine = BINS, last = -1;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        front[q] = run;
+        run += x[q];
+        if (x[q] > 0.0) {
+            last = threadIdx.x * PER + q;
+            if (mine == BINS && run >= target) mine = last;
+        }
+    }
+    if (mine < BINS) atomicMin(&found[0], (uint32_t)mine);
+    if (last >= 0) atomicMax(&found[1], (uint32_t)last);
+    __syncthreads();
+    const int b = found[0] < BINS ? (int)found[0] : (int)found[1];
+    if (b / PER == (int)threadIdx.x) {
+#pragma unroll
+        for (int q = 0; q < PER; ++q) if (q == b % PER) part[WAVES] = front[q];
+    }
+    __syncthreads();
+    above = part[WAVES];
+    return b;
+}
+
+// (what has been formed from these is formed again: kept for every score, the parts of its weight would not fit the registers)
+template <int N> __device__ __forceinline__ void forget(float v[N]) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) asm volatile("" : "+v"(v[q]));
+}
+
+template <int WAVES, int TPW> struct CutScratch {
+    static constexpr int ROOM = WAVES * TPW * 256 < 1024 ? WAVES * TPW * 256 : 1024, LOG_BINS = WAVES * TPW <= 4 ? 8 : 10, BINS = 1 << LOG_BINS;
+    uint64_t bins[BINS > ROOM ? BINS : ROOM];  // then the list
+    uint64_t sorted[256];
+    double sums[ROOM], part[WAVES + 1];
+    uint32_t slots[2 * WAVES], rank[256], found[2], count;
+};
+
+// What top-p keeps of a workgroup's scores.
+template <int WAVES, int TPW, typename L>
+__device__ __forceinline__ Kept cut_by_weight(float v[TPW * 4], const L& low, float best, float worst, const Weights& w, double inv_t, double top_p,
+                                              CutScratch<WAVES, TPW>& s) {
+    constexpr int N = TPW * 4, THREADS = WAVES * 64, BITS = 46;  // 2^15 scores of up to 2^47.5
+    constexpr int ROOM = CutScratch<WAVES, TPW>::ROOM, LOG_BINS = CutScratch<WAVES, TPW>::LOG_BINS, BINS = 1 << LOG_BINS;
+    const int lane = threadIdx.x & 63;
+    BinRule<LOG_BINS> r = first_bins<LOG_BINS>(best, worst, inv_t);
+    double target = 0.0, above = 0.0;
+    int count = 0;
+    for (int round = 0;; ++round) {
+        __syncthreads();
+        for (int b = threadIdx.x; b < BINS; b += THREADS) s.bins[b] = 0;
+        __syncthreads();
+        forget<N>(v);
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            if (round == 0 ? v[q] > -INFINITY : r.in(v[q])) {
+                const int b = r.bin(v[q]);
+                const uint64_t x = whole_weight(w, v[q], r.exponent(b), BITS);
+                if (x) atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins[b]), (unsigned long long)x);
+            }
+        }
+        __syncthreads();
+        const int b = find_bin<THREADS, LOG_BINS>(s.bins, r, BITS, round == 0, top_p, target, above, s.part, s.found);
+        r = next_bins(r, b, w);
+        const float t0 = key_score(r.lo), t1 = key_score(r.hi);
+        int c = 0;
+#pragma unroll
+        for (int q = 0; q < N; ++q) c += __popcll(__ballot(v[q] >= t0 && v[q] <= t1));
+        __syncthreads();
+        count = block_count<WAVES>(c, s.slots);
+        if (count <= ROOM || r.lo == r.hi) break;
+    }
+    Kept kept = {key_score(r.hi), 0u, 0u};
+    __syncthreads();
+    if (count > ROOM) {  // all equal: as many as it takes, the first ones
+        const double need = ceil((target - above) / w.of(kept.t));
+        if (need < count) kept.least = select_equal<WAVES, N>(v, kept.t, low, need < 1.0 ? 1 : (int)need, s.slots);
+        return kept;
+    }
+    if (threadIdx.x == 0) s.count = 0;
+    __syncthreads();
+    const float t0 = key_score(r.lo), t1 = key_score(r.hi);
+#pragma unroll
+    for (int q = 0; q < N; ++q) append_entry(v[q] >= t0 && v[q] <= t1, (uint64_t)order_key(v[q]) << 32 | low(q), s.bins, &s.count);
+    __syncthreads();
+    const uint64_t* list = order_list<THREADS>(s.bins, s.sorted, s.rank, count);
+    for (int e = threadIdx.x; e < count; e += THREADS) s.sums[e] = w.of(key_score((uint32_t)(list[e] >> 32)));
+    __syncthreads();
+    if (threadIdx.x < 64) {  // the first entry at which the sum reaches the target
+        double carry = above;
+        int cut = count - 1;
+        for (int e0 = 0; e0 < count; e0 += 64) {
+            const double x = carry + wave_scan64(e0 + lane < count ? s.sums[e0 + lane] : 0.0, lane);
+            const uint64_t there = __ballot(e0 + lane < count && x >= target);
+            if (there) { cut = e0 + __ffsll((unsigned long long)there) - 1; break; }
+            carry = lane64(x, 63);
+        }
+        if (lane == 0) { s.found[0] = (uint32_t)(list[cut] >> 32); s.found[1] = (uint32_t)list[cut]; }
+    }
+    __syncthreads();
+    kept.t = key_score(s.found[0]);
+    kept.least = s.found[1];
+    return kept;
+}
+
+enum { CUT_MIN, CUT_WEIGHT, CUT_LIST };  // min-p alone; top-p and min-p; top-k and what follows it
 
 template <int DT, int WAVES, int TPW, int CUT>
 __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
@@ -151,90 +430,31 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
         uint64_t* list = order_list<THREADS>(b.list, b.sorted, b.rank, count);
         draw_from_list<THREADS>(a, row, list, min(count, a.top_k), sums, &kept_entries);
     } else {
-        __shared__ double sums[TILES], part[2 * WAVES];
-        __shared__ uint32_t slots[2 * WAVES];
+        __shared__ double sums[TILES];
         const Weights weights(best, a.inv_t);
         Kept kept = {-INFINITY, 0u, 0u};
-        double w[N];
-#pragma unroll
-        for (int q = 0; q < N; ++q) w[q] = weights.of(v[q]);
         if constexpr (CUT == CUT_WEIGHT) {
-            int round = 0;
-            auto weight_from = [&](uint32_t key) {  // of the scores at or above a key's
-                const float t = key_score(key);
-                double z = 0.0;
+            __shared__ CutScratch<WAVES, TPW> scratch;
+            float worst = INFINITY;
 #pragma unroll
-                for (int q = 0; q < N; ++q) z += v[q] >= t ? w[q] : 0.0;
-                z = wave_sum64(z);
-                if constexpr (WAVES == 1) return z;
-                double* p = part + (round++ & 1) * WAVES;
-                if (lane == 0) p[wave] = z;
-                __syncthreads();
-                z = 0.0;
-#pragma unroll
-                for (int x = 0; x < WAVES; ++x) z += p[x];
-                return z;
-            };
-            const double target = a.top_p * weight_from(LOWEST_KEY);
-            uint32_t lo = LOWEST_KEY, hi = order_key(best);  // largest threshold that reaches the target
-            while (lo < hi) {
-                const uint32_t mid = lo + (hi - lo) / 2 + ((hi - lo) & 1);
-                if (weight_from(mid) >= target) lo = mid; else hi = mid - 1;
-            }
-            kept.t = key_score(lo);
-            int equal = 0;
-#pragma unroll
-            for (int q = 0; q < N; ++q) equal += __popcll(__ballot(v[q] == kept.t));
-            __syncthreads();
-            equal = block_count<WAVES>(equal, slots);
-            const double above = lo < order_key(best) ? weight_from(lo + 1) : 0.0;
-            const double need = ceil((target - above) / weights.of(kept.t));
-            const int c = need >= equal ? equal : need < 1.0 ? 1 : (int)need;
-            if (c < equal) kept.least = select_equal<WAVES, N>(v, kept.t, low, c, slots);
+            for (int q = 0; q < N; ++q) worst = v[q] > -INFINITY ? fminf(worst, v[q]) : worst;
+            worst = -block_max<WAVES>(-worst, maxima);
+            kept = cut_by_weight<WAVES, TPW>(v, low, best, worst, weights, a.inv_t, a.top_p, scratch);
+            forget<N>(v);
         }
 #pragma unroll
         for (int i = 0; i < TPW; ++i) {
             double z = 0.0;
 #pragma unroll
             for (int q = 4 * i; q < 4 * i + 4; ++q) {
-                const bool in = CUT == CUT_NONE || v[q] > kept.t || (v[q] == kept.t && low(q) >= kept.least);
-                z += in && w[q] >= a.min_p ? w[q] : 0.0;
+                const bool in = CUT == CUT_MIN || v[q] > kept.t || (v[q] == kept.t && low(q) >= kept.least);
+                const double w = in ? weights.of(v[q]) : 0.0;
+                z += w >= a.min_p ? w : 0.0;
             }
             z = wave_sum64(z);
             if (lane == 0) sums[i * WAVES + wave] = z;
         }
-        __syncthreads();
-        if (wave == 0) {
-            double carry = 0.0;
-#pragma unroll
-            for (int t0 = 0; t0 < TILES; t0 += 64) {
-                const double x = carry + wave_scan64(t0 + lane < TILES ? sums[t0 + lane] : 0.0, lane);
-                if (t0 + lane < TILES) sums[t0 + lane] = x;
-                carry = __shfl(x, 63, 64);
-            }
-        }
-        __syncthreads();
-        const double total = sums[TILES - 1];
-        for (int d = wave; d < a.draws; d += WAVES) {
-            const double want = unit_number(a.u[row * a.draws + d]) * total;
-            int tile = -1, fallback = 0;
-#pragma unroll
-            for (int t0 = 0; t0 < TILES; t0 += 64) {
-                const bool there = t0 + lane < TILES;
-                const double x = there ? sums[t0 + lane] : 0.0, before = t0 + lane > 0 && there ? sums[t0 + lane - 1] : 0.0;
-                const uint64_t past = __ballot(there && x > want), some = __ballot(there && x > before);
-                if (tile < 0 && past) tile = t0 + __ffsll((unsigned long long)past) - 1;
-                if (some) fallback = t0 + 63 - __clzll(some);
-            }
-            if (tile < 0) tile = fallback;
-            int64_t id = -1;
-            double weight = 0.0;
-            draw_in_tile<DT, false>(s, (int64_t)tile * 256, a.in.n, kept, weights, a.min_p, 0u, tile > 0 ? sums[tile - 1] : 0.0, want, lane, id, weight);
-            if (lane == 0) {
-                a.ids[row * a.draws + d] = id;
-                if (a.logp) a.logp[row * a.draws + d] = (float)log(weight / total);
-            }
-        }
+        draw_from_tiles<DT, WAVES, TILES>(a, row, s, TILES, sums, nullptr, kept, weights, a.min_p);
     }
 }
 
@@ -259,283 +479,235 @@ __global__ __launch_bounds__(256) void k_draw_lists(DrawArgs a, const uint64_t* 
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// Long rows, segments of KGE_ROW_SEGMENT scores = SEG_TILES tiles.
-// Weights as whole numbers, for sums whose order is not fixed: w * 2^bits, and the next `bits` bits behind the point in a word of their
-// own; bits is such that the sum of either word over a row stays below 2^63.
+// Long rows: groups of GROUP scores = GROUP_TILES tiles.  Sums per tile and group by k_tiles (nothing cut) or k_draw_sums (what is kept), running
+// sums over the groups, then a wave per draw.
+// top-p: rounds of bins over the whole row, each a launch; a launch finds the bin of the round before it by itself.  From the second round on few
+// scores are left: the workgroups note those of their part of the row, and later rounds read the notes.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int SEG_WAVES = 16, SEG_TPW = 4, SEG_TILES = SEG_WAVES * SEG_TPW, BINS = 2048, LEVELS = 3;
+constexpr int LOG_BINS = 11, BINS = 1 << LOG_BINS;
+constexpr int ROUNDS = 4;  // bins of equal width, then 2^32 keys in three rounds
+constexpr int PART_GROUPS = 16, NOTES = 1024;  // groups per workgroup of k_draw_bins, scores that it can note
 
 struct RowCut {
-    uint32_t lo, hi;      // the threshold's key is in lo .. hi
-    uint32_t t, ties;     // the result
-    uint64_t above[2];    // weights of the keys above hi
-    double target;        // in units of the second word
+    BinRule<LOG_BINS> rule;
+    double target, above;
     float best;
-    int pad;
+    uint32_t t, ties;  // the result, t = 0: nothing is cut by weight
 };
 
 struct LongArgs {
     DrawArgs d;
-    int segments, bits, cut;  // cut: anything is left out
-    double* parts;        // [rows][segments][2] best score and sum of a segment, then running sums over the segments
-    double* tiles;        // [rows][segments][SEG_TILES] sums
-    uint32_t* tile_ties;  // [rows][segments][SEG_TILES] keys equal to the threshold
-    uint32_t* seg_ties;   // [rows][segments]
-    uint64_t* bins;       // [LEVELS][rows][BINS][2]
-    RowCut* rows;
+    int64_t groups, parts;  // of a row
+    int bits;
+    int by_weight;
+    float* tile_best;       // [rows][groups][GROUP_TILES] what the tile's sum is relative to
+    double* tile_sum;
+    uint32_t* tile_ties;    // equal to the threshold
+    float* group_best;      // [rows][groups]
+    float* group_worst;
+    double* group_sum;      // then running sums
+    uint32_t* group_ties;   // then the number in front
+    uint64_t* bins;         // [rows][ROUNDS][BINS]
+    RowCut* cuts;           // [ROUNDS + 1][rows]: before each round, and the result
+    uint32_t* notes;        // [rows][parts]: how many, more than NOTES: not noted
+    float* noted;           // [rows][parts][NOTES]
 };
 
-// Sums per tile.  First pass (PASS 0): relative to the segment's own best score, which it notes.  PASS 1: what is kept, relative to
-// the row's.
-template <int DT, int PASS>
-__global__ __launch_bounds__(SEG_WAVES * 64) void k_draw_sums(LongArgs a) {
-    __shared__ uint32_t slots[SEG_WAVES];
-    __shared__ float maxima[SEG_WAVES];
-    __shared__ double sums[SEG_WAVES];
+// The row's cut before round `round` (ROUNDS: the result), by a workgroup of 256 threads.
+__device__ __forceinline__ RowCut cut_before(const LongArgs& a, int64_t row, int round, float* maxima /* [4] */, double* part /* [5] */, uint32_t* found /* [2] */) {
+    if (round == 0) {
+        RowCut c = {};
+        float best = -INFINITY, lowest = -INFINITY;
+        for (int64_t g = threadIdx.x; g < a.groups; g += 256) {
+            best = fmaxf(best, a.group_best[row * a.groups + g]);
+            lowest = fmaxf(lowest, -a.group_worst[row * a.groups + g]);
+        }
+        c.best = block_max<4>(best, maxima);
+        lowest = block_max<4>(lowest, maxima);
+        if (c.best > -INFINITY) c.rule = first_bins<LOG_BINS>(c.best, -lowest, a.d.inv_t);
+        return c;
+    }
+    RowCut c = a.cuts[(round - 1) * a.d.in.rows + row];
+    if (!(c.best > -INFINITY)) return c;
+    const Weights w(c.best, a.d.inv_t);
+    if (round == 1 || c.rule.hi > c.rule.lo) {
+        const int b = find_bin<256, LOG_BINS>(a.bins + (row * ROUNDS + round - 1) * BINS, c.rule, a.bits, round == 1, a.d.top_p, c.target, c.above, part, found);
+        c.rule = next_bins(c.rule, b, w);
+    }
+    if (round == ROUNDS) {
+        c.t = c.rule.hi;
+        const double need = ceil((c.target - c.above) / w.of(key_score(c.t)));
+        c.ties = need >= 4294967295.0 ? 0xFFFFFFFFu : need < 1.0 ? 1u : (uint32_t)need;
+    }
+    return c;
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void k_draw_bins(LongArgs a, int round) {
+    __shared__ unsigned long long bins[BINS];
+    __shared__ float maxima[4];
+    __shared__ double found_sum[5];
+    __shared__ uint32_t found[2], noted;
     const int64_t block = flat_block();
-    if (block >= a.d.in.rows * a.segments) return;
-    const int64_t row = block / a.segments, seg = block - row * a.segments;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const auto* s = static_cast<const typename Score<DT>::type*>(a.d.in.p) + row * a.d.in.ld;
-    float v[SEG_TPW * 4];
-    const float mine = load_tiles<DT, SEG_WAVES, SEG_TPW>(s, seg * KGE_ROW_SEGMENT, a.d.in.n, v);
-    float t = -INFINITY, best;
-    if constexpr (PASS == 0) {
-        best = block_max<SEG_WAVES>(mine, maxima);
-        if (a.bins) {  // clear the row's bins
-            const int64_t words = 2 * BINS;
-            for (int level = 0; level < LEVELS; ++level)
-                for (int64_t x = seg * 1024 + threadIdx.x; x < words; x += a.segments * 1024)
-                    a.bins[((int64_t)level * a.d.in.rows + row) * words + x] = 0;
+    if (block >= a.d.in.rows * a.parts) return;
+    const int64_t row = block / a.parts, part = block - row * a.parts;
+    const RowCut c = cut_before(a, row, round, maxima, found_sum, found);
+    if (part == 0 && threadIdx.x == 0) a.cuts[round * a.d.in.rows + row] = c;
+    if (!(c.best > -INFINITY) || (round > 0 && c.rule.hi == c.rule.lo)) return;
+    const Weights w(c.best, a.d.inv_t);
+    for (int b = threadIdx.x; b < BINS; b += 256) bins[b] = 0;
+    if (threadIdx.x == 0) noted = 0;
+    __syncthreads();
+    auto add = [&](float s) {
+        const int b = c.rule.bin(s);
+        const uint64_t x = whole_weight(w, s, c.rule.exponent(b), a.bits);
+        if (x) atomicAdd(&bins[b], (unsigned long long)x);
+    };
+    const uint32_t have = round > 1 ? a.notes[block] : NOTES + 1;
+    if (have <= NOTES) {
+        for (uint32_t e = threadIdx.x; e < have; e += 256) {
+            const float s = a.noted[block * NOTES + e];
+            if (c.rule.in(s)) add(s);
         }
     } else {
-        best = a.rows[row].best;
-        if (a.rows[row].t) t = key_score(a.rows[row].t);
-    }
-    const Weights weights(best, a.d.inv_t);
-    const double min_p = PASS == 0 ? 0.0 : a.d.min_p;
-    double all = 0.0;
-    uint32_t equal = 0;
+        const auto* s = static_cast<const typename Score<DT>::type*>(a.d.in.p) + row * a.d.in.ld;
+        const int64_t last = min((part + 1) * PART_GROUPS, a.groups);
+        for (int64_t g = part * PART_GROUPS; g < last; ++g) {
+            float v[16];
+            load_tiles<DT, 4, 4>(s, g * GROUP, a.d.in.n, v);
+            if (round == 0) {
 #pragma unroll
-    for (int i = 0; i < SEG_TPW; ++i) {
+                for (int q = 0; q < 16; ++q) if (v[q] > -INFINITY) add(v[q]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    const bool in = c.rule.in(v[q]);
+                    const uint64_t who = __ballot(in);
+                    if (!who) continue;
+                    if (round == 1) {
+                        uint32_t base = 0;
+                        if ((threadIdx.x & 63) == 0) base = atomicAdd(&noted, (uint32_t)__popcll(who));
+                        base = (uint32_t)__builtin_amdgcn_readfirstlane((int)base) + __popcll(who & (((uint64_t)1 << (threadIdx.x & 63)) - 1));
+                        if (in && base < NOTES) a.noted[block * NOTES + base] = v[q];
+                    }
+                    if (in) add(v[q]);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    unsigned long long* out = reinterpret_cast<unsigned long long*>(a.bins) + (row * ROUNDS + round) * BINS;
+    for (int b = threadIdx.x; b < BINS; b += 256)
+        if (bins[b]) atomicAdd(&out[b], bins[b]);
+    if (round == 1 && threadIdx.x == 0) a.notes[block] = noted;
+}
+
+// Sums of what is kept, relative to the row's best score.
+template <int DT>
+__global__ __launch_bounds__(256) void k_draw_sums(LongArgs a) {
+    __shared__ float maxima[4];
+    __shared__ double sums[GROUP_TILES];
+    __shared__ double found_sum[5];
+    __shared__ uint32_t found[2], ties[GROUP_TILES];
+    const int64_t block = flat_block();
+    if (block >= a.d.in.rows * a.groups) return;
+    const int64_t row = block / a.groups, group = block - row * a.groups;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const auto* s = static_cast<const typename Score<DT>::type*>(a.d.in.p) + row * a.d.in.ld;
+    float v[16];
+    load_tiles<DT, 4, 4>(s, group * GROUP, a.d.in.n, v);
+    const RowCut c = a.by_weight ? a.cuts[ROUNDS * a.d.in.rows + row] : cut_before(a, row, 0, maxima, found_sum, found);
+    if (!a.by_weight && group == 0 && threadIdx.x == 0) a.cuts[ROUNDS * a.d.in.rows + row] = c;
+    const float t = c.t ? key_score(c.t) : -INFINITY;
+    const Weights w(c.best, a.d.inv_t);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
         double z = 0.0;
         uint32_t e = 0;
 #pragma unroll
         for (int q = 4 * i; q < 4 * i + 4; ++q) {
-            const double w = v[q] > t ? weights.of(v[q]) : 0.0;
-            z += w >= min_p ? w : 0.0;
-            if constexpr (PASS == 1) e += t > -INFINITY ? __popcll(__ballot(v[q] == t)) : 0;
+            const double x = v[q] > t ? w.of(v[q]) : 0.0;
+            z += x >= a.d.min_p ? x : 0.0;
+            e += __popcll(__ballot(v[q] == t));
         }
         z = wave_sum64(z);
-        all += z;
-        equal += e;
-        if (lane == 0) {
-            const int64_t tile = block * SEG_TILES + i * SEG_WAVES + wave;
-            a.tiles[tile] = z;
-            if constexpr (PASS == 1) a.tile_ties[tile] = e;
-        }
+        if (lane == 0) { sums[i * 4 + wave] = z; ties[i * 4 + wave] = c.t ? e : 0; }
     }
-    if (lane == 0) { sums[wave] = all; slots[wave] = equal; }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        double z = 0.0;
-        uint32_t e = 0;
-        for (int w = 0; w < SEG_WAVES; ++w) { z += sums[w]; e += slots[w]; }
-        a.parts[2 * block] = best;
-        a.parts[2 * block + 1] = z;
-        if constexpr (PASS == 1) a.seg_ties[block] = e;
+    if (threadIdx.x >= 64) return;
+    const double z = lane < GROUP_TILES ? sums[lane] : 0.0;
+    uint32_t e = lane < GROUP_TILES ? ties[lane] : 0;
+    if (lane < GROUP_TILES) {
+        a.tile_best[block * GROUP_TILES + lane] = c.best;
+        a.tile_sum[block * GROUP_TILES + lane] = z;
+        a.tile_ties[block * GROUP_TILES + lane] = e;
     }
+    const double all = wave_sum64(z);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) e += __shfl_xor((int)e, o, 64);
+    if (lane == 0) { a.group_best[block] = c.best; a.group_sum[block] = all; a.group_ties[block] = e; }
 }
 
-// The row's best score; with top-p the interval in which its threshold is looked for.
-__global__ __launch_bounds__(256) void k_draw_begin(LongArgs a) {
+// The result of the rounds, once for all workgroups of k_draw_sums.
+__global__ __launch_bounds__(256) void k_draw_cut(LongArgs a) {
     __shared__ float maxima[4];
+    __shared__ double found_sum[5];
+    __shared__ uint32_t found[2];
     const int64_t row = flat_block();
     if (row >= a.d.in.rows) return;
-    float best = -INFINITY;
-    for (int64_t g = threadIdx.x; g < a.segments; g += 256) best = fmaxf(best, (float)a.parts[2 * (row * a.segments + g)]);
-    best = block_max<4>(best, maxima);
-    if (threadIdx.x == 0) {
-        RowCut r = {};
-        r.best = best;
-        r.lo = LOWEST_KEY; r.hi = order_key(best);
-        a.rows[row] = r;
-    }
+    const RowCut c = cut_before(a, row, ROUNDS, maxima, found_sum, found);
+    if (threadIdx.x == 0) a.cuts[ROUNDS * a.d.in.rows + row] = c;
 }
 
-__device__ __forceinline__ int bin_shift(uint32_t lo, uint32_t hi) { return max(0, 32 - __clz(hi - lo) - 11); }  // hi > lo
-
-// Weights of the keys in the row's interval, by bin.
-template <int DT>
-__global__ __launch_bounds__(SEG_WAVES * 64) void k_draw_bins(LongArgs a, int level) {
-    __shared__ unsigned long long bins[BINS * 2];
-    const int64_t block = flat_block();
-    if (block >= a.d.in.rows * a.segments) return;
-    const int64_t row = block / a.segments, seg = block - row * a.segments;
-    const RowCut r = a.rows[row];
-    const auto* s = static_cast<const typename Score<DT>::type*>(a.d.in.p) + row * a.d.in.ld;
-    for (int x = threadIdx.x; x < BINS * 2; x += 1024) bins[x] = 0;
-    float v[SEG_TPW * 4];
-    load_tiles<DT, SEG_WAVES, SEG_TPW>(s, seg * KGE_ROW_SEGMENT, a.d.in.n, v);
-    __syncthreads();
-    const Weights weights(r.best, a.d.inv_t);
-    const int shift = r.hi > r.lo ? bin_shift(r.lo, r.hi) : 0;
-    const double unit = (double)((uint64_t)1 << a.bits);
+__device__ __forceinline__ uint32_t wave_scan_u32(uint32_t v, int lane) {
 #pragma unroll
-    for (int q = 0; q < SEG_TPW * 4; ++q) {
-        const uint32_t key = order_key(v[q]);
-        if (key >= r.lo && key <= r.hi) {
-            const int bin = (int)((r.hi - key) >> shift);
-            const double w = weights.of(v[q]) * unit, whole = floor(w);
-            const uint64_t x = (uint64_t)whole, y = (uint64_t)((w - whole) * unit);
-            if (x) atomicAdd(&bins[2 * bin], (unsigned long long)x);
-            if (y) atomicAdd(&bins[2 * bin + 1], (unsigned long long)y);
-        }
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up((int)v, o, 64);
+        if (lane >= o) v += y;
     }
-    __syncthreads();
-    unsigned long long* out = reinterpret_cast<unsigned long long*>(a.bins) + ((int64_t)level * a.d.in.rows + row) * BINS * 2;
-    for (int x = threadIdx.x; x < BINS * 2; x += 1024)
-        if (bins[x]) atomicAdd(&out[x], bins[x]);
+    return v;
 }
 
-// The bin in which the running sum, from the best key down, reaches the target becomes the interval.
-__global__ __launch_bounds__(256) void k_draw_narrow(LongArgs a, int level) {
-    constexpr int PER = BINS / 256;
-    __shared__ uint64_t wave_part[2][4];
-    __shared__ uint32_t found;
-    const int64_t row = flat_block();
-    if (row >= a.d.in.rows) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    RowCut r = a.rows[row];
-    if (!(r.best > -INFINITY)) return;  // no candidate
-    const uint64_t* bins = a.bins + ((int64_t)level * a.d.in.rows + row) * BINS * 2 + threadIdx.x * PER * 2;
-    uint64_t x[PER][2], sum[2] = {0, 0};
-#pragma unroll
-    for (int q = 0; q < PER; ++q)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) { x[q][h] = bins[2 * q + h]; sum[h] += x[q][h]; }
-    uint64_t before[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        uint64_t v = sum[h];
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint64_t y = __shfl_up((unsigned long long)v, o, 64);
-            if (lane >= o) v += y;
-        }
-        if (lane == 63) wave_part[h][wave] = v;
-        before[h] = v - sum[h];
-    }
-    if (threadIdx.x == 0) found = BINS;
-    __syncthreads();
-    const double unit = (double)((uint64_t)1 << a.bits);
-    uint64_t all[2] = {0, 0};
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) before[h] += wave_part[h][w];
-            all[h] += wave_part[h][w];
-        }
-    auto whole = [&](const uint64_t v[2]) { return ((unsigned __int128)v[0] << a.bits) + v[1]; };
-    auto number = [&](double v) {  // to a whole number, v >= 0 and below 2^126
-        const double high = floor(v * 0x1p-63);
-        return ((unsigned __int128)(uint64_t)high << 63) + (uint64_t)(v - high * 0x1p63);
-    };
-    if (level == 0) {
-        const unsigned __int128 z = whole(all);
-        r.target = a.d.top_p * ((double)(uint64_t)(z >> 63) * 0x1p63 + (double)(uint64_t)(z & (((unsigned __int128)1 << 63) - 1)));
-    }
-    const unsigned __int128 want = number(r.target);
-    uint64_t run[2] = {r.above[0] + before[0], r.above[1] + before[1]};
-    uint64_t above[PER][2];
-    int mine = BINS;
-#pragma unroll
-    for (int q = 0; q < PER; ++q) {
-        above[q][0] = run[0]; above[q][1] = run[1];
-        run[0] += x[q][0]; run[1] += x[q][1];
-        if (mine == BINS && (x[q][0] | x[q][1]) && whole(run) >= want) mine = threadIdx.x * PER + q;
-    }
-    if (mine < BINS) atomicMin(&found, (uint32_t)mine);
-    __syncthreads();
-    // rounding of the target may leave no bin: the last one that holds anything
-    if (found == BINS) {
-        int last = -1;
-#pragma unroll
-        for (int q = 0; q < PER; ++q) if (x[q][0] | x[q][1]) last = threadIdx.x * PER + q;
-        __syncthreads();
-        if (threadIdx.x == 0) found = 0;
-        __syncthreads();
-        if (last >= 0) atomicMax(&found, (uint32_t)last);
-        __syncthreads();
-    }
-    if ((int)(found / PER) == (int)threadIdx.x) {
-        const int q = found % PER;
-        const int shift = r.hi > r.lo ? bin_shift(r.lo, r.hi) : 0;
-        uint64_t over[2] = {0, 0};
-#pragma unroll
-        for (int v = 0; v < PER; ++v) if (v == q) { over[0] = above[v][0]; over[1] = above[v][1]; }
-        r.above[0] = over[0]; r.above[1] = over[1];
-        const uint32_t top = r.hi - ((uint32_t)found << shift), width = (uint32_t)1 << shift;
-        r.hi = top;
-        r.lo = top >= width && top - width + 1 > r.lo ? top - width + 1 : r.lo;
-        if (level == LEVELS - 1) {
-            r.t = r.hi;
-            const double w = Weights(r.best, a.d.inv_t).of(key_score(r.t)) * unit, down = floor(w);
-            const uint64_t one[2] = {(uint64_t)down, (uint64_t)((w - down) * unit)};
-            const unsigned __int128 each = whole(one), have = whole(r.above);
-            unsigned __int128 c = 1;
-            if (want > have && each > 0) c = (want - have + each - 1) / each;
-            r.ties = c < 1 ? 1 : c > 0xFFFFFFFFu ? 0xFFFFFFFFu : (uint32_t)c;
-        }
-        a.rows[row] = r;
-    }
-}
-
-// Running sums over the segments of a row.
-__global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a) {
+// Running sums over the groups of a row.
+__global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a, int cut) {
     __shared__ double part[16];
     __shared__ uint32_t tpart[16];
     __shared__ float maxima[16];
     const int64_t row = flat_block();
     if (row >= a.d.in.rows) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    double* parts = a.parts + 2 * row * a.segments;
+    const float* bests = a.group_best + row * a.groups;
+    double* sums = a.group_sum + row * a.groups;
+    uint32_t* ties = a.group_ties + row * a.groups;
     float best = -INFINITY;
-    for (int64_t g = threadIdx.x; g < a.segments; g += 1024) best = fmaxf(best, (float)parts[2 * g]);
+    for (int64_t g = threadIdx.x; g < a.groups; g += 1024) best = fmaxf(best, bests[g]);
     best = block_max<16>(best, maxima);
     const Weights weights(best, a.d.inv_t);
     uint32_t t = 0, most = 0;
     double each = 0.0;
-    if (a.cut) {
-        const RowCut r = a.rows[row];
-        t = r.t; most = r.ties;
+    if (cut) {
+        const RowCut c = a.cuts[ROUNDS * a.d.in.rows + row];
+        t = c.t; most = c.ties;
         if (t) {
             each = weights.of(key_score(t));
             if (!(each >= a.d.min_p)) each = 0.0;
         }
     } else if (threadIdx.x == 0) {
-        RowCut r = {};
-        r.best = best;
-        a.rows[row] = r;
+        RowCut c = {};
+        c.best = best;
+        a.cuts[ROUNDS * a.d.in.rows + row] = c;
     }
     double carry = 0.0;
     uint32_t tcarry = 0;
-    for (int64_t g0 = 0; g0 < a.segments; g0 += 1024) {
+    for (int64_t g0 = 0; g0 < a.groups; g0 += 1024) {
         const int64_t g = g0 + threadIdx.x;
         double v = 0.0;
         uint32_t e = 0;
-        if (g < a.segments) {
-            const float own = (float)parts[2 * g];
-            v = own > -INFINITY ? parts[2 * g + 1] * weights.of(own) : 0.0;
-            if (t) e = a.seg_ties[row * a.segments + g];
+        if (g < a.groups) {
+            v = bests[g] > -INFINITY ? sums[g] * weights.of(bests[g]) : 0.0;
+            if (t) e = ties[g];
         }
-        uint32_t es = e;  // equal keys up to this segment
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t y = __shfl_up((int)es, o, 64);
-            if (lane >= o) es += y;
-        }
+        const uint32_t es = wave_scan_u32(e, lane);  // equal scores up to this group
         if (lane == 63) tpart[wave] = es;
         __syncthreads();
         uint32_t ebase = tcarry;
@@ -553,15 +725,15 @@ __global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a) {
             if (w < wave) base += part[w];
             carry += part[w];
         }
-        if (g < a.segments) {
-            parts[2 * g + 1] = base + v;
-            if (t) a.seg_ties[row * a.segments + g] = before;
+        if (g < a.groups) {
+            sums[g] = base + v;
+            if (t) ties[g] = before;
         }
         __syncthreads();
     }
 }
 
-// One wave per draw: segment, tile, position.
+// One wave per draw: group, tile, position.
 template <int DT>
 __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
     const int lane = threadIdx.x & 63;
@@ -569,10 +741,12 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
     if (d >= a.d.in.rows * a.d.draws) return;
     const int64_t row = d / a.d.draws;
     const auto* s = static_cast<const typename Score<DT>::type*>(a.d.in.p) + row * a.d.in.ld;
-    const RowCut r = a.rows[row];
-    const double* parts = a.parts + 2 * row * a.segments;
-    const double total = parts[2 * (a.segments - 1) + 1];
-    if (!(r.best > -INFINITY)) {
+    const RowCut& c = a.cuts[ROUNDS * a.d.in.rows + row];
+    const float best = c.best;
+    const uint32_t t = c.t, most = c.ties;
+    const double* sums = a.group_sum + row * a.groups;
+    const double total = sums[a.groups - 1];
+    if (!(best > -INFINITY)) {
         if (lane == 0) {
             a.d.ids[d] = -1;
             if (a.d.logp) a.d.logp[d] = -INFINITY;
@@ -580,39 +754,38 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
         return;
     }
     const double want = unit_number(a.d.u[d]) * total;
-    int64_t lo = 0, hi = a.segments - 1;
+    int64_t lo = 0, hi = a.groups - 1;  // the first group whose sum exceeds `want` is in lo .. hi (or none does)
     while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if (parts[2 * mid + 1] > want) hi = mid; else lo = mid + 1;
+        const int64_t step = (hi - lo + 63) / 64, at = min(lo + (lane + 1) * step - 1, hi);
+        const uint64_t past = __ballot(sums[at] > want);
+        const int first = past ? __ffsll((unsigned long long)past) - 1 : 63;
+        hi = min(lo + (first + 1) * step - 1, hi);
+        lo = min(lo + first * step, hi);
     }
-    while (lo > 0 && !(parts[2 * lo + 1] > parts[2 * lo - 1])) --lo;  // (never a segment without weight)
-    const int64_t block = row * a.segments + lo;
-    const float own = (float)parts[2 * lo];
-    const Weights weights(r.best, a.d.inv_t);
-    double base = lo > 0 ? parts[2 * lo - 1] : 0.0;
-    double v = a.tiles[block * SEG_TILES + lane] * weights.of(own);
-    uint32_t before = 0;
-    if (r.t) {
-        const uint32_t e = a.tile_ties[block * SEG_TILES + lane];
-        uint32_t es = e;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t y = __shfl_up((int)es, o, 64);
-            if (lane >= o) es += y;
-        }
-        before = a.seg_ties[block] + es - e;
-        const double each = weights.of(key_score(r.t));
-        if (before < r.ties && each >= a.d.min_p) v += each * (double)min(e, r.ties - before);
+    while (lo > 0 && !(sums[lo] > sums[lo - 1])) --lo;  // (never a group without weight)
+    const int64_t group = row * a.groups + lo;
+    const Weights weights(best, a.d.inv_t);
+    double base = lo > 0 ? sums[lo - 1] : 0.0, v = 0.0;
+    uint32_t e = 0, before = 0;
+    if (lane < GROUP_TILES) {
+        const float own = a.tile_best[group * GROUP_TILES + lane];
+        v = own > -INFINITY ? a.tile_sum[group * GROUP_TILES + lane] * weights.of(own) : 0.0;
+        if (t) e = a.tile_ties[group * GROUP_TILES + lane];
+    }
+    if (t) {
+        before = a.group_ties[group] + wave_scan_u32(e, lane) - e;
+        const double each = weights.of(key_score(t));
+        if (before < most && each >= a.d.min_p) v += each * (double)min(e, most - before);
     }
     const double incl = base + wave_scan64(v, lane);
     const uint64_t past = __ballot(incl > want && v > 0.0), any = __ballot(v > 0.0);
     const int tile = past ? __ffsll((unsigned long long)past) - 1 : any ? 63 - __clzll(any) : 0;
-    base = __shfl(incl - v, tile, 64);
+    base = lane64(incl - v, tile);
     before = __shfl((int)before, tile, 64);
-    const Kept kept = {r.t ? key_score(r.t) : -INFINITY, 0u, r.ties};
+    const Kept kept = {t ? key_score(t) : -INFINITY, 0u, most};
     int64_t id = -1;
     double weight = 0.0;
-    draw_in_tile<DT, true>(s, lo * KGE_ROW_SEGMENT + (int64_t)tile * 256, a.d.in.n, kept, weights, a.d.min_p, before, base, want, lane, id, weight);
+    draw_in_tile<DT, true>(s, lo * GROUP + (int64_t)tile * 256, a.d.in.n, kept, weights, a.d.min_p, before, base, want, lane, id, weight);
     if (lane == 0) {
         a.d.ids[d] = id;
         if (a.d.logp) a.d.logp[d] = (float)log(weight / total);
@@ -630,55 +803,80 @@ void launch_rows(const DrawArgs& a, hipStream_t st) {
     else k_draw_rows<DT, 16, 8, CUT><<<grid, 1024, 0, st>>>(a);
 }
 
+template <int DT>
+void launch_whole(const DrawArgs& a, hipStream_t st) {
+    const int64_t tiles = pieces(a.in.n, 256);
+    const dim3 grid = flat_grid(a.in.rows);
+    if (tiles <= 4) k_draw_whole<DT, 1><<<grid, 64, 0, st>>>(a);
+    else if (tiles <= 16 || a.in.rows >= 512) k_draw_whole<DT, 4><<<grid, 256, 0, st>>>(a);
+    else k_draw_whole<DT, 16><<<grid, 1024, 0, st>>>(a);
+}
+
 // The pieces of the workspace of long rows; returns its size.
-int64_t carve(LongArgs* a, char* base, int64_t rows, int64_t n, bool weight_cut) {
-    const int64_t segments = pieces(n, KGE_ROW_SEGMENT), blocks = rows * segments;
+int64_t carve(LongArgs* a, char* base, int64_t rows, int64_t n, bool by_weight) {
+    const int64_t groups = pieces(n, GROUP), blocks = rows * groups, parts = pieces(groups, PART_GROUPS);
     int64_t off = 0;
     auto take = [&](int64_t bytes) { const int64_t o = off; off += up256(bytes); return base ? base + o : nullptr; };
-    char* parts = take(blocks * 16);
-    char* tiles = take(blocks * SEG_TILES * 8);
-    char* tile_ties = take(blocks * SEG_TILES * 4);
-    char* seg_ties = take(blocks * 4);
-    char* cuts = take(rows * (int64_t)sizeof(RowCut));
-    char* bins = weight_cut ? take(rows * LEVELS * BINS * 16) : nullptr;
+    char* tile_best = take(blocks * GROUP_TILES * 4);
+    char* tile_sum = take(blocks * GROUP_TILES * 8);
+    char* tile_ties = take(blocks * GROUP_TILES * 4);
+    char* group_best = take(blocks * 4);
+    char* group_worst = take(blocks * 4);
+    char* group_sum = take(blocks * 8);
+    char* group_ties = take(blocks * 4);
+    char* cuts = take((ROUNDS + 1) * rows * (int64_t)sizeof(RowCut));
+    char* bins = by_weight ? take(rows * ROUNDS * BINS * 8) : nullptr;
+    char* notes = by_weight ? take(rows * parts * 4) : nullptr;
+    char* noted = by_weight ? take(rows * parts * NOTES * 4) : nullptr;
     if (a) {
-        a->segments = (int)segments;
-        a->parts = reinterpret_cast<double*>(parts);
-        a->tiles = reinterpret_cast<double*>(tiles);
+        a->groups = groups;
+        a->parts = parts;
+        a->tile_best = reinterpret_cast<float*>(tile_best);
+        a->tile_sum = reinterpret_cast<double*>(tile_sum);
         a->tile_ties = reinterpret_cast<uint32_t*>(tile_ties);
-        a->seg_ties = reinterpret_cast<uint32_t*>(seg_ties);
-        a->rows = reinterpret_cast<RowCut*>(cuts);
+        a->group_best = reinterpret_cast<float*>(group_best);
+        a->group_worst = reinterpret_cast<float*>(group_worst);
+        a->group_sum = reinterpret_cast<double*>(group_sum);
+        a->group_ties = reinterpret_cast<uint32_t*>(group_ties);
+        a->cuts = reinterpret_cast<RowCut*>(cuts);
         a->bins = reinterpret_cast<uint64_t*>(bins);
+        a->notes = reinterpret_cast<uint32_t*>(notes);
+        a->noted = reinterpret_cast<float*>(noted);
     }
     return off;
 }
 
 template <int DT>
 void launch(const DrawArgs& d, void* workspace, hipStream_t st) {
-    const bool weight_cut = d.top_k == 0 && d.top_p < 1.0;
+    const bool by_weight = d.top_k == 0 && d.top_p < 1.0;
     if (d.in.n <= KGE_ROW_RESIDENT) {
         if (d.top_k > 0) launch_rows<DT, CUT_LIST>(d, st);
-        else if (weight_cut) launch_rows<DT, CUT_WEIGHT>(d, st);
-        else launch_rows<DT, CUT_NONE>(d, st);
+        else if (by_weight) launch_rows<DT, CUT_WEIGHT>(d, st);
+        else if (d.min_p > 0.0) launch_rows<DT, CUT_MIN>(d, st);
+        else launch_whole<DT>(d, st);
         return;
     }
     LongArgs a = {};
     a.d = d;
-    carve(&a, static_cast<char*>(workspace), d.in.rows, d.in.n, weight_cut);
-    a.cut = weight_cut || d.min_p > 0.0;
-    a.bits = 62;
-    while (((int64_t)1 << (62 - a.bits)) < d.in.n) --a.bits;
-    const dim3 segs = flat_grid(d.in.rows * a.segments), rows = flat_grid(d.in.rows);
-    k_draw_sums<DT, 0><<<segs, SEG_WAVES * 64, 0, st>>>(a);
-    if (a.cut) {
-        k_draw_begin<<<rows, 256, 0, st>>>(a);
-        for (int level = 0; weight_cut && level < LEVELS; ++level) {
-            k_draw_bins<DT><<<segs, SEG_WAVES * 64, 0, st>>>(a, level);
-            k_draw_narrow<<<rows, 256, 0, st>>>(a, level);
-        }
-        k_draw_sums<DT, 1><<<segs, SEG_WAVES * 64, 0, st>>>(a);
+    carve(&a, static_cast<char*>(workspace), d.in.rows, d.in.n, by_weight);
+    a.by_weight = by_weight;
+    const bool cut = by_weight || d.min_p > 0.0;
+    a.bits = 50;  // n weights of up to 2^(bits + 1.5) in 64 bits
+    while (((int64_t)1 << (61 - a.bits)) < d.in.n) --a.bits;
+    TileArgs t = {};
+    t.in = d.in; t.inv_t = d.inv_t; t.groups = a.groups;
+    t.group_best = a.group_best;
+    if (cut) t.group_worst = a.group_worst;
+    else { t.tile_best = a.tile_best; t.tile_sum = a.tile_sum; t.group_sum = a.group_sum; }
+    if (by_weight) { t.clear = a.bins; t.clear_words = ROUNDS * BINS; }
+    kge_launch_tiles(t, !cut, st);
+    const dim3 rows = flat_grid(d.in.rows);
+    if (by_weight) {
+        for (int round = 0; round < ROUNDS; ++round) k_draw_bins<DT><<<flat_grid(d.in.rows * a.parts), 256, 0, st>>>(a, round);
+        k_draw_cut<<<rows, 256, 0, st>>>(a);
     }
-    k_draw_scan<<<rows, 1024, 0, st>>>(a);
+    if (cut) k_draw_sums<DT><<<flat_grid(d.in.rows * a.groups), 256, 0, st>>>(a);
+    k_draw_scan<<<rows, 1024, 0, st>>>(a, cut);
     k_draw_pick<DT><<<flat_grid(pieces(d.in.rows * d.draws, 4)), 256, 0, st>>>(a);
 }
 

@@ -23,6 +23,21 @@ struct RowScores {
 inline int64_t pieces(int64_t n, int64_t of) { return (n + of - 1) / of; }
 inline int64_t up256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
+constexpr int GROUP_TILES = 16, GROUP = GROUP_TILES * 256;  // scores of long rows that a workgroup of k_tiles takes
+struct TileArgs {
+    RowScores in;
+    double inv_t;
+    int64_t groups;       // of a row
+    float* tile_best;     // [rows][groups][GROUP_TILES], may be null
+    double* tile_sum;     // the same, relative to the tile's best; may be null
+    float* group_best;    // [rows][groups]
+    double* group_sum;    // relative to the group's best
+    float* group_worst;   // lowest score that is not masked, +inf without one; may be null (only without sums)
+    uint64_t* clear;      // [rows][clear_words] that the pass sets to 0, may be null
+    int64_t clear_words;
+};
+void kge_launch_tiles(const TileArgs& a, bool sums, hipStream_t st);
+
 int64_t kge_top_workspace(int64_t rows, int64_t n, int m);
 // (ids and scores, or the sorted entries alone; lse may be null)
 void kge_launch_top(const RowScores& in, int m, float temperature, int64_t* ids, float* scores, uint64_t* entries, float* lse,
