@@ -146,11 +146,13 @@ __global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
     float best = -INFINITY;
 #pragma unroll
     for (int i = 0; i < TPW; ++i) {
-        const int64_t j = first + (int64_t)(i * WAVES + wave) * 256 + lane * 4;
-        load4<DT>(r.s, j, r.n, v + 4 * i);
+        const int64_t tile = first + (int64_t)(i * WAVES + wave) * 256;
+        Quad<DT> x;
+        x.load(r.s, tile + lane * 4, r.n);
+        x.template values<false>(tile, r.n, v + 4 * i);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            if constexpr (STEP) { if (j + q < r.n) v[4 * i + q] = r.of(v[4 * i + q]); }
+            if constexpr (STEP) { if (tile + lane * 4 + q < r.n) v[4 * i + q] = r.of(v[4 * i + q]); }
             best = fmaxf(best, v[4 * i + q]);
         }
     }
@@ -254,9 +256,13 @@ __global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < TPW; ++i) {
-            const int64_t j = (int64_t)(i * WAVES + wave) * 256 + lane * 4;
+            const int64_t tile = (int64_t)(i * WAVES + wave) * 256, j = tile + lane * 4;
             float x[4], raw[4] = {};
-            if constexpr (STEP) load4<DT>(in, j, r.n - first, raw);
+            if constexpr (STEP) {
+                Quad<DT> again;
+                again.load(in, j, r.n);
+                again.template values<false>(tile, r.n, raw);
+            }
 #pragma unroll
             for (int q = 0; q < 4; ++q) x[q] = shape(v[4 * i + q] * g.other, raw[q]);
             if (j < r.n - first) store4<DT>(out, j, r.n - first, x);

@@ -41,7 +41,9 @@ template <int DT, bool COUNTED>
 __device__ __forceinline__ void draw_in_tile(const typename Score<DT>::type* s, int64_t first, int64_t n, const Kept& k, const Weights& weights, double min_p,
                                              uint32_t ties_before, double base, double target, int lane, int64_t& id, double& weight) {
     float v[4];
-    load4<DT>(s, first + lane * 4, n, v);
+    Quad<DT> x;
+    x.load(s, first + lane * 4, n);
+    x.values(first, n, v);
     double w[4], sum = 0.0;
     uint32_t rank = ties_before;
     if constexpr (COUNTED) {
@@ -51,9 +53,8 @@ __device__ __forceinline__ void draw_in_tile(const typename Score<DT>::type* s, 
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        v[q] = fmaxf(v[q], -INFINITY);
         const bool equal = v[q] == k.t, in = v[q] > k.t || (equal && (COUNTED ? rank < k.ties : ~(uint32_t)(first + lane * 4 + q) >= k.least));
-        w[q] = in ? weights.of(v[q]) : 0.0;
+        w[q] = weights.of(v[q], in);
         rank += equal;
         if (!(w[q] >= min_p)) w[q] = 0.0;
         sum += w[q];
@@ -84,7 +85,8 @@ template <int THREADS>
 __device__ __forceinline__ void draw_from_list(const DrawArgs& a, int64_t row, uint64_t* list, int count, double* sums, int* kept) {
     if (count == 0) { write_empty<THREADS>(a, row); return; }
     const int lane = threadIdx.x & 63;
-    const Weights weights(key_score((uint32_t)(list[0] >> 32)), a.inv_t);
+    const Scale scale(a.inv_t);
+    const Weights weights(key_score((uint32_t)(list[0] >> 32)), scale);
     auto scan = [&](int n) {  // sums of weights -> running sums, by the first wave
         __syncthreads();
         if (threadIdx.x < 64) {
@@ -177,28 +179,30 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_whole(DrawArgs a) {
     __shared__ float bests[TILES], maxima[WAVES];
     const int64_t row = flat_block();
     if (row >= a.in.rows) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tiles = (int)((a.in.n + 255) / 256);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tiles = (int)((a.in.n + 255) / 256);
     const auto* s = static_cast<const typename Score<DT>::type*>(a.in.p) + row * a.in.ld;
+    const Scale scale(a.inv_t);
     float most = -INFINITY;
-    for (int t0 = wave; t0 < tiles; t0 += 4 * WAVES) {
+    Quad<DT> x[4];
+    auto load = [&](int t0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i].load(s, (int64_t)(t0 + i) * 256 + lane * 4, a.in.n);
+    };
+    load(wave * 4);
+    for (int t0 = wave * 4; t0 < tiles; t0 += 4 * WAVES) {
         float v[16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load4<DT>(s, (int64_t)(t0 + i * WAVES) * 256 + lane * 4, a.in.n, v + 4 * i);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int q = 4 * i; q < 4 * i + 4; ++q) v[q] = fmaxf(v[q], -INFINITY);
-            const float best = wave_most(fmaxf(fmaxf(v[4 * i], v[4 * i + 1]), fmaxf(v[4 * i + 2], v[4 * i + 3])));
-            const Weights w(best, a.inv_t);
-            const double z = wave_sum64((w.of(v[4 * i]) + w.of(v[4 * i + 1])) + (w.of(v[4 * i + 2]) + w.of(v[4 * i + 3])));
-            if (t0 + i * WAVES < tiles && lane == 0) { sums[t0 + i * WAVES] = z; bests[t0 + i * WAVES] = best; }
-            most = fmaxf(most, best);
-        }
+        for (int i = 0; i < 4; ++i) x[i].values((int64_t)(t0 + i) * 256, a.in.n, v + 4 * i);
+        if (t0 + 4 * WAVES < tiles) load(t0 + 4 * WAVES);  // (arrives while these are worked on)
+        const float best = best_of_tiles(v);
+        const double z = sum_of_tiles(v, best, scale);
+        const int tile = t0 + tile_of_row(lane >> 4);
+        if ((lane & 15) == 15 && tile < tiles) { sums[tile] = z; bests[tile] = best; most = fmaxf(most, best); }
     }
     most = block_max<WAVES>(most, maxima);
     if (!(most > -INFINITY)) { write_empty<WAVES * 64>(a, row); return; }
     const Kept kept = {-INFINITY, 0u, 0u};
-    draw_from_tiles<DT, WAVES, TILES>(a, row, s, tiles, sums, bests, kept, Weights(most, a.inv_t), 0.0);
+    draw_from_tiles<DT, WAVES, TILES>(a, row, s, tiles, sums, bests, kept, Weights(most, scale), 0.0);
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -431,7 +435,8 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
         draw_from_list<THREADS>(a, row, list, min(count, a.top_k), sums, &kept_entries);
     } else {
         __shared__ double sums[TILES];
-        const Weights weights(best, a.inv_t);
+        const Scale scale(a.inv_t);
+        const Weights weights(best, scale);
         Kept kept = {-INFINITY, 0u, 0u};
         if constexpr (CUT == CUT_WEIGHT) {
             __shared__ CutScratch<WAVES, TPW> scratch;
@@ -448,7 +453,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
 #pragma unroll
             for (int q = 4 * i; q < 4 * i + 4; ++q) {
                 const bool in = CUT == CUT_MIN || v[q] > kept.t || (v[q] == kept.t && low(q) >= kept.least);
-                const double w = in ? weights.of(v[q]) : 0.0;
+                const double w = weights.of(v[q], in);
                 z += w >= a.min_p ? w : 0.0;
             }
             z = wave_sum64(z);
@@ -529,7 +534,8 @@ __device__ __forceinline__ RowCut cut_before(const LongArgs& a, int64_t row, int
     }
     RowCut c = a.cuts[(round - 1) * a.d.in.rows + row];
     if (!(c.best > -INFINITY)) return c;
-    const Weights w(c.best, a.d.inv_t);
+    const Scale scale(a.d.inv_t);
+    const Weights w(c.best, scale);
     if (round == 1 || c.rule.hi > c.rule.lo) {
         const int b = find_bin<256, LOG_BINS>(a.bins + (row * ROUNDS + round - 1) * BINS, c.rule, a.bits, round == 1, a.d.top_p, c.target, c.above, part, found);
         c.rule = next_bins(c.rule, b, w);
@@ -554,7 +560,8 @@ __global__ __launch_bounds__(256) void k_draw_bins(LongArgs a, int round) {
     const RowCut c = cut_before(a, row, round, maxima, found_sum, found);
     if (part == 0 && threadIdx.x == 0) a.cuts[round * a.d.in.rows + row] = c;
     if (!(c.best > -INFINITY) || (round > 0 && c.rule.hi == c.rule.lo)) return;
-    const Weights w(c.best, a.d.inv_t);
+    const Scale scale(a.d.inv_t);
+    const Weights w(c.best, scale);
     for (int b = threadIdx.x; b < BINS; b += 256) bins[b] = 0;
     if (threadIdx.x == 0) noted = 0;
     __syncthreads();
@@ -602,60 +609,76 @@ __global__ __launch_bounds__(256) void k_draw_bins(LongArgs a, int round) {
     if (round == 1 && threadIdx.x == 0) a.notes[block] = noted;
 }
 
-// Sums of what is kept, relative to the row's best score.
+// Sums of what is kept, relative to the row's best score.  (Ranges of groups as in k_tiles.)
 template <int DT>
-__global__ __launch_bounds__(256) void k_draw_sums(LongArgs a) {
-    __shared__ float maxima[4];
-    __shared__ double sums[GROUP_TILES];
-    __shared__ double found_sum[5];
-    __shared__ uint32_t found[2], ties[GROUP_TILES];
-    const int64_t block = flat_block();
-    if (block >= a.d.in.rows * a.groups) return;
-    const int64_t row = block / a.groups, group = block - row * a.groups;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const auto* s = static_cast<const typename Score<DT>::type*>(a.d.in.p) + row * a.d.in.ld;
-    float v[16];
-    load_tiles<DT, 4, 4>(s, group * GROUP, a.d.in.n, v);
-    const RowCut c = a.by_weight ? a.cuts[ROUNDS * a.d.in.rows + row] : cut_before(a, row, 0, maxima, found_sum, found);
-    if (!a.by_weight && group == 0 && threadIdx.x == 0) a.cuts[ROUNDS * a.d.in.rows + row] = c;
-    const float t = c.t ? key_score(c.t) : -INFINITY;
-    const Weights w(c.best, a.d.inv_t);
+__global__ __launch_bounds__(256) void k_draw_sums(LongArgs a, int64_t per) {
+    __shared__ double sums[2][GROUP_TILES];
+    __shared__ uint32_t ties[2][GROUP_TILES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t blocks = a.d.in.rows * a.groups, start = (int64_t)flat_block() * per, end = min(start + per, blocks);
+    if (start >= blocks) return;
+    int64_t row = start / a.groups, group = start - row * a.groups;
+    const auto* scores = static_cast<const typename Score<DT>::type*>(a.d.in.p);
+    Quad<DT> x[4];
+    auto load = [&](int64_t r, int64_t g) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        double z = 0.0;
-        uint32_t e = 0;
-#pragma unroll
-        for (int q = 4 * i; q < 4 * i + 4; ++q) {
-            const double x = v[q] > t ? w.of(v[q]) : 0.0;
-            z += x >= a.d.min_p ? x : 0.0;
-            e += __popcll(__ballot(v[q] == t));
+        for (int i = 0; i < 4; ++i) x[i].load(scores + r * a.d.in.ld, g * GROUP + (wave * 4 + i) * 256 + lane * 4, a.d.in.n);
+    };
+    load(row, group);
+    const Scale scale(a.d.inv_t);
+    float best = -INFINITY, t = -INFINITY;
+    for (int64_t block = start; block < end; ++block) {
+        if (block == start || group == 0) {
+            const RowCut& c = a.cuts[ROUNDS * a.d.in.rows + row];
+            best = c.best;
+            t = c.t ? key_score(c.t) : -INFINITY;
         }
-        z = wave_sum64(z);
-        if (lane == 0) { sums[i * 4 + wave] = z; ties[i * 4 + wave] = c.t ? e : 0; }
-    }
-    __syncthreads();
-    if (threadIdx.x >= 64) return;
-    const double z = lane < GROUP_TILES ? sums[lane] : 0.0;
-    uint32_t e = lane < GROUP_TILES ? ties[lane] : 0;
-    if (lane < GROUP_TILES) {
-        a.tile_best[block * GROUP_TILES + lane] = c.best;
-        a.tile_sum[block * GROUP_TILES + lane] = z;
-        a.tile_ties[block * GROUP_TILES + lane] = e;
-    }
-    const double all = wave_sum64(z);
+        float v[16];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) e += __shfl_xor((int)e, o, 64);
-    if (lane == 0) { a.group_best[block] = c.best; a.group_sum[block] = all; a.group_ties[block] = e; }
+        for (int i = 0; i < 4; ++i) x[i].values(group * GROUP + (wave * 4 + i) * 256, a.d.in.n, v + 4 * i);
+        if (++group == a.groups) { group = 0; ++row; }
+        if (block + 1 < end) load(row, group);
+        const int half = (int)(block - start) & 1;
+        const Weights w(best, scale);
+        double z[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t e = 0;
+            z[i] = 0.0;
+#pragma unroll
+            for (int q = 4 * i; q < 4 * i + 4; ++q) {
+                const double y = w.of(v[q], v[q] > t);
+                z[i] += y >= a.d.min_p ? y : 0.0;
+                e += t > -INFINITY ? __popcll(__ballot(v[q] == t)) : 0;
+            }
+            if (lane == 0) ties[half][wave * 4 + i] = e;
+        }
+        const double sum = sum_four(z);
+        if ((lane & 15) == 15) sums[half][wave * 4 + tile_of_row(lane >> 4)] = sum;
+        __syncthreads();
+        if (wave != (int)(block & 3)) continue;
+        const double y = lane < GROUP_TILES ? sums[half][lane] : 0.0;
+        uint32_t e = lane < GROUP_TILES ? ties[half][lane] : 0;
+        if (lane < GROUP_TILES) {
+            a.tile_best[block * GROUP_TILES + lane] = best;
+            a.tile_sum[block * GROUP_TILES + lane] = y;
+            a.tile_ties[block * GROUP_TILES + lane] = e;
+        }
+        const double all = wave_sum64(y);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) e += __shfl_xor((int)e, o, 64);
+        if (lane == 0) { a.group_best[block] = best; a.group_sum[block] = all; a.group_ties[block] = e; }
+    }
 }
 
-// The result of the rounds, once for all workgroups of k_draw_sums.
+// The result of the rounds, or with min-p alone the row's best score, once for all workgroups of k_draw_sums.
 __global__ __launch_bounds__(256) void k_draw_cut(LongArgs a) {
     __shared__ float maxima[4];
     __shared__ double found_sum[5];
     __shared__ uint32_t found[2];
     const int64_t row = flat_block();
     if (row >= a.d.in.rows) return;
-    const RowCut c = cut_before(a, row, ROUNDS, maxima, found_sum, found);
+    const RowCut c = cut_before(a, row, a.by_weight ? ROUNDS : 0, maxima, found_sum, found);
     if (threadIdx.x == 0) a.cuts[ROUNDS * a.d.in.rows + row] = c;
 }
 
@@ -682,7 +705,8 @@ __global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a, int cut) {
     float best = -INFINITY;
     for (int64_t g = threadIdx.x; g < a.groups; g += 1024) best = fmaxf(best, bests[g]);
     best = block_max<16>(best, maxima);
-    const Weights weights(best, a.d.inv_t);
+    const Scale scale(a.d.inv_t);
+    const Weights weights(best, scale);
     uint32_t t = 0, most = 0;
     double each = 0.0;
     if (cut) {
@@ -764,7 +788,8 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
     }
     while (lo > 0 && !(sums[lo] > sums[lo - 1])) --lo;  // (never a group without weight)
     const int64_t group = row * a.groups + lo;
-    const Weights weights(best, a.d.inv_t);
+    const Scale scale(a.d.inv_t);
+    const Weights weights(best, scale);
     double base = lo > 0 ? sums[lo - 1] : 0.0, v = 0.0;
     uint32_t e = 0, before = 0;
     if (lane < GROUP_TILES) {
@@ -873,9 +898,12 @@ void launch(const DrawArgs& d, void* workspace, hipStream_t st) {
     const dim3 rows = flat_grid(d.in.rows);
     if (by_weight) {
         for (int round = 0; round < ROUNDS; ++round) k_draw_bins<DT><<<flat_grid(d.in.rows * a.parts), 256, 0, st>>>(a, round);
-        k_draw_cut<<<rows, 256, 0, st>>>(a);
     }
-    if (cut) k_draw_sums<DT><<<flat_grid(d.in.rows * a.groups), 256, 0, st>>>(a);
+    if (cut) {
+        const int64_t blocks = d.in.rows * a.groups, per = groups_per_workgroup(blocks);
+        k_draw_cut<<<rows, 256, 0, st>>>(a);
+        k_draw_sums<DT><<<flat_grid(pieces(blocks, per)), 256, 0, st>>>(a, per);
+    }
     k_draw_scan<<<rows, 1024, 0, st>>>(a, cut);
     k_draw_pick<DT><<<flat_grid(pieces(d.in.rows * d.draws, 4)), 256, 0, st>>>(a);
 }

@@ -8,6 +8,8 @@
 // becomes an unsigned key of the same order (0: masked; -0 counts as +0), and key and position together a 64-bit number
 // that is unique in its row.
 #pragma once
+#include <type_traits>
+
 #include "kge_common.h"
 
 constexpr int KGE_TOP_MAX = 1024;           // longest list of best candidates
@@ -35,8 +37,11 @@ struct TileArgs {
     float* group_worst;   // lowest score that is not masked, +inf without one; may be null (only without sums)
     uint64_t* clear;      // [rows][clear_words] that the pass sets to 0, may be null
     int64_t clear_words;
+    int64_t per;          // groups of a workgroup (set by the launcher)
 };
-void kge_launch_tiles(const TileArgs& a, bool sums, hipStream_t st);
+// Groups in a row for each of the workgroups of 256 threads that fill the chip, 8 per CU.
+inline int64_t groups_per_workgroup(int64_t groups) { return pieces(groups, 2048); }
+void kge_launch_tiles(TileArgs a, bool sums, hipStream_t st);
 
 int64_t kge_top_workspace(int64_t rows, int64_t n, int m);
 // (ids and scores, or the sorted entries alone; lse may be null)
@@ -84,21 +89,40 @@ template <int DT> __device__ __forceinline__ typename Score<DT>::type narrow(flo
     else return __builtin_bit_cast(unsigned short, (_Float16)v);
 }
 
-// Scores j .. j + 3 of a row of n, -inf behind its end.  (Rows start at any multiple of a score's size.)
-template <int DT> __device__ __forceinline__ void load4(const typename Score<DT>::type* row, int64_t j, int64_t n, float v[4]) {
-    if (j + 4 <= n) {
-        if constexpr (DT == KGE_F32) {
-            const f32x4u x = *reinterpret_cast<const f32x4u*>(row + j);
-            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-        } else {
-            const u16x4u x = *reinterpret_cast<const u16x4u*>(row + j);
-            v[0] = widen<DT>(x.x); v[1] = widen<DT>(x.y); v[2] = widen<DT>(x.z); v[3] = widen<DT>(x.w);
+// The 4 scores of a lane from position j of a row of n on, -inf behind its end.  (Rows start at any multiple of a score's
+// size.)  The load is the same whatever the position, so that many are in flight: a lane at or behind the end reads the row's last four
+// scores, and those of the tile that the row ends in are moved into place when the values are used.
+template <int DT> struct Quad {
+    using Vec = typename std::conditional<DT == KGE_F32, f32x4u, u16x4u>::type;
+    Vec raw;
+    __device__ __forceinline__ void load(const typename Score<DT>::type* row, int64_t j, int64_t n) {
+        if (n >= 4) {
+            raw = *reinterpret_cast<const Vec*>(row + min(j, n - 4));
+        } else {  // (the positions of a row this short are 0 .. 3; what is behind its end is not used)
+            raw.x = row[0];
+            raw.y = row[min((int64_t)1, n - 1)];
+            raw.z = row[n - 1];
+            raw.w = row[n - 1];
         }
-    } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = j + q < n ? widen<DT>(row[j + q]) : -INFINITY;
     }
-}
+    // first: of the tile, 256 scores that the wave holds.  MASK: NaN becomes -inf
+    template <bool MASK = true> __device__ __forceinline__ void values(int64_t first, int64_t n, float v[4]) const {
+        v[0] = widen<DT>(raw.x); v[1] = widen<DT>(raw.y); v[2] = widen<DT>(raw.z); v[3] = widen<DT>(raw.w);
+        if (first + 256 > n) {
+            const int64_t j = first + (threadIdx.x & 63) * 4, beyond = n >= 4 ? j - (n - 4) : 0;
+#pragma unroll
+            for (int k = 1; k <= 4; ++k) {
+                if (beyond >= k) { v[0] = v[1]; v[1] = v[2]; v[2] = v[3]; v[3] = -INFINITY; }
+            }
+            if (n < 4) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) if (j + q >= n) v[q] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) if (MASK) v[q] = fmaxf(v[q], -INFINITY);
+    }
+};
 
 __device__ __forceinline__ uint32_t order_key(float s) {
     const uint32_t u = __float_as_uint(s + 0.f);  // -0 -> +0
@@ -112,41 +136,50 @@ __device__ __forceinline__ int64_t entry_position(uint64_t e) { return (int64_t)
 
 // exp((s - best) / T) in 64 bits, 0 of a masked score (-inf): which candidate a random number falls on is decided by sums of these, and
 // the sums of 32-bit weights would move thousands of borders by more than the numbers' spacing.  As p * 2^n: n the whole number nearest to
-// the exponent of 2 (its low bits appear where 1.5 * 2^52 is added), p the polynomial of degree 10 that interpolates exp2 on
-// [-1/2, 1/2] at the Chebyshev nodes, off by 3e-16.  About 20 instructions where the library's exp takes twice as many; of the
+// the exponent of 2 (its low bits appear where 1.5 * 2^52 is added), p the polynomial of degree 9 that interpolates exp2 on
+// [-1/2, 1/2] at the Chebyshev nodes, off by 4e-14.  About 20 instructions where the library's exp takes twice as many; of the
 // kernels that form a weight per score they are what bounds it beside the reads: 64 scores take a SIMD some 90 cycles.
+struct Scale {  // what all weights of a kernel have in common
+    double per, c[9];  // log2(e) / T; coefficients
+    float far;         // a weight 2^-1000 lies that far below the best score
+    __device__ __forceinline__ explicit Scale(double inv_t) : per(inv_t * 1.4426950408889634),
+        c{0x1.62e42fefa39f7p-1, 0x1.ebfbdff8149f2p-3, 0x1.c6b08d7044119p-5, 0x1.3b2ab72b175eep-7, 0x1.5d87fe908f88ap-10, 0x1.43088e257f341p-13,
+          0x1.ffcb76789860fp-17, 0x1.63ef969a64d3cp-20, 0x1.b6571de2f2351p-24}, far((float)fmin(1000.0 / per, 3.4e38)) {
+        // (in scalar registers: a coefficient in a vector register is copied for every step, the instruction adds to its own output)
+#pragma unroll
+        for (int i = 0; i < 9; ++i) asm("" : "+s"(c[i]));
+    }
+};
 struct Weights {
-    double best, scale;  // best score, log2(e) / T
-    float floor;         // scores below have a weight of 0 (2^-1000 and less)
-    __device__ __forceinline__ Weights(float b, double inv_t) : scale(inv_t * 1.4426950408889634) {
-        floor = (float)fmax((double)b - 1000.0 / scale, -3.402823466e38);  // (b = +inf: above every number)
+    const Scale& scale;
+    double best;
+    float floor;  // scores below have a weight of 0: 2^-1000 and less, or that of no number between the floor and the best
+    __device__ __forceinline__ Weights(float b, const Scale& s) : scale(s) {
+        const float f = b - s.far;
+        floor = fmaxf(fminf(b, fmaf(fabsf(f), 0x1p-22f, f)), -3.402823466e38f);  // (rounded up; b = +inf: above every number)
         best = (double)fminf(b, 3.402823466e38f);
     }
     __device__ __forceinline__ bool none(float s) const { return !(s >= floor); }
     __device__ __forceinline__ void split(float s, double& p, int& n) const {
-        const double x = ((double)__builtin_amdgcn_fmed3f(s, fminf(floor, 3.402823466e38f), 3.402823466e38f) - best) * scale;
+        const double x = ((double)__builtin_amdgcn_fmed3f(s, fminf(floor, 3.402823466e38f), 3.402823466e38f) - best) * scale.per;
         const double shifted = x + 0x1.8p52, f = x - (shifted - 0x1.8p52);
         n = __double2loint(shifted);
-        p = 0x1.e6063f7217bc6p-28;
-        p = fma(p, f, 0x1.b675bca4eeebbp-24);
-        p = fma(p, f, 0x1.62bfd47773353p-20);
-        p = fma(p, f, 0x1.ffcb54062e698p-17);
-        p = fma(p, f, 0x1.430913096fd9fp-13);
-        p = fma(p, f, 0x1.5d87fe9d7a584p-10);
-        p = fma(p, f, 0x1.3b2ab6fba1ddap-7);
-        p = fma(p, f, 0x1.c6b08d703ce49p-5);
-        p = fma(p, f, 0x1.ebfbdff82c598p-3);
-        p = fma(p, f, 0x1.62e42fefa3a19p-1);
+        p = scale.c[8];
+#pragma unroll
+        for (int i = 7; i >= 0; --i) p = fma(p, f, scale.c[i]);
         p = fma(p, f, 1.0);
     }
     static __device__ __forceinline__ double scaled(double p, int n) {  // p * 2^n, p and the result normal numbers
         return __hiloint2double(__double2hiint(p) + (n << 20), __double2loint(p));
     }
-    __device__ __forceinline__ double of(float s) const {
+    // (masked by its bits: a choice between it and 0 would become a branch around every weight)
+    __device__ __forceinline__ double of(float s, bool keep = true) const {
         double p;
         int n;
         split(s, p, n);
-        return none(s) ? 0.0 : scaled(p, n);
+        const int mask = keep && !none(s) ? -1 : 0;
+        p = scaled(p, n);
+        return __hiloint2double(__double2hiint(p) & mask, __double2loint(p) & mask);
     }
 };
 
@@ -170,9 +203,49 @@ __device__ __forceinline__ double lane64(double v, int lane) {  // of one lane, 
     return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
 }
 __device__ __forceinline__ double wave_sum64(double v) { return lane64(wave_scan64(v, 0), 63); }
+// Of four tiles at once: the halves of two tiles' values are joined in one register, then the quarters of four, so that the steps within a row of 16
+// lanes serve all.  Lane 15 of row k ends with the tile k = 0, 2, 1, 3.
+__device__ __forceinline__ int row_of_tile(int i) { return i == 1 ? 2 : i == 2 ? 1 : i; }
+__device__ __forceinline__ void swap32(int& a, int& b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = r[0]; b = r[1];
+}
+__device__ __forceinline__ void swap16(int& a, int& b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0]; b = r[1];
+}
+template <bool HALVES> __device__ __forceinline__ double join64(double a, double b) {
+    int al = __double2loint(a), ah = __double2hiint(a), bl = __double2loint(b), bh = __double2hiint(b);
+    if (HALVES) { swap32(al, bl); swap32(ah, bh); }
+    else { swap16(al, bl); swap16(ah, bh); }
+    return __hiloint2double(ah, al) + __hiloint2double(bh, bl);
+}
+__device__ __forceinline__ double sum_four(const double z[4]) {
+    double v = join64<false>(join64<true>(z[0], z[1]), join64<true>(z[2], z[3]));
+    v += moved64<ROW_SHR + 1, 0xf>(v);
+    v += moved64<ROW_SHR + 2, 0xf>(v);
+    v += moved64<ROW_SHR + 4, 0xf>(v);
+    v += moved64<ROW_SHR + 8, 0xf>(v);
+    return v;
+}
+template <bool HALVES> __device__ __forceinline__ float join_max(float a, float b) {
+    int x = __float_as_int(a), y = __float_as_int(b);
+    if (HALVES) swap32(x, y);
+    else swap16(x, y);
+    return fmaxf(__int_as_float(x), __int_as_float(y));
+}
+
 template <int CTRL, int ROWS> __device__ __forceinline__ float max_moved(float v) {
     return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(-INFINITY), __float_as_int(v), CTRL, ROWS, 0xf, false)));
 }
+__device__ __forceinline__ float max_four(const float z[4]) {
+    float v = join_max<false>(join_max<true>(z[0], z[1]), join_max<true>(z[2], z[3]));
+    v = max_moved<ROW_SHR + 1, 0xf>(v);
+    v = max_moved<ROW_SHR + 2, 0xf>(v);
+    v = max_moved<ROW_SHR + 4, 0xf>(v);
+    return max_moved<ROW_SHR + 8, 0xf>(v);
+}
+__device__ __forceinline__ float of_tile(float v, int i) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), row_of_tile(i) * 16 + 15)); }
 __device__ __forceinline__ float wave_most(float v) {
     v = max_moved<ROW_SHR + 1, 0xf>(v);
     v = max_moved<ROW_SHR + 2, 0xf>(v);
@@ -206,20 +279,40 @@ template <int WAVES> __device__ __forceinline__ float block_max(float v, float* 
     return v;
 }
 
-// The tiles of a workgroup in registers, masked scores as -inf; returns this thread's largest.
+// The tiles of a workgroup in registers; returns this thread's largest score.
 template <int DT, int WAVES, int TPW>
 __device__ __forceinline__ float load_tiles(const typename Score<DT>::type* row, int64_t first, int64_t n, float v[TPW * 4]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Quad<DT> x[TPW];
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) x[i].load(row, first + (i * WAVES + wave) * 256 + lane * 4, n);
     float best = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < TPW; ++i) load4<DT>(row, first + (int64_t)(i * WAVES + wave) * 256 + lane * 4, n, v + 4 * i);
-#pragma unroll
-    for (int q = 0; q < TPW * 4; ++q) {
-        v[q] = fmaxf(v[q], -INFINITY);  // (NaN: -inf)
-        best = fmaxf(best, v[q]);
+    for (int i = 0; i < TPW; ++i) {
+        x[i].values(first + (i * WAVES + wave) * 256, n, v + 4 * i);
+        best = fmaxf(best, fmaxf(fmaxf(v[4 * i], v[4 * i + 1]), fmaxf(v[4 * i + 2], v[4 * i + 3])));
     }
     return best;
 }
+
+// Best scores and sums of weights of four tiles that a wave holds.  The sums (and bests) are in lane 15 of the rows, see sum_four.
+__device__ __forceinline__ float best_of_tiles(const float v[16]) {
+    float m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = fmaxf(fmaxf(v[4 * i], v[4 * i + 1]), fmaxf(v[4 * i + 2], v[4 * i + 3]));
+    return max_four(m);
+}
+__device__ __forceinline__ double sum_of_tiles(const float v[16], float bests, const Scale& scale) {
+    double z[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Weights w(of_tile(bests, i), scale);
+        z[i] = (w.of(v[4 * i]) + w.of(v[4 * i + 1])) + (w.of(v[4 * i + 2]) + w.of(v[4 * i + 3]));
+    }
+    return sum_four(z);
+}
+__device__ __forceinline__ int tile_of_row(int row) { return row == 1 ? 2 : row == 2 ? 1 : row; }
+
 template <int WAVES> __device__ __forceinline__ int tile_position(int q) {  // of register q, in the workgroup's tiles
     return ((q / 4) * WAVES + (int)(threadIdx.x >> 6)) * 256 + (int)(threadIdx.x & 63) * 4 + q % 4;
 }

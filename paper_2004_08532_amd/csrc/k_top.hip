@@ -50,7 +50,8 @@ __global__ __launch_bounds__(WAVES * 64) void k_top_rows(TopArgs a) {
     if (a.want_lse) {
         double z = 0.0;
         if (!empty) {
-            const Weights w(best, a.inv_t);
+            const Scale scale(a.inv_t);
+            const Weights w(best, scale);
 #pragma unroll
             for (int q = 0; q < TPW * 4; ++q) z += w.of(v[q]);
             z = block_sum64<WAVES>(z, sums);
@@ -119,7 +120,8 @@ __global__ __launch_bounds__(WAVES * 64) void k_top_merge(MergeArgs a) {
     write_list<THREADS>(list, count, a.m, a.ids + row * a.m, a.scores + row * a.m);
     if (a.parts) {
         const double* p = a.parts + 2 * row * a.segments;
-        const Weights w(best, a.inv_t);
+        const Scale scale(a.inv_t);
+        const Weights w(best, scale);
         double z = 0.0;
         for (int g = threadIdx.x; g < a.segments; g += THREADS)
             if (p[2 * g + 1] > 0.0) z += p[2 * g + 1] * w.of((float)p[2 * g]);

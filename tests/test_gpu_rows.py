@@ -168,6 +168,18 @@ def test_sample(kge, rows, n, draws, setting):
     check_sample(kge, rows_of(x, dtype, pad=n % 4, offset=n % 3), u, **SETTINGS[setting])
 
 
+@pytest.mark.parametrize("size", [1e6, 1e10, 1e30])
+@pytest.mark.parametrize("n", [50, 900, 6000, 80_000])
+def test_sample_of_large_scores(kge, n, size):
+    """Neighbouring numbers are further apart than the scores that matter; small temperatures and large ones."""
+    g = np.random.default_rng(n)
+    x = (size * (1 + 2.0 ** -23 * g.integers(-3, 4, (3, n)))).astype(np.float32)
+    x[1] = -x[1]
+    for T in (1.0, 1e-3, size * 2.0 ** -23):
+        check_sample(kge, rows_of(torch.from_numpy(x)), g.random((3, 9)), T=T)
+        check_sample(kge, rows_of(torch.from_numpy(x)), g.random((3, 9)), T=T, top_p=0.8)
+
+
 @pytest.mark.parametrize("setting", range(len(SETTINGS)))
 @pytest.mark.parametrize("n", [50, 900, 6000, 33_000, 80_000])
 def test_sample_of_equal_and_extreme_scores(kge, n, setting):
