@@ -28,18 +28,27 @@ template <int THREADS> __device__ __forceinline__ void write_empty(const DrawArg
     }
 }
 
-// What is kept, of scores with a weight of at least min_p: those above t, and of those equal to it the ones whose inverted position is
-// at least `least`, or the first `ties` of the row.
+// What is kept: the scores above `over`, and of those equal to t the ones whose inverted position is at least `least` (in rows held by a
+// workgroup) or the first `ties` of the row (in long ones).  t is not above `over`; NaN: none of them.
 struct Kept {
-    float t;
+    float over, t;
     uint32_t least, ties;
 };
+// The weights of what is kept are at least min_p and not 0.  (Asked by a whole wave.)
+__device__ __forceinline__ void keep_from_min_p(Kept& k, const Weights& w, float best, double min_p) {
+    float least = w.floor;
+    if (min_p > 0.0) {
+        least = key_score(lowest_key(order_key(least), order_key(best), [&](uint32_t key) { return w.of(key_score(key)) >= min_p; }));
+    }
+    if (!(k.t >= least)) k.t = __uint_as_float(0x7FC00000u);
+    k.over = fmaxf(k.over, score_below(least));
+}
 
 // Position in a tile (256 scores from `first` on) at which the sum passes `target`, `base` of it in front of the tile; the tile's
 // last kept position where rounding leaves none.  COUNTED: equal scores are kept by `ties`, `ties_before` of them lie in front of the tile.
 template <int DT, bool COUNTED>
-__device__ __forceinline__ void draw_in_tile(const typename Score<DT>::type* s, int64_t first, int64_t n, const Kept& k, const Weights& weights, double min_p,
-                                             uint32_t ties_before, double base, double target, int lane, int64_t& id, double& weight) {
+__device__ __forceinline__ void draw_in_tile(const typename Score<DT>::type* s, int64_t first, int64_t n, const Kept& k, const Weights& weights, uint32_t ties_before,
+                                             double base, double target, int lane, int64_t& id, double& weight) {
     float v[4];
     Quad<DT> x;
     x.load(s, first + lane * 4, n);
@@ -53,10 +62,9 @@ __device__ __forceinline__ void draw_in_tile(const typename Score<DT>::type* s, 
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const bool equal = v[q] == k.t, in = v[q] > k.t || (equal && (COUNTED ? rank < k.ties : ~(uint32_t)(first + lane * 4 + q) >= k.least));
-        w[q] = weights.of(v[q], in);
+        const bool equal = v[q] == k.t;
+        w[q] = weights.of(v[q], v[q] > k.over || (equal && (COUNTED ? rank < k.ties : ~(uint32_t)(first + lane * 4 + q) >= k.least)));
         rank += equal;
-        if (!(w[q] >= min_p)) w[q] = 0.0;
         sum += w[q];
     }
     const double incl = base + wave_scan64(sum, lane);
@@ -132,7 +140,7 @@ __device__ __forceinline__ void draw_from_list(const DrawArgs& a, int64_t row, u
 // The draws of a row whose tile sums a workgroup has in LDS.  sums[t]: of tile t, relative to best[t] (a row's best where that is null).
 template <int DT, int WAVES, int TILES>
 __device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, const typename Score<DT>::type* s, int tiles, double* sums,
-                                                const float* tile_best, const Kept& kept, const Weights& weights, double min_p) {
+                                                const float* tile_best, const Kept& kept, const Weights& weights) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     __syncthreads();
     if (wave == 0) {  // running sums
@@ -163,7 +171,7 @@ __device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, 
         if (tile < 0) tile = fallback;
         int64_t id = -1;
         double weight = 0.0;
-        draw_in_tile<DT, false>(s, (int64_t)tile * 256, a.in.n, kept, weights, min_p, 0u, tile > 0 ? sums[tile - 1] : 0.0, want, lane, id, weight);
+        draw_in_tile<DT, false>(s, (int64_t)tile * 256, a.in.n, kept, weights, 0u, tile > 0 ? sums[tile - 1] : 0.0, want, lane, id, weight);
         if (lane == 0) {
             a.ids[row * a.draws + d] = id;
             if (a.logp) a.logp[row * a.draws + d] = (float)log(weight / total);
@@ -201,8 +209,9 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_whole(DrawArgs a) {
     }
     most = block_max<WAVES>(most, maxima);
     if (!(most > -INFINITY)) { write_empty<WAVES * 64>(a, row); return; }
-    const Kept kept = {-INFINITY, 0u, 0u};
-    draw_from_tiles<DT, WAVES, TILES>(a, row, s, tiles, sums, bests, kept, Weights(most, scale), 0.0);
+    const Weights weights(most, scale);
+    const Kept kept = {score_below(weights.floor), __uint_as_float(0x7FC00000u), 0u, 0u};
+    draw_from_tiles<DT, WAVES, TILES>(a, row, s, tiles, sums, bests, kept, weights);
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -218,7 +227,7 @@ template <int LOG_BINS> struct BinRule {
     uint32_t lo, hi;   // interval of keys
     int shift;         // keys per bin: 2^shift; negative: bins of equal width
     float best, per;   // bins per unit of the score
-    double drop;       // exponents per bin
+    float drop;        // exponents per bin
     int top;           // exponent at the interval's upper end
     __device__ __forceinline__ int bin(float s) const {
         if (shift < 0) {
@@ -228,7 +237,7 @@ template <int LOG_BINS> struct BinRule {
         return (int)((hi - order_key(s)) >> shift);
     }
     __device__ __forceinline__ bool in(float s) const { return s >= key_score(lo) && s <= key_score(hi); }
-    __device__ __forceinline__ int exponent(int b) const { return shift < 0 ? (int)floor(-(double)b * drop) : top; }
+    __device__ __forceinline__ int exponent(int b) const { return shift < 0 ? (int)floorf(-(float)b * drop) : top; }
 };
 
 // Rule of the first round.
@@ -239,7 +248,7 @@ template <int LOG_BINS> __device__ __forceinline__ BinRule<LOG_BINS> first_bins(
     r.shift = -1; r.best = best;
     const float range = fminf(best - worst, (float)fmin(40.0 / inv_t, 3e38));
     r.per = range > 0.f ? (float)BINS / range : 0.f;
-    r.drop = r.per > 0.f ? inv_t * 1.4426950408889634 / (double)r.per : 0.0;
+    r.drop = r.per > 0.f ? (float)(inv_t * 1.4426950408889634 / (double)r.per) : 0.f;
     r.top = 0;
     return r;
 }
@@ -247,18 +256,8 @@ template <int LOG_BINS> __device__ __forceinline__ BinRule<LOG_BINS> first_bins(
 template <int LOG_BINS> __device__ __forceinline__ BinRule<LOG_BINS> next_bins(const BinRule<LOG_BINS>& r, int b, const Weights& w) {
     BinRule<LOG_BINS> x = r;
     if (r.shift < 0) {  // the keys whose bin is b: a larger key never has a larger bin
-        uint32_t lo = r.lo, hi = r.hi;
-        while (lo < hi) {  // the lowest key whose bin is at most b
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (r.bin(key_score(mid)) <= b) hi = mid; else lo = mid + 1;
-        }
-        x.lo = lo;
-        hi = r.hi;
-        while (lo < hi) {  // the highest whose bin is at least b
-            const uint32_t mid = lo + (hi - lo) / 2 + ((hi - lo) & 1);
-            if (r.bin(key_score(mid)) >= b) lo = mid; else hi = mid - 1;
-        }
-        x.hi = lo;
+        x.lo = lowest_key(r.lo, r.hi, [&](uint32_t key) { return r.bin(key_score(key)) <= b; });
+        x.hi = b > 0 ? lowest_key(r.lo, r.hi, [&](uint32_t key) { return r.bin(key_score(key)) < b; }) - 1 : r.hi;
     } else {
         x.hi = r.hi - ((uint32_t)b << r.shift);
         const uint32_t last = ((uint32_t)1 << r.shift) - 1;
@@ -275,7 +274,7 @@ __device__ __forceinline__ uint64_t whole_weight(const Weights& w, float s, int 
     int n;
     w.split(s, p, n);
     const int up = n - exponent + bits;
-    if (w.none(s) || up < -2) return 0;
+    if (!(s >= w.floor) || up < -2) return 0;
     return (uint64_t)__double_as_longlong(Weights::scaled(p, up) + 0x1p52) & (((uint64_t)1 << 52) - 1);
 }
 
@@ -377,11 +376,12 @@ __device__ __forceinline__ Kept cut_by_weight(float v[TPW * 4], const L& low, fl
         count = block_count<WAVES>(c, s.slots);
         if (count <= ROOM || r.lo == r.hi) break;
     }
-    Kept kept = {key_score(r.hi), 0u, 0u};
+    Kept kept = {key_score(r.hi), key_score(r.hi), 0u, 0u};
     __syncthreads();
     if (count > ROOM) {  // all equal: as many as it takes, the first ones
         const double need = ceil((target - above) / w.of(kept.t));
         if (need < count) kept.least = select_equal<WAVES, N>(v, kept.t, low, need < 1.0 ? 1 : (int)need, s.slots);
+        else kept.over = score_below(kept.t);
         return kept;
     }
     if (threadIdx.x == 0) s.count = 0;
@@ -402,11 +402,15 @@ __device__ __forceinline__ Kept cut_by_weight(float v[TPW * 4], const L& low, fl
             if (there) { cut = e0 + __ffsll((unsigned long long)there) - 1; break; }
             carry = lane64(x, 63);
         }
-        if (lane == 0) { s.found[0] = (uint32_t)(list[cut] >> 32); s.found[1] = (uint32_t)list[cut]; }
+        if (lane == 0) {  // (no other score like it behind the cut: all of them are kept)
+            s.found[0] = (uint32_t)(list[cut] >> 32);
+            s.found[1] = cut + 1 < count && (uint32_t)(list[cut + 1] >> 32) == s.found[0] ? (uint32_t)list[cut] : 0u;
+        }
     }
     __syncthreads();
-    kept.t = key_score(s.found[0]);
+    kept.t = kept.over = key_score(s.found[0]);
     kept.least = s.found[1];
+    if (kept.least == 0) kept.over = score_below(kept.t);
     return kept;
 }
 
@@ -437,7 +441,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
         __shared__ double sums[TILES];
         const Scale scale(a.inv_t);
         const Weights weights(best, scale);
-        Kept kept = {-INFINITY, 0u, 0u};
+        Kept kept = {-INFINITY, __uint_as_float(0x7FC00000u), 0u, 0u};
         if constexpr (CUT == CUT_WEIGHT) {
             __shared__ CutScratch<WAVES, TPW> scratch;
             float worst = INFINITY;
@@ -447,19 +451,30 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
             kept = cut_by_weight<WAVES, TPW>(v, low, best, worst, weights, a.inv_t, a.top_p, scratch);
             forget<N>(v);
         }
+        keep_from_min_p(kept, weights, best, a.min_p);
+        const bool some = CUT == CUT_WEIGHT && kept.least > 0;  // of the equal ones some are not kept
+        double four[4];
 #pragma unroll
         for (int i = 0; i < TPW; ++i) {
             double z = 0.0;
 #pragma unroll
-            for (int q = 4 * i; q < 4 * i + 4; ++q) {
-                const bool in = CUT == CUT_MIN || v[q] > kept.t || (v[q] == kept.t && low(q) >= kept.least);
-                const double w = weights.of(v[q], in);
-                z += w >= a.min_p ? w : 0.0;
+            for (int q = 4 * i; q < 4 * i + 4; ++q) z += weights.of(v[q], v[q] > kept.over);
+            if (some) {
+#pragma unroll
+                for (int q = 4 * i; q < 4 * i + 4; ++q) if (v[q] == kept.t && low(q) >= kept.least) z += weights.of(v[q]);
             }
-            z = wave_sum64(z);
-            if (lane == 0) sums[i * WAVES + wave] = z;
+            if constexpr (TPW % 4 == 0) {
+                four[i % 4] = z;
+                if (i % 4 == 3) {
+                    z = sum_four(four);
+                    if ((lane & 15) == 15) sums[(i - 3 + tile_of_row(lane >> 4)) * WAVES + wave] = z;
+                }
+            } else {
+                z = wave_sum64(z);
+                if (lane == 0) sums[i * WAVES + wave] = z;
+            }
         }
-        draw_from_tiles<DT, WAVES, TILES>(a, row, s, TILES, sums, nullptr, kept, weights, a.min_p);
+        draw_from_tiles<DT, WAVES, TILES>(a, row, s, TILES, sums, nullptr, kept, weights);
     }
 }
 
@@ -497,7 +512,8 @@ struct RowCut {
     BinRule<LOG_BINS> rule;
     double target, above;
     float best;
-    uint32_t t, ties;  // the result, t = 0: nothing is cut by weight
+    uint32_t equal;    // scores of the interval, where it is a single key
+    Kept kept;         // the result
 };
 
 struct LongArgs {
@@ -537,13 +553,20 @@ __device__ __forceinline__ RowCut cut_before(const LongArgs& a, int64_t row, int
     const Scale scale(a.d.inv_t);
     const Weights w(c.best, scale);
     if (round == 1 || c.rule.hi > c.rule.lo) {
-        const int b = find_bin<256, LOG_BINS>(a.bins + (row * ROUNDS + round - 1) * BINS, c.rule, a.bits, round == 1, a.d.top_p, c.target, c.above, part, found);
+        const uint64_t* bins = a.bins + (row * ROUNDS + round - 1) * BINS;
+        const int b = find_bin<256, LOG_BINS>(bins, c.rule, a.bits, round == 1, a.d.top_p, c.target, c.above, part, found);
+        const int exponent = c.rule.exponent(b);
         c.rule = next_bins(c.rule, b, w);
+        if (c.rule.hi == c.rule.lo) {  // every score added the same number
+            const uint64_t each = whole_weight(w, key_score(c.rule.hi), exponent, a.bits);
+            c.equal = each ? (uint32_t)((bins[b] + each / 2) / each) : 0u;
+        }
     }
     if (round == ROUNDS) {
-        c.t = c.rule.hi;
-        const double need = ceil((c.target - c.above) / w.of(key_score(c.t)));
-        c.ties = need >= 4294967295.0 ? 0xFFFFFFFFu : need < 1.0 ? 1u : (uint32_t)need;
+        const float t = key_score(c.rule.hi);
+        const double need = ceil((c.target - c.above) / w.of(t));
+        const bool all = need >= (double)c.equal;
+        c.kept = {all ? score_below(t) : t, all ? __uint_as_float(0x7FC00000u) : t, 0u, all ? 0u : need < 1.0 ? 1u : (uint32_t)need};
     }
     return c;
 }
@@ -626,12 +649,13 @@ __global__ __launch_bounds__(256) void k_draw_sums(LongArgs a, int64_t per) {
     };
     load(row, group);
     const Scale scale(a.d.inv_t);
-    float best = -INFINITY, t = -INFINITY;
+    float best = -INFINITY;
+    Kept kept = {};
     for (int64_t block = start; block < end; ++block) {
         if (block == start || group == 0) {
             const RowCut& c = a.cuts[ROUNDS * a.d.in.rows + row];
             best = c.best;
-            t = c.t ? key_score(c.t) : -INFINITY;
+            kept = c.kept;
         }
         float v[16];
 #pragma unroll
@@ -643,22 +667,25 @@ __global__ __launch_bounds__(256) void k_draw_sums(LongArgs a, int64_t per) {
         double z[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            uint32_t e = 0;
             z[i] = 0.0;
 #pragma unroll
-            for (int q = 4 * i; q < 4 * i + 4; ++q) {
-                const double y = w.of(v[q], v[q] > t);
-                z[i] += y >= a.d.min_p ? y : 0.0;
-                e += t > -INFINITY ? __popcll(__ballot(v[q] == t)) : 0;
+            for (int q = 4 * i; q < 4 * i + 4; ++q) z[i] += w.of(v[q], v[q] > kept.over);
+        }
+        if (kept.ties) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t e = 0;
+#pragma unroll
+                for (int q = 4 * i; q < 4 * i + 4; ++q) e += __popcll(__ballot(v[q] == kept.t));
+                if (lane == 0) ties[half][wave * 4 + i] = e;
             }
-            if (lane == 0) ties[half][wave * 4 + i] = e;
         }
         const double sum = sum_four(z);
         if ((lane & 15) == 15) sums[half][wave * 4 + tile_of_row(lane >> 4)] = sum;
         __syncthreads();
         if (wave != (int)(block & 3)) continue;
         const double y = lane < GROUP_TILES ? sums[half][lane] : 0.0;
-        uint32_t e = lane < GROUP_TILES ? ties[half][lane] : 0;
+        uint32_t e = kept.ties && lane < GROUP_TILES ? ties[half][lane] : 0;
         if (lane < GROUP_TILES) {
             a.tile_best[block * GROUP_TILES + lane] = best;
             a.tile_sum[block * GROUP_TILES + lane] = y;
@@ -678,7 +705,13 @@ __global__ __launch_bounds__(256) void k_draw_cut(LongArgs a) {
     __shared__ uint32_t found[2];
     const int64_t row = flat_block();
     if (row >= a.d.in.rows) return;
-    const RowCut c = cut_before(a, row, a.by_weight ? ROUNDS : 0, maxima, found_sum, found);
+    RowCut c = cut_before(a, row, a.by_weight ? ROUNDS : 0, maxima, found_sum, found);
+    if (!a.by_weight) c.kept = {-INFINITY, __uint_as_float(0x7FC00000u), 0u, 0u};
+    if (c.best > -INFINITY) {
+        const Scale scale(a.d.inv_t);
+        keep_from_min_p(c.kept, Weights(c.best, scale), c.best, a.d.min_p);
+        if (!(c.kept.t == c.kept.t)) c.kept.ties = 0;
+    }
     if (threadIdx.x == 0) a.cuts[ROUNDS * a.d.in.rows + row] = c;
 }
 
@@ -707,18 +740,16 @@ __global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a, int cut) {
     best = block_max<16>(best, maxima);
     const Scale scale(a.d.inv_t);
     const Weights weights(best, scale);
-    uint32_t t = 0, most = 0;
+    uint32_t most = 0;
     double each = 0.0;
     if (cut) {
-        const RowCut c = a.cuts[ROUNDS * a.d.in.rows + row];
-        t = c.t; most = c.ties;
-        if (t) {
-            each = weights.of(key_score(t));
-            if (!(each >= a.d.min_p)) each = 0.0;
-        }
+        const RowCut& c = a.cuts[ROUNDS * a.d.in.rows + row];
+        most = c.kept.ties;
+        if (most) each = weights.of(c.kept.t);
     } else if (threadIdx.x == 0) {
         RowCut c = {};
         c.best = best;
+        c.kept = {score_below(weights.floor), __uint_as_float(0x7FC00000u), 0u, 0u};
         a.cuts[ROUNDS * a.d.in.rows + row] = c;
     }
     double carry = 0.0;
@@ -729,7 +760,7 @@ __global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a, int cut) {
         uint32_t e = 0;
         if (g < a.groups) {
             v = bests[g] > -INFINITY ? sums[g] * weights.of(bests[g]) : 0.0;
-            if (t) e = ties[g];
+            if (most) e = ties[g];
         }
         const uint32_t es = wave_scan_u32(e, lane);  // equal scores up to this group
         if (lane == 63) tpart[wave] = es;
@@ -740,7 +771,7 @@ __global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a, int cut) {
             tcarry += tpart[w];
         }
         const uint32_t before = ebase + es - e;
-        if (t && before < most) v += each * (double)min(e, most - before);
+        if (before < most) v += each * (double)min(e, most - before);
         v = wave_scan64(v, lane);
         if (lane == 63) part[wave] = v;
         __syncthreads();
@@ -751,7 +782,7 @@ __global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a, int cut) {
         }
         if (g < a.groups) {
             sums[g] = base + v;
-            if (t) ties[g] = before;
+            if (most) ties[g] = before;
         }
         __syncthreads();
     }
@@ -767,7 +798,7 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
     const auto* s = static_cast<const typename Score<DT>::type*>(a.d.in.p) + row * a.d.in.ld;
     const RowCut& c = a.cuts[ROUNDS * a.d.in.rows + row];
     const float best = c.best;
-    const uint32_t t = c.t, most = c.ties;
+    const Kept kept = c.kept;
     const double* sums = a.group_sum + row * a.groups;
     const double total = sums[a.groups - 1];
     if (!(best > -INFINITY)) {
@@ -795,22 +826,20 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
     if (lane < GROUP_TILES) {
         const float own = a.tile_best[group * GROUP_TILES + lane];
         v = own > -INFINITY ? a.tile_sum[group * GROUP_TILES + lane] * weights.of(own) : 0.0;
-        if (t) e = a.tile_ties[group * GROUP_TILES + lane];
+        if (kept.ties) e = a.tile_ties[group * GROUP_TILES + lane];
     }
-    if (t) {
+    if (kept.ties) {
         before = a.group_ties[group] + wave_scan_u32(e, lane) - e;
-        const double each = weights.of(key_score(t));
-        if (before < most && each >= a.d.min_p) v += each * (double)min(e, most - before);
+        if (before < kept.ties) v += weights.of(kept.t) * (double)min(e, kept.ties - before);
     }
     const double incl = base + wave_scan64(v, lane);
     const uint64_t past = __ballot(incl > want && v > 0.0), any = __ballot(v > 0.0);
     const int tile = past ? __ffsll((unsigned long long)past) - 1 : any ? 63 - __clzll(any) : 0;
     base = lane64(incl - v, tile);
     before = __shfl((int)before, tile, 64);
-    const Kept kept = {t ? key_score(t) : -INFINITY, 0u, most};
     int64_t id = -1;
     double weight = 0.0;
-    draw_in_tile<DT, true>(s, lo * GROUP + (int64_t)tile * 256, a.d.in.n, kept, weights, a.d.min_p, before, base, want, lane, id, weight);
+    draw_in_tile<DT, true>(s, lo * GROUP + (int64_t)tile * 256, a.d.in.n, kept, weights, before, base, want, lane, id, weight);
     if (lane == 0) {
         a.d.ids[d] = id;
         if (a.d.logp) a.d.logp[d] = (float)log(weight / total);

@@ -124,6 +124,7 @@ template <int DT> struct Quad {
     }
 };
 
+constexpr uint32_t LOWEST_KEY = 0x00800000u;  // of the lowest finite number
 __device__ __forceinline__ uint32_t order_key(float s) {
     const uint32_t u = __float_as_uint(s + 0.f);  // -0 -> +0
     const uint32_t k = u >> 31 ? ~u : u | 0x80000000u;
@@ -159,10 +160,10 @@ struct Weights {
         floor = fmaxf(fminf(b, fmaf(fabsf(f), 0x1p-22f, f)), -3.402823466e38f);  // (rounded up; b = +inf: above every number)
         best = (double)fminf(b, 3.402823466e38f);
     }
-    __device__ __forceinline__ bool none(float s) const { return !(s >= floor); }
+    // (of a score at or above the floor; something else below it)
     __device__ __forceinline__ void split(float s, double& p, int& n) const {
-        const double x = ((double)__builtin_amdgcn_fmed3f(s, fminf(floor, 3.402823466e38f), 3.402823466e38f) - best) * scale.per;
-        const double shifted = x + 0x1.8p52, f = x - (shifted - 0x1.8p52);
+        const double d = (double)__builtin_amdgcn_fmed3f(s, -3.402823466e38f, 3.402823466e38f) - best, shifted = fma(d, scale.per, 0x1.8p52);
+        const double f = fma(d, scale.per, -(shifted - 0x1.8p52));
         n = __double2loint(shifted);
         p = scale.c[8];
 #pragma unroll
@@ -172,16 +173,37 @@ struct Weights {
     static __device__ __forceinline__ double scaled(double p, int n) {  // p * 2^n, p and the result normal numbers
         return __hiloint2double(__double2hiint(p) + (n << 20), __double2loint(p));
     }
-    // (masked by its bits: a choice between it and 0 would become a branch around every weight)
-    __device__ __forceinline__ double of(float s, bool keep = true) const {
+    // 0 where `keep`, which implies that s is at or above the floor, does not hold.  (Masked by its bits: a choice between the weight
+    // and 0 would become a branch around every weight.)
+    __device__ __forceinline__ double of(float s, bool keep) const {
         double p;
         int n;
         split(s, p, n);
-        const int mask = keep && !none(s) ? -1 : 0;
+        const int mask = keep ? -1 : 0;
         p = scaled(p, n);
         return __hiloint2double(__double2hiint(p) & mask, __double2loint(p) & mask);
     }
+    __device__ __forceinline__ double of(float s) const { return of(s, s >= floor); }
 };
+
+// The lowest key in lo .. hi for which `yes` holds, asked by a wave for 64 keys at a time; it holds for hi and for every key above one for
+// which it holds.
+template <typename F> __device__ __forceinline__ uint32_t lowest_key(uint32_t lo, uint32_t hi, const F& yes) {
+    while (lo < hi) {
+        const uint32_t step = (hi - lo) / 64 + 1;
+        const uint64_t at = (uint64_t)lo + (uint64_t)((threadIdx.x & 63) + 1) * step - 1;
+        const uint64_t who = __ballot(at >= hi || yes((uint32_t)at));
+        const uint32_t first = (uint32_t)__ffsll((unsigned long long)who) - 1;
+        hi = (uint32_t)min((uint64_t)hi, (uint64_t)lo + (uint64_t)(first + 1) * step - 1);
+        lo += first * step;
+    }
+    return lo;
+}
+// The next lower score (of 0 the negative number next to it, not -0): -inf below the lowest number.
+__device__ __forceinline__ float score_below(float s) {
+    const uint32_t k = order_key(s);
+    return k <= LOWEST_KEY ? -INFINITY : key_score(k - (k == 0x80000000u ? 2 : 1));
+}
 
 // Sums and maxima of a wave by moves within rows of 16 lanes and from row to row: no LDS on the way.
 template <int CTRL, int ROWS> __device__ __forceinline__ double moved64(double v) {  // lanes without a source: 0
@@ -330,7 +352,6 @@ template <int WAVES> __device__ __forceinline__ int block_count(int c, uint32_t*
 // Key of the largest score that at least m of the workgroup's scores reach, by halving the interval of keys: every round
 // counts the scores at or above its middle.  Ends early where exactly m do.  `reach`: how many reach the result.  Fewer than m
 // candidates: the lowest key.
-constexpr uint32_t LOWEST_KEY = 0x00800000u;  // of the lowest finite number
 template <int WAVES, int N>
 __device__ __forceinline__ uint32_t select_threshold(const float v[N], uint32_t best, int m, uint32_t* slots /* [2 * WAVES] */, int& reach) {
     uint32_t lo = LOWEST_KEY, hi = best;  // count(>= lo) >= m, count(> hi) < m
