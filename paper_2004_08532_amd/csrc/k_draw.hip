@@ -44,14 +44,12 @@ __device__ __forceinline__ void keep_from_min_p(Kept& k, const Weights& w, float
     k.over = fmaxf(k.over, score_below(least));
 }
 
-// Position in a tile (256 scores from `first` on) at which the sum passes `target`, `base` of it in front of the tile; the tile's
+// Position in a tile (256 scores from `first` on, read by the caller) at which the sum passes `target`, `base` of it in front of the tile; the tile's
 // last kept position where rounding leaves none.  COUNTED: equal scores are kept by `ties`, `ties_before` of them lie in front of the tile.
 template <int DT, bool COUNTED>
-__device__ __forceinline__ void draw_in_tile(const typename Score<DT>::type* s, int64_t first, int64_t n, const Kept& k, const Weights& weights, uint32_t ties_before,
+__device__ __forceinline__ void draw_in_tile(const Quad<DT>& x, int64_t first, int64_t n, const Kept& k, const Weights& weights, uint32_t ties_before,
                                              double base, double target, int lane, int64_t& id, double& weight) {
     float v[4];
-    Quad<DT> x;
-    x.load(s, first + lane * 4, n);
     x.values(first, n, v);
     double w[4], sum = 0.0;
     uint32_t rank = ties_before;
@@ -157,24 +155,40 @@ __device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, 
     }
     __syncthreads();
     const double total = sums[tiles - 1];
-    for (int d = wave; d < a.draws; d += WAVES) {
-        const double want = unit_number(a.u[row * a.draws + d]) * total;
-        int tile = -1, fallback = 0;
+    double x[TILES / 64 + 1];
+    int last = 0;  // tile with a weight
 #pragma unroll
-        for (int t0 = 0; t0 < TILES; t0 += 64) {
-            const bool there = t0 + lane < tiles;
-            const double x = there ? sums[t0 + lane] : 0.0, before = t0 + lane > 0 && there ? sums[t0 + lane - 1] : 0.0;
-            const uint64_t past = __ballot(there && x > want), some = __ballot(there && x > before);
-            if (tile < 0 && past) tile = t0 + __ffsll((unsigned long long)past) - 1;
-            if (some) fallback = t0 + 63 - __clzll(some);
+    for (int k = 0; k * 64 < TILES; ++k) {
+        const int t = k * 64 + lane;
+        x[k] = t < tiles ? sums[t] : INFINITY;
+        const uint64_t some = __ballot(t < tiles && x[k] > (t > 0 ? sums[t - 1] : 0.0));
+        if (some) last = k * 64 + 63 - __clzll(some);
+    }
+    constexpr int AT_ONCE = 4;  // draws of a wave whose tiles are read together
+    for (int d0 = wave * AT_ONCE; d0 < a.draws; d0 += WAVES * AT_ONCE) {
+        const int n = min(AT_ONCE, a.draws - d0);
+        const double own = lane < n ? unit_number(a.u[row * a.draws + d0 + lane]) * total : 0.0;
+        Quad<DT> quad[AT_ONCE];
+        int tile[AT_ONCE];
+#pragma unroll
+        for (int d = 0; d < AT_ONCE; ++d) {
+            const double want = lane64(own, d);
+            int at = 0;
+#pragma unroll
+            for (int k = 0; k * 64 < TILES; ++k) at += __popcll(__ballot(x[k] <= want));  // (running sums: the tiles in front)
+            tile[d] = min(at, last);
+            quad[d].load(s, (int64_t)tile[d] * 256 + lane * 4, a.in.n);
         }
-        if (tile < 0) tile = fallback;
-        int64_t id = -1;
-        double weight = 0.0;
-        draw_in_tile<DT, false>(s, (int64_t)tile * 256, a.in.n, kept, weights, 0u, tile > 0 ? sums[tile - 1] : 0.0, want, lane, id, weight);
-        if (lane == 0) {
-            a.ids[row * a.draws + d] = id;
-            if (a.logp) a.logp[row * a.draws + d] = (float)log(weight / total);
+#pragma unroll
+        for (int d = 0; d < AT_ONCE; ++d) {
+            if (d >= n) break;
+            int64_t id = -1;
+            double weight = 0.0;
+            draw_in_tile<DT, false>(quad[d], (int64_t)tile[d] * 256, a.in.n, kept, weights, 0u, tile[d] > 0 ? sums[tile[d] - 1] : 0.0, lane64(own, d), lane, id, weight);
+            if (lane == 0) {
+                a.ids[row * a.draws + d0 + d] = id;
+                if (a.logp) a.logp[row * a.draws + d0 + d] = (float)log(weight / total);
+            }
         }
     }
 }
@@ -202,8 +216,9 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_whole(DrawArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i].values((int64_t)(t0 + i) * 256, a.in.n, v + 4 * i);
         if (t0 + 4 * WAVES < tiles) load(t0 + 4 * WAVES);  // (arrives while these are worked on)
-        const float best = best_of_tiles(v);
-        const double z = sum_of_tiles(v, best, scale);
+        const float best = best_of(v);
+        const Weights w(best, scale);
+        const double z = sum_of_tiles(v, w, score_below(w.floor));
         const int tile = t0 + tile_of_row(lane >> 4);
         if ((lane & 15) == 15 && tile < tiles) { sums[tile] = z; bests[tile] = best; most = fmaxf(most, best); }
     }
@@ -453,25 +468,27 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
         }
         keep_from_min_p(kept, weights, best, a.min_p);
         const bool some = CUT == CUT_WEIGHT && kept.least > 0;  // of the equal ones some are not kept
-        double four[4];
+        if constexpr (TPW % 4 == 0) {
 #pragma unroll
-        for (int i = 0; i < TPW; ++i) {
+            for (int i = 0; i < TPW; i += 4) {
+                const double z = sum_of_tiles(v + 4 * i, weights, kept.over);
+                if ((lane & 15) == 15) sums[(i + tile_of_row(lane >> 4)) * WAVES + wave] = z;
+            }
+        } else {
             double z = 0.0;
 #pragma unroll
-            for (int q = 4 * i; q < 4 * i + 4; ++q) z += weights.of(v[q], v[q] > kept.over);
-            if (some) {
+            for (int q = 0; q < 4; ++q) z += weights.of(v[q], v[q] > kept.over);
+            z = wave_sum64(z);
+            if (lane == 0) sums[wave] = z;
+        }
+        if (some) {
+            const double each = weights.of(kept.t);
 #pragma unroll
-                for (int q = 4 * i; q < 4 * i + 4; ++q) if (v[q] == kept.t && low(q) >= kept.least) z += weights.of(v[q]);
-            }
-            if constexpr (TPW % 4 == 0) {
-                four[i % 4] = z;
-                if (i % 4 == 3) {
-                    z = sum_four(four);
-                    if ((lane & 15) == 15) sums[(i - 3 + tile_of_row(lane >> 4)) * WAVES + wave] = z;
-                }
-            } else {
-                z = wave_sum64(z);
-                if (lane == 0) sums[i * WAVES + wave] = z;
+            for (int i = 0; i < TPW; ++i) {
+                int c = 0;
+#pragma unroll
+                for (int q = 4 * i; q < 4 * i + 4; ++q) c += __popcll(__ballot(v[q] == kept.t && low(q) >= kept.least));
+                if (lane == 0) sums[i * WAVES + wave] += (double)c * each;
             }
         }
         draw_from_tiles<DT, WAVES, TILES>(a, row, s, TILES, sums, nullptr, kept, weights);
@@ -663,14 +680,7 @@ __global__ __launch_bounds__(256) void k_draw_sums(LongArgs a, int64_t per) {
         if (++group == a.groups) { group = 0; ++row; }
         if (block + 1 < end) load(row, group);
         const int half = (int)(block - start) & 1;
-        const Weights w(best, scale);
-        double z[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            z[i] = 0.0;
-#pragma unroll
-            for (int q = 4 * i; q < 4 * i + 4; ++q) z[i] += w.of(v[q], v[q] > kept.over);
-        }
+        const double sum = sum_of_tiles(v, Weights(best, scale), kept.over);
         if (kept.ties) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -680,7 +690,6 @@ __global__ __launch_bounds__(256) void k_draw_sums(LongArgs a, int64_t per) {
                 if (lane == 0) ties[half][wave * 4 + i] = e;
             }
         }
-        const double sum = sum_four(z);
         if ((lane & 15) == 15) sums[half][wave * 4 + tile_of_row(lane >> 4)] = sum;
         __syncthreads();
         if (wave != (int)(block & 3)) continue;
@@ -839,7 +848,9 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
     before = __shfl((int)before, tile, 64);
     int64_t id = -1;
     double weight = 0.0;
-    draw_in_tile<DT, true>(s, lo * GROUP + (int64_t)tile * 256, a.d.in.n, kept, weights, before, base, want, lane, id, weight);
+    Quad<DT> x;
+    x.load(s, lo * GROUP + (int64_t)tile * 256 + lane * 4, a.d.in.n);
+    draw_in_tile<DT, true>(x, lo * GROUP + (int64_t)tile * 256, a.d.in.n, kept, weights, before, base, want, lane, id, weight);
     if (lane == 0) {
         a.d.ids[d] = id;
         if (a.d.logp) a.d.logp[d] = (float)log(weight / total);

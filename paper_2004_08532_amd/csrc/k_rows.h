@@ -30,8 +30,8 @@ struct TileArgs {
     RowScores in;
     double inv_t;
     int64_t groups;       // of a row
-    float* tile_best;     // [rows][groups][GROUP_TILES], may be null
-    double* tile_sum;     // the same, relative to the tile's best; may be null
+    float* tile_best;     // [rows][groups][GROUP_TILES] what the tile's sum is relative to, may be null
+    double* tile_sum;     // may be null
     float* group_best;    // [rows][groups]
     double* group_sum;    // relative to the group's best
     float* group_worst;   // lowest score that is not masked, +inf without one; may be null (only without sums)
@@ -184,6 +184,17 @@ struct Weights {
         return __hiloint2double(__double2hiint(p) & mask, __double2loint(p) & mask);
     }
     __device__ __forceinline__ double of(float s) const { return of(s, s >= floor); }
+    // For sums of many, of scores of a row whose best is finite: less than 2^-1040 instead of 0 (see some_weight).
+    __device__ __forceinline__ double loose(float s, bool keep) const {
+        const double d = (double)s - best, shifted = fma(d, scale.per, 0x1.8p52), f = fma(d, scale.per, -(shifted - 0x1.8p52));
+        double p = scale.c[8];
+#pragma unroll
+        for (int i = 7; i >= 0; --i) p = fma(p, f, scale.c[i]);
+        p = scaled(fma(p, f, 1.0), __double2loint(shifted));
+        return __hiloint2double(keep ? __double2hiint(p) : 0, __double2loint(p));
+    }
+    // The sum of up to 2^10 loose weights, 0 where none of them is one.
+    static __device__ __forceinline__ double some_weight(double z) { return z < 0x1p-1025 ? 0.0 : z; }
 };
 
 // The lowest key in lo .. hi for which `yes` holds, asked by a wave for 64 keys at a time; it holds for hi and for every key above one for
@@ -227,7 +238,6 @@ __device__ __forceinline__ double lane64(double v, int lane) {  // of one lane, 
 __device__ __forceinline__ double wave_sum64(double v) { return lane64(wave_scan64(v, 0), 63); }
 // Of four tiles at once: the halves of two tiles' values are joined in one register, then the quarters of four, so that the steps within a row of 16
 // lanes serve all.  Lane 15 of row k ends with the tile k = 0, 2, 1, 3.
-__device__ __forceinline__ int row_of_tile(int i) { return i == 1 ? 2 : i == 2 ? 1 : i; }
 __device__ __forceinline__ void swap32(int& a, int& b) {
     const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
     a = r[0]; b = r[1];
@@ -250,24 +260,9 @@ __device__ __forceinline__ double sum_four(const double z[4]) {
     v += moved64<ROW_SHR + 8, 0xf>(v);
     return v;
 }
-template <bool HALVES> __device__ __forceinline__ float join_max(float a, float b) {
-    int x = __float_as_int(a), y = __float_as_int(b);
-    if (HALVES) swap32(x, y);
-    else swap16(x, y);
-    return fmaxf(__int_as_float(x), __int_as_float(y));
-}
-
 template <int CTRL, int ROWS> __device__ __forceinline__ float max_moved(float v) {
     return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(-INFINITY), __float_as_int(v), CTRL, ROWS, 0xf, false)));
 }
-__device__ __forceinline__ float max_four(const float z[4]) {
-    float v = join_max<false>(join_max<true>(z[0], z[1]), join_max<true>(z[2], z[3]));
-    v = max_moved<ROW_SHR + 1, 0xf>(v);
-    v = max_moved<ROW_SHR + 2, 0xf>(v);
-    v = max_moved<ROW_SHR + 4, 0xf>(v);
-    return max_moved<ROW_SHR + 8, 0xf>(v);
-}
-__device__ __forceinline__ float of_tile(float v, int i) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), row_of_tile(i) * 16 + 15)); }
 __device__ __forceinline__ float wave_most(float v) {
     v = max_moved<ROW_SHR + 1, 0xf>(v);
     v = max_moved<ROW_SHR + 2, 0xf>(v);
@@ -317,21 +312,30 @@ __device__ __forceinline__ float load_tiles(const typename Score<DT>::type* row,
     return best;
 }
 
-// Best scores and sums of weights of four tiles that a wave holds.  The sums (and bests) are in lane 15 of the rows, see sum_four.
-__device__ __forceinline__ float best_of_tiles(const float v[16]) {
-    float m[4];
+// Sums of the weights of four tiles that a wave holds, relative to the best score among them; of scores above `over`.  The sums are in lane 15 of
+// the rows, see sum_four.
+__device__ __forceinline__ float best_of(const float v[16]) {
+    float m = v[0];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m[i] = fmaxf(fmaxf(v[4 * i], v[4 * i + 1]), fmaxf(v[4 * i + 2], v[4 * i + 3]));
-    return max_four(m);
+    for (int q = 1; q < 16; ++q) m = fmaxf(m, v[q]);
+    return wave_most(m);
 }
-__device__ __forceinline__ double sum_of_tiles(const float v[16], float bests, const Scale& scale) {
+__device__ __forceinline__ double sum_of_tiles(const float v[16], const Weights& w, float over) {
     double z[4];
+    if (w.floor == INFINITY) {  // (the best is +inf: the same for the wave)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const Weights w(of_tile(bests, i), scale);
-        z[i] = (w.of(v[4 * i]) + w.of(v[4 * i + 1])) + (w.of(v[4 * i + 2]) + w.of(v[4 * i + 3]));
+        for (int i = 0; i < 4; ++i) {
+            z[i] = 0.0;
+#pragma unroll
+            for (int q = 4 * i; q < 4 * i + 4; ++q) z[i] += v[q] == INFINITY && v[q] > over ? 1.0 : 0.0;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            z[i] = (w.loose(v[4 * i], v[4 * i] > over) + w.loose(v[4 * i + 1], v[4 * i + 1] > over)) +
+                   (w.loose(v[4 * i + 2], v[4 * i + 2] > over) + w.loose(v[4 * i + 3], v[4 * i + 3] > over));
     }
-    return sum_four(z);
+    return Weights::some_weight(sum_four(z));
 }
 __device__ __forceinline__ int tile_of_row(int row) { return row == 1 ? 2 : row == 2 ? 1 : row; }
 

@@ -1,8 +1,8 @@
-// Best score and sum of weights of every tile (256 scores) and group (16 tiles) of long rows: the one pass over the scores that
+// Sum of weights of every tile (256 scores), best score and sum of every group (16 tiles) of long rows: the one pass over the scores that
 // kge_top_scores and kge_sample_scores make where nothing is cut, and the first one where something is.
 //
-// Weights are relative to the best score of their own tile, so that waves work for themselves: no score has to be known before the
-// others are read.  Every workgroup goes through a range of groups and has the next one's scores on their way while it works on one's: reads and
+// Weights are relative to the best score of the four tiles that a wave has at a time, so that waves work for themselves: no score has to be known
+// before the others are read.  Every workgroup goes through a range of groups and has the next one's scores on their way while it works on one's: reads and
 // arithmetic take about the same time (20 M fp32 scores: 16 us each).
 #include "k_rows.h"
 
@@ -32,10 +32,11 @@ __global__ __launch_bounds__(256) void k_tiles(TileArgs a) {
         if (++group == a.groups) { group = 0; ++row; }
         if (block + 1 < end) load(row, group);  // the next one's scores arrive while these are worked on
         const int half = (int)(block - start) & 1;
-        const float best = best_of_tiles(v);
+        const float best = best_of(v);  // of the wave's four tiles
         const int tile = wave * 4 + tile_of_row(lane >> 4);
         if constexpr (SUMS) {
-            const double z = sum_of_tiles(v, best, scale);
+            const Weights w(best, scale);
+            const double z = sum_of_tiles(v, w, score_below(w.floor));
             if ((lane & 15) == 15) sums[half][tile] = z;
         } else {
             float worst = INFINITY;
