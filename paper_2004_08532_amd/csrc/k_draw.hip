@@ -6,27 +6,9 @@
 //
 // Sums are kept per tile of 256 scores; a draw is a wave that finds its tile among the sums and its position in the tile.  All sums are
 // formed in 64 bits, in a fixed order or as whole numbers, so a draw depends on the row and its number alone.
-#include "k_rows.h"
+#include "k_draw_list.h"
 
 namespace {
-
-struct DrawArgs {
-    RowScores in;
-    const double* u;  // [rows][draws]
-    int draws, top_k;
-    double inv_t, top_p, min_p;
-    int64_t* ids;
-    float* logp;
-};
-
-__device__ __forceinline__ double unit_number(double u) { return u > 0.0 ? u : 0.0; }  // (NaN: 0)
-
-template <int THREADS> __device__ __forceinline__ void write_empty(const DrawArgs& a, int64_t row) {
-    for (int d = threadIdx.x; d < a.draws; d += THREADS) {
-        a.ids[row * a.draws + d] = -1;
-        if (a.logp) a.logp[row * a.draws + d] = -INFINITY;
-    }
-}
 
 // What is kept: the scores above `over`, and of those equal to t the ones whose inverted position is at least `least` (in rows held by a
 // workgroup) or the first `ties` of the row (in long ones).  t is not above `over`; NaN: none of them.
@@ -83,56 +65,6 @@ __device__ __forceinline__ void draw_in_tile(const Quad<DT>& x, int64_t first, i
     }
     id = __shfl((long long)id, who, 64);
     weight = __shfl(weight, who, 64);
-}
-
-// The draws from a sorted list of the row's best candidates.  list: LDS, KGE_TOP_MAX entries, the first `count` of them
-// filled; sums: LDS, as many.
-template <int THREADS>
-__device__ __forceinline__ void draw_from_list(const DrawArgs& a, int64_t row, uint64_t* list, int count, double* sums, int* kept) {
-    if (count == 0) { write_empty<THREADS>(a, row); return; }
-    const int lane = threadIdx.x & 63;
-    const Scale scale(a.inv_t);
-    const Weights weights(key_score((uint32_t)(list[0] >> 32)), scale);
-    auto scan = [&](int n) {  // sums of weights -> running sums, by the first wave
-        __syncthreads();
-        if (threadIdx.x < 64) {
-            double carry = 0.0;
-            for (int e0 = 0; e0 < n; e0 += 64) {
-                const double v = carry + wave_scan64(e0 + lane < n ? sums[e0 + lane] : 0.0, lane);
-                if (e0 + lane < n) sums[e0 + lane] = v;
-                carry = __shfl(v, 63, 64);
-            }
-        }
-        __syncthreads();
-    };
-    for (int e = threadIdx.x; e < count; e += THREADS) sums[e] = weights.of(key_score((uint32_t)(list[e] >> 32)));
-    if (threadIdx.x == 0) *kept = 0;
-    scan(count);
-    const double target = a.top_p < 1.0 ? a.top_p * sums[count - 1] : INFINITY;
-    for (int e = threadIdx.x; e < count; e += THREADS) {
-        const bool in = e == 0 || (sums[e - 1] < target && weights.of(key_score((uint32_t)(list[e] >> 32))) >= a.min_p);
-        if (in) atomicMax(kept, e + 1);
-    }
-    __syncthreads();
-    count = *kept;
-    const int size = power_of_two(count);
-    // into the order of positions; the key goes below the inverted position
-    for (int e = threadIdx.x; e < size; e += THREADS) list[e] = e < count ? list[e] << 32 | list[e] >> 32 : 0;
-    sort_descending<THREADS>(list, size);
-    for (int e = threadIdx.x; e < count; e += THREADS) sums[e] = weights.of(key_score((uint32_t)list[e]));
-    scan(count);
-    const double total = sums[count - 1];
-    for (int d = threadIdx.x; d < a.draws; d += THREADS) {
-        const double want = unit_number(a.u[row * a.draws + d]) * total;
-        int lo = 0, hi = count - 1;  // first entry whose running sum exceeds `want`, the last one where none does
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (sums[mid] > want) hi = mid; else lo = mid + 1;
-        }
-        while (lo > 0 && !(sums[lo] > sums[lo - 1])) --lo;  // (an entry without weight is never drawn)
-        a.ids[row * a.draws + d] = (int64_t)(uint32_t)~(uint32_t)(list[lo] >> 32);
-        if (a.logp) a.logp[row * a.draws + d] = (float)log(weights.of(key_score((uint32_t)list[lo])) / total);
-    }
 }
 
 // The draws of a row whose tile sums a workgroup has in LDS.  sums[t]: of tile t, relative to best[t] (a row's best where that is null).
@@ -402,8 +334,10 @@ __device__ __forceinline__ Kept cut_by_weight(float v[TPW * 4], const L& low, fl
     if (threadIdx.x == 0) s.count = 0;
     __syncthreads();
     const float t0 = key_score(r.lo), t1 = key_score(r.hi);
+    uint32_t marked = 0;
 #pragma unroll
-    for (int q = 0; q < N; ++q) append_entry(v[q] >= t0 && v[q] <= t1, (uint64_t)order_key(v[q]) << 32 | low(q), s.bins, &s.count);
+    for (int q = 0; q < N; ++q) marked |= (uint32_t)(v[q] >= t0 && v[q] <= t1) << q;
+    append_marked<N>(v, marked, low, s.bins, ROOM, &s.count);
     __syncthreads();
     const uint64_t* list = order_list<THREADS>(s.bins, s.sorted, s.rank, count);
     for (int e = threadIdx.x; e < count; e += THREADS) s.sums[e] = w.of(key_score((uint32_t)(list[e] >> 32)));
@@ -451,7 +385,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
         __shared__ int kept_entries;
         const int count = collect_best<WAVES, TPW>(v, low, mine, order_key(best), a.top_k, b);
         uint64_t* list = order_list<THREADS>(b.list, b.sorted, b.rank, count);
-        draw_from_list<THREADS>(a, row, list, min(count, a.top_k), sums, &kept_entries);
+        draw_from_list<THREADS>(a, row, list, list == b.sorted ? b.list : b.sorted, b.rank, min(count, a.top_k), sums, &kept_entries);
     } else {
         __shared__ double sums[TILES];
         const Scale scale(a.inv_t);
@@ -497,9 +431,9 @@ __global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
 
 // top-k of long rows: the draws from the lists that k_top leaves
 __global__ __launch_bounds__(256) void k_draw_lists(DrawArgs a, const uint64_t* lists) {
-    __shared__ uint64_t list[KGE_TOP_MAX];
+    __shared__ uint64_t list[KGE_TOP_MAX], spare[256];
     __shared__ double sums[KGE_TOP_MAX];
-    __shared__ uint32_t filled;
+    __shared__ uint32_t filled, rank[256];
     __shared__ int kept_entries;
     const int64_t row = flat_block();
     if (row >= a.in.rows) return;
@@ -512,7 +446,7 @@ __global__ __launch_bounds__(256) void k_draw_lists(DrawArgs a, const uint64_t* 
         if (x) atomicMax(&filled, (uint32_t)(e + 1));
     }
     __syncthreads();
-    draw_from_list<256>(a, row, list, (int)filled, sums, &kept_entries);
+    draw_from_list<256>(a, row, list, spare, rank, (int)filled, sums, &kept_entries);
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -724,15 +658,6 @@ __global__ __launch_bounds__(256) void k_draw_cut(LongArgs a) {
     if (threadIdx.x == 0) a.cuts[ROUNDS * a.d.in.rows + row] = c;
 }
 
-__device__ __forceinline__ uint32_t wave_scan_u32(uint32_t v, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t y = __shfl_up((int)v, o, 64);
-        if (lane >= o) v += y;
-    }
-    return v;
-}
-
 // Running sums over the groups of a row.
 __global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a, int cut) {
     __shared__ double part[16];
@@ -771,7 +696,7 @@ __global__ __launch_bounds__(1024) void k_draw_scan(LongArgs a, int cut) {
             v = bests[g] > -INFINITY ? sums[g] * weights.of(bests[g]) : 0.0;
             if (most) e = ties[g];
         }
-        const uint32_t es = wave_scan_u32(e, lane);  // equal scores up to this group
+        const uint32_t es = wave_scan_u32(e);  // equal scores up to this group
         if (lane == 63) tpart[wave] = es;
         __syncthreads();
         uint32_t ebase = tcarry;
@@ -838,7 +763,7 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
         if (kept.ties) e = a.tile_ties[group * GROUP_TILES + lane];
     }
     if (kept.ties) {
-        before = a.group_ties[group] + wave_scan_u32(e, lane) - e;
+        before = a.group_ties[group] + wave_scan_u32(e) - e;
         if (before < kept.ties) v += weights.of(kept.t) * (double)min(e, kept.ties - before);
     }
     const double incl = base + wave_scan64(v, lane);
@@ -934,7 +859,7 @@ void launch(const DrawArgs& d, void* workspace, hipStream_t st) {
     if (cut) t.group_worst = a.group_worst;
     else { t.tile_best = a.tile_best; t.tile_sum = a.tile_sum; t.group_sum = a.group_sum; }
     if (by_weight) { t.clear = a.bins; t.clear_words = ROUNDS * BINS; }
-    kge_launch_tiles(t, !cut, st);
+    kge_launch_tiles(t, cut ? TILES_RANGE : TILES_SUMS, st);
     const dim3 rows = flat_grid(d.in.rows);
     if (by_weight) {
         for (int round = 0; round < ROUNDS; ++round) k_draw_bins<DT><<<flat_grid(d.in.rows * a.parts), 256, 0, st>>>(a, round);
@@ -965,8 +890,9 @@ void kge_launch_draw(const RowScores& in, const double* u, int draws, float temp
     if (top_k > 0 && in.n > KGE_ROW_RESIDENT) {
         char* ws = static_cast<char*>(workspace);
         uint64_t* lists = reinterpret_cast<uint64_t*>(ws);
-        kge_launch_top(in, top_k, 1.f, nullptr, nullptr, lists, nullptr, ws + up256(in.rows * (int64_t)top_k * 8), st);
-        k_draw_lists<<<flat_grid(in.rows), 256, 0, st>>>(a, lists);
+        const bool by_tiles = kge_top_by_tiles(in.n, top_k);
+        kge_launch_top(in, top_k, 1.f, nullptr, nullptr, lists, nullptr, by_tiles ? &a : nullptr, ws + up256(in.rows * (int64_t)top_k * 8), st);
+        if (!by_tiles) k_draw_lists<<<flat_grid(in.rows), 256, 0, st>>>(a, lists);
         return;
     }
     if (in.dtype == KGE_F32) launch<KGE_F32>(a, workspace, st);

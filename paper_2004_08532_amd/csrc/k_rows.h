@@ -26,27 +26,36 @@ inline int64_t pieces(int64_t n, int64_t of) { return (n + of - 1) / of; }
 inline int64_t up256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
 constexpr int GROUP_TILES = 16, GROUP = GROUP_TILES * 256;  // scores of long rows that a workgroup of k_tiles takes
+enum TileMode {
+    TILES_SUMS,       // sums of tiles and groups
+    TILES_RANGE,      // best and lowest score of groups
+    TILES_BEST,       // best score of every tile
+    TILES_BEST_SUMS,  // the same, and sums of groups
+};
 struct TileArgs {
     RowScores in;
     double inv_t;
     int64_t groups;       // of a row
-    float* tile_best;     // [rows][groups][GROUP_TILES] what the tile's sum is relative to, may be null
-    double* tile_sum;     // may be null
-    float* group_best;    // [rows][groups]
+    float* tile_best;     // [rows][groups][GROUP_TILES]; TILES_SUMS: what the tile's sum is relative to
+    double* tile_sum;
+    float* group_best;    // [rows][groups]; not TILES_BEST
     double* group_sum;    // relative to the group's best
-    float* group_worst;   // lowest score that is not masked, +inf without one; may be null (only without sums)
+    float* group_worst;   // of the scores that are not masked, +inf without one
     uint64_t* clear;      // [rows][clear_words] that the pass sets to 0, may be null
     int64_t clear_words;
     int64_t per;          // groups of a workgroup (set by the launcher)
 };
 // Groups in a row for each of the workgroups of 256 threads that fill the chip, 8 per CU.
 inline int64_t groups_per_workgroup(int64_t groups) { return pieces(groups, 2048); }
-void kge_launch_tiles(TileArgs a, bool sums, hipStream_t st);
+void kge_launch_tiles(TileArgs a, TileMode mode, hipStream_t st);
 
 int64_t kge_top_workspace(int64_t rows, int64_t n, int m);
-// (ids and scores, or the sorted entries alone; lse may be null)
+// Long rows whose lists are found among the tiles' best scores, and not segment by segment
+bool kge_top_by_tiles(int64_t n, int m);
+struct DrawArgs;  // (k_draw_list.h)
+// (ids and scores, or with by_tiles the draws of `draw`, or else the sorted entries alone; lse may be null)
 void kge_launch_top(const RowScores& in, int m, float temperature, int64_t* ids, float* scores, uint64_t* entries, float* lse,
-                    void* workspace, hipStream_t st);
+                    const DrawArgs* draw, void* workspace, hipStream_t st);
 int64_t kge_draw_workspace(int64_t rows, int64_t n, int top_k, float top_p);
 void kge_launch_draw(const RowScores& in, const double* u, int draws, float temperature, int top_k, float top_p, float min_p, int64_t* ids,
                      float* logp, void* workspace, hipStream_t st);
@@ -232,6 +241,16 @@ __device__ __forceinline__ double wave_scan64(double v, int) {  // sum over lane
     v += moved64<BCAST_31, 0xc>(v);
     return v;
 }
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved32(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ uint32_t wave_scan_u32(uint32_t v) {
+    v += moved32<ROW_SHR + 1, 0xf>(v);
+    v += moved32<ROW_SHR + 2, 0xf>(v);
+    v += moved32<ROW_SHR + 4, 0xf>(v);
+    v += moved32<ROW_SHR + 8, 0xf>(v);
+    v += moved32<BCAST_15, 0xa>(v);
+    v += moved32<BCAST_31, 0xc>(v);
+    return v;
+}
 __device__ __forceinline__ double lane64(double v, int lane) {  // of one lane, the same for all
     return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
 }
@@ -262,6 +281,18 @@ __device__ __forceinline__ double sum_four(const double z[4]) {
 }
 template <int CTRL, int ROWS> __device__ __forceinline__ float max_moved(float v) {
     return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(-INFINITY), __float_as_int(v), CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ float max_four(const float z[4]) {  // (in the lanes of sum_four)
+    auto join = [](float a, float b, auto swap) {
+        int x = __float_as_int(a), y = __float_as_int(b);
+        swap(x, y);
+        return fmaxf(__int_as_float(x), __int_as_float(y));
+    };
+    float v = join(join(z[0], z[1], swap32), join(z[2], z[3], swap32), swap16);
+    v = max_moved<ROW_SHR + 1, 0xf>(v);
+    v = max_moved<ROW_SHR + 2, 0xf>(v);
+    v = max_moved<ROW_SHR + 4, 0xf>(v);
+    return max_moved<ROW_SHR + 8, 0xf>(v);
 }
 __device__ __forceinline__ float wave_most(float v) {
     v = max_moved<ROW_SHR + 1, 0xf>(v);
@@ -400,15 +431,22 @@ __device__ __forceinline__ uint32_t select_equal(const float v[N], float t, cons
     return lo;
 }
 
-// Appends the entries that `take` says to a list in LDS (in any order); *n starts at 0 and ends at their number.
-__device__ __forceinline__ void append_entry(bool take, uint64_t entry, uint64_t* list, uint32_t* n) {
-    const int lane = threadIdx.x & 63;
-    const uint64_t who = __ballot(take);
-    if (!who) return;
-    uint32_t base = 0;
-    if (lane == 0) base = atomicAdd(n, (uint32_t)__popcll(who));
-    base = __shfl((int)base, 0, 64);
-    if (take) list[base + __popcll(who & (((uint64_t)1 << lane) - 1))] = entry;
+// Appends a thread's scores whose bit is set, as entries, to a list in LDS (in any order) that has room for `room`; *n starts at 0 and ends at the
+// number of those that there are.
+template <int N, typename L>
+__device__ __forceinline__ void append_marked(const float v[N], uint32_t marked, const L& low, uint64_t* list, uint32_t room, uint32_t* n) {
+    if (!__ballot(marked != 0)) return;
+    const uint32_t own = (uint32_t)__popc(marked), upto = wave_scan_u32(own);
+    uint32_t at = 0;
+    if ((threadIdx.x & 63) == 63) at = atomicAdd(n, upto);
+    at = (uint32_t)__builtin_amdgcn_readlane((int)at, 63) + upto - own;
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        if (marked >> q & 1) {
+            if (at < room) list[at] = (uint64_t)order_key(v[q]) << 32 | low(q);
+            ++at;
+        }
+    }
 }
 
 // Sorts the first `size` (a power of two) entries of a list in LDS, the largest first.
@@ -522,13 +560,16 @@ __device__ __forceinline__ int collect_best(const float v[TPW * 4], const L& low
     }
     __syncthreads();
     float t = key_score(bound);
-    uint32_t least = 0;  // of the inverted positions of scores that equal t
-    if constexpr (CAP > ROOM) {
-        int c = 0;
+    uint32_t marked = 0;
 #pragma unroll
-        for (int q = 0; q < N; ++q) c += __popcll(__ballot(v[q] >= t));
-        if (block_count<WAVES>(c, s.slots) > ROOM) {
+    for (int q = 0; q < N; ++q) marked |= (uint32_t)(v[q] >= t) << q;
+    append_marked<N>(v, marked, low, s.list, ROOM, &s.count);
+    __syncthreads();
+    if constexpr (CAP > ROOM) {
+        if (s.count > ROOM) {  // (the same for all) too many: exactly those that count
+            uint32_t least = 0;  // of the inverted positions of scores that equal t
             __syncthreads();
+            if (threadIdx.x == 0) s.count = 0;
             int reach;
             t = key_score(select_threshold<WAVES, N>(v, best, m, s.slots, reach));
             if (reach > m) {  // more than m reach it: equal scores, of which the first ones count
@@ -539,14 +580,14 @@ __device__ __forceinline__ int collect_best(const float v[TPW * 4], const L& low
                 above = block_count<WAVES>(above, s.slots);
                 least = select_equal<WAVES, N>(v, t, low, m - above, s.slots);
             }
+            __syncthreads();
+            marked = 0;
+#pragma unroll
+            for (int q = 0; q < N; ++q) marked |= (uint32_t)(v[q] > t || (v[q] == t && low(q) >= least)) << q;
+            append_marked<N>(v, marked, low, s.list, ROOM, &s.count);
+            __syncthreads();
         }
     }
-#pragma unroll
-    for (int q = 0; q < N; ++q) {
-        const uint32_t at = low(q);
-        append_entry(v[q] > t || (v[q] == t && at >= least), (uint64_t)order_key(v[q]) << 32 | at, s.list, &s.count);
-    }
-    __syncthreads();
     return (int)s.count;
 }
 

@@ -8,9 +8,10 @@
 
 namespace {
 
-template <int DT, bool SUMS>
+template <int DT, int MODE>
 __global__ __launch_bounds__(256) void k_tiles(TileArgs a) {
-    __shared__ float bests[2][GROUP_TILES], worsts[2][4];
+    constexpr bool SUMS = MODE == TILES_SUMS || MODE == TILES_BEST_SUMS, EACH = MODE == TILES_BEST || MODE == TILES_BEST_SUMS;
+    __shared__ float bests[2][GROUP_TILES], worsts[2][4], tops[2][4];
     __shared__ double sums[2][GROUP_TILES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t blocks = a.in.rows * a.groups, start = (int64_t)flat_block() * a.per, end = min(start + a.per, blocks);
@@ -32,50 +33,65 @@ __global__ __launch_bounds__(256) void k_tiles(TileArgs a) {
         if (++group == a.groups) { group = 0; ++row; }
         if (block + 1 < end) load(row, group);  // the next one's scores arrive while these are worked on
         const int half = (int)(block - start) & 1;
-        const float best = best_of(v);  // of the wave's four tiles
         const int tile = wave * 4 + tile_of_row(lane >> 4);
-        if constexpr (SUMS) {
-            const Weights w(best, scale);
-            const double z = sum_of_tiles(v, w, score_below(w.floor));
-            if ((lane & 15) == 15) sums[half][tile] = z;
-        } else {
-            float worst = INFINITY;
+        if constexpr (EACH) {
+            float m[4];
 #pragma unroll
-            for (int q = 0; q < 16; ++q) worst = v[q] > -INFINITY ? fminf(worst, v[q]) : worst;
-            worst = -wave_most(-worst);
-            if (lane == 0) worsts[half][wave] = worst;
+            for (int i = 0; i < 4; ++i) m[i] = fmaxf(fmaxf(v[4 * i], v[4 * i + 1]), fmaxf(v[4 * i + 2], v[4 * i + 3]));
+            const float most = max_four(m);
+            if ((lane & 15) == 15) bests[half][tile] = most;
         }
-        if ((lane & 15) == 15) bests[half][tile] = best;
+        if constexpr (MODE != TILES_BEST) {
+            const float best = best_of(v);  // of the wave's four tiles
+            if constexpr (SUMS) {
+                const Weights w(best, scale);
+                const double z = sum_of_tiles(v, w, score_below(w.floor));
+                if ((lane & 15) == 15) sums[half][tile] = z;
+            } else {
+                float worst = INFINITY;
+#pragma unroll
+                for (int q = 0; q < 16; ++q) worst = v[q] > -INFINITY ? fminf(worst, v[q]) : worst;
+                worst = -wave_most(-worst);
+                if (lane == 0) worsts[half][wave] = worst;
+            }
+            if (lane == 0) tops[half][wave] = best;
+        }
         if (a.clear)
             for (int64_t w = this_group * 256 + threadIdx.x; w < a.clear_words; w += a.groups * 256) a.clear[this_row * a.clear_words + w] = 0;
         __syncthreads();  // (the halves: the next group's values do not wait for this one's to be read)
         if (wave != (int)(block & 3)) continue;
-        const float own = lane < GROUP_TILES ? bests[half][lane] : -INFINITY, top = wave_most(own);
-        if (lane < GROUP_TILES && a.tile_best) a.tile_best[block * GROUP_TILES + lane] = own;
+        if (EACH && lane < GROUP_TILES) a.tile_best[block * GROUP_TILES + lane] = bests[half][lane];
+        if constexpr (MODE == TILES_BEST) continue;
+        const float own = tops[half][(lane & 15) / 4], top = fmaxf(fmaxf(tops[half][0], tops[half][1]), fmaxf(tops[half][2], tops[half][3]));
         if (lane == 0) a.group_best[block] = top;
         if constexpr (SUMS) {
             const Weights w(top, scale);
             const double z = lane < GROUP_TILES ? sums[half][lane] : 0.0;
-            if (lane < GROUP_TILES && a.tile_sum) a.tile_sum[block * GROUP_TILES + lane] = z;
+            if (MODE == TILES_SUMS && lane < GROUP_TILES) {
+                a.tile_best[block * GROUP_TILES + lane] = own;
+                a.tile_sum[block * GROUP_TILES + lane] = z;
+            }
             const double all = wave_sum64(own > -INFINITY ? z * w.of(own) : 0.0);
             if (lane == 0) a.group_sum[block] = all;
-        } else if (a.group_worst) {
+        } else {
             if (lane == 0) a.group_worst[block] = fminf(fminf(worsts[half][0], worsts[half][1]), fminf(worsts[half][2], worsts[half][3]));
         }
     }
 }
 
-template <int DT> void launch(const TileArgs& a, bool sums, hipStream_t st) {
+template <int DT> void launch(const TileArgs& a, int mode, hipStream_t st) {
     const dim3 grid = flat_grid(pieces(a.in.rows * a.groups, a.per));
-    if (sums) k_tiles<DT, true><<<grid, 256, 0, st>>>(a);
-    else k_tiles<DT, false><<<grid, 256, 0, st>>>(a);
+    if (mode == TILES_SUMS) k_tiles<DT, TILES_SUMS><<<grid, 256, 0, st>>>(a);
+    else if (mode == TILES_RANGE) k_tiles<DT, TILES_RANGE><<<grid, 256, 0, st>>>(a);
+    else if (mode == TILES_BEST) k_tiles<DT, TILES_BEST><<<grid, 256, 0, st>>>(a);
+    else k_tiles<DT, TILES_BEST_SUMS><<<grid, 256, 0, st>>>(a);
 }
 
 }  // namespace
 
-void kge_launch_tiles(TileArgs a, bool sums, hipStream_t st) {
+void kge_launch_tiles(TileArgs a, TileMode mode, hipStream_t st) {
     a.per = groups_per_workgroup(a.in.rows * a.groups);
-    if (a.in.dtype == KGE_F32) launch<KGE_F32>(a, sums, st);
-    else if (a.in.dtype == KGE_BF16) launch<KGE_BF16>(a, sums, st);
-    else launch<KGE_F16>(a, sums, st);
+    if (a.in.dtype == KGE_F32) launch<KGE_F32>(a, mode, st);
+    else if (a.in.dtype == KGE_BF16) launch<KGE_BF16>(a, mode, st);
+    else launch<KGE_F16>(a, mode, st);
 }

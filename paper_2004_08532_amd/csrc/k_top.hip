@@ -4,7 +4,7 @@
 // puts them in order in LDS (collect_best, order_list).  Of a row in segments every workgroup leaves its candidates, at least
 // its best m; they are collected and ordered in the same way, level by level, until one list is left.
 // log-sum-exp: the weights exp((s - best) / T) of a segment are summed in 64 bits beside it.
-#include "k_rows.h"
+#include "k_draw_list.h"
 
 namespace {
 
@@ -130,6 +130,184 @@ __global__ __launch_bounds__(WAVES * 64) void k_top_merge(MergeArgs a) {
     }
 }
 
+// ---------------------------------------------------------------------------------------------------------
+// Long rows of which every tile's best score is known (k_tiles): a score that m groups of tiles reach with their best bounds the list, so that
+// only the few tiles which reach it are read again, by one workgroup per row.  (100 best of 2.5 M: about 103 tiles of 9766.)
+// ---------------------------------------------------------------------------------------------------------
+struct FinishArgs {
+    RowScores in;
+    int m;
+    int64_t tiles;            // of a row, and the distance of two rows' in tile_best
+    int64_t pitch;
+    const float* tile_best;
+    const float* group_best;  // log-sum-exp: groups of pitch / GROUP_TILES
+    const double* group_sum;
+    double inv_t;
+    int64_t* ids;
+    float* scores;
+    float* lse;               // null: none
+};
+
+template <int DT, int PER, bool DRAW>  // PER: groups of tiles per thread, m <= PER * 512
+__global__ __launch_bounds__(1024) void k_top_finish(FinishArgs a, DrawArgs draw) {
+    constexpr int THREADS = 1024, WAVES = 16, ROOM = BEST_ROOM, TILE_ROOM = 4096;
+    __shared__ uint64_t list[ROOM], sorted[256], masks[WAVES];
+    __shared__ float most[PER * THREADS], maxima[WAVES];
+    __shared__ uint32_t tile_list[TILE_ROOM], rank[256], slots[2 * WAVES], count, n_tiles, shared_bound;
+    __shared__ double sums[DRAW ? KGE_TOP_MAX : WAVES];
+    __shared__ int kept_entries;
+    const int64_t row = flat_block();
+    if (row >= a.in.rows) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const auto* s = static_cast<const typename Score<DT>::type*>(a.in.p) + row * a.in.ld;
+    const float* bests = a.tile_best + row * a.pitch;
+
+    float mine[PER], best = -INFINITY;
+#pragma unroll
+    for (int g = 0; g < PER; ++g) mine[g] = -INFINITY;
+    for (int64_t t0 = threadIdx.x; t0 < a.tiles; t0 += PER * THREADS) {
+#pragma unroll
+        for (int g = 0; g < PER; ++g) {
+            const int64_t t = t0 + g * THREADS;
+            mine[g] = fmaxf(mine[g], t < a.tiles ? bests[t] : -INFINITY);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < PER; ++g) {
+        most[g * THREADS + threadIdx.x] = mine[g];
+        best = fmaxf(best, mine[g]);
+    }
+    if (threadIdx.x == 0) { count = 0; n_tiles = 0; }
+    best = block_max<WAVES>(best, maxima);
+    if (!(best > -INFINITY)) {
+        if constexpr (DRAW) write_empty<THREADS>(draw, row);
+        else write_list<THREADS>(list, 0, a.m, a.ids + row * a.m, a.scores + row * a.m);
+        if (!DRAW && a.lse && threadIdx.x == 0) a.lse[row] = -INFINITY;
+        return;
+    }
+    if (wave == 0) {
+        float x[PER * WAVES];
+#pragma unroll
+        for (int w = 0; w < PER * WAVES; ++w) x[w] = most[w * 64 + lane];
+        const uint32_t b = wave_bound<PER * WAVES>(x, order_key(best), a.m);
+        if (lane == 0) shared_bound = b;
+    }
+    __syncthreads();
+    float t = key_score(shared_bound);
+    for (int64_t i0 = 0; i0 < a.tiles; i0 += THREADS) {
+        const int64_t i = i0 + threadIdx.x;
+        const bool in = i < a.tiles && bests[i] >= t;
+        const uint64_t who = __ballot(in);
+        if (!who) continue;
+        uint32_t at = 0;
+        if (lane == 0) at = atomicAdd(&n_tiles, (uint32_t)__popcll(who));
+        at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + (uint32_t)__popcll(who & (((uint64_t)1 << lane) - 1));
+        if (in && at < TILE_ROOM) tile_list[at] = (uint32_t)i;
+    }
+    __syncthreads();
+    const uint32_t found = n_tiles;
+    if (found <= TILE_ROOM) {
+        constexpr int AT_ONCE = 4;
+        for (uint32_t e0 = wave * AT_ONCE; e0 < found; e0 += WAVES * AT_ONCE) {
+            Quad<DT> x[AT_ONCE];
+            int64_t first[AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                first[k] = (int64_t)tile_list[min(e0 + k, found - 1)] * 256;
+                x[k].load(s, first[k] + lane * 4, a.in.n);
+            }
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                if (e0 + k >= found) break;
+                float v[4];
+                x[k].values(first[k], a.in.n, v);
+                uint32_t marked = 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) marked |= (uint32_t)(v[q] >= t) << q;
+                append_marked<4>(v, marked, [&](int q) { return ~(uint32_t)(first[k] + lane * 4 + q); }, list, ROOM, &count);
+            }
+        }
+        __syncthreads();
+    }
+    int have = (int)count;
+    if (found > TILE_ROOM || have > ROOM) {
+        // Too many scores reach the bound (many equal ones): the tiles in their order, four at a time, into a list that is cut to its best m where it
+        // gets full; from then on only what is above its last entry can enter, since equal scores count by position.
+        bool above = false;
+        have = 0;
+        for (int64_t i0 = 0; i0 < a.tiles; i0 += THREADS) {
+            const int64_t i = i0 + threadIdx.x;
+            const float b = i < a.tiles ? bests[i] : -INFINITY;
+            const uint64_t who = __ballot(above ? b > t : b >= t);
+            __syncthreads();
+            if (lane == 0) masks[wave] = who;
+            __syncthreads();
+            for (int w = 0; w < WAVES; ++w) {
+                uint64_t left = masks[w];
+                while (left) {
+                    int64_t tile = -1;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (!left) break;
+                        const int b2 = __ffsll((unsigned long long)left) - 1;
+                        left &= left - 1;
+                        if (wave / 4 == k) tile = i0 + w * 64 + b2;
+                    }
+                    const int64_t j = tile * 256 + (threadIdx.x & 255);
+                    float v = tile >= 0 && j < a.in.n ? widen<DT>(s[j]) : -INFINITY;
+                    v = fmaxf(v, -INFINITY);
+                    bool in = above ? v > t : v >= t;
+                    if (threadIdx.x == 0) count = have;
+                    int c = block_count<WAVES>(__popcll(__ballot(in)), slots);
+                    if (have + c > ROOM) {
+                        __syncthreads();
+                        uint64_t* sl = order_list<THREADS>(list, sorted, rank, have);
+                        t = key_score((uint32_t)(sl[a.m - 1] >> 32));
+                        above = true;
+                        have = a.m;
+                        in = v > t;
+                        if (threadIdx.x == 0) count = have;
+                        c = block_count<WAVES>(__popcll(__ballot(in)), slots + WAVES);
+                    }
+                    append_marked<1>(&v, in, [&](int) { return ~(uint32_t)j; }, list, ROOM, &count);
+                    have += c;
+                    __syncthreads();
+                }
+            }
+        }
+    }
+    uint64_t* in_order = order_list<THREADS>(list, sorted, rank, have);
+    if constexpr (DRAW) {
+        draw_from_list<THREADS>(draw, row, in_order, in_order == sorted ? list : sorted, rank, min(have, a.m), sums, &kept_entries);
+    } else {
+        write_list<THREADS>(in_order, have, a.m, a.ids + row * a.m, a.scores + row * a.m);
+        if (a.lse) {
+            const int64_t groups = a.pitch / GROUP_TILES;
+            const Scale scale(a.inv_t);
+            const Weights w(best, scale);
+            double z = 0.0;
+            for (int64_t g = threadIdx.x; g < groups; g += THREADS) {
+                const float b = a.group_best[row * groups + g];
+                if (b > -INFINITY) z += a.group_sum[row * groups + g] * w.of(b);
+            }
+            z = block_sum64<WAVES>(z, sums);
+            if (threadIdx.x == 0) a.lse[row] = lse_of(best, z, a.inv_t);
+        }
+    }
+}
+
+template <int DT>
+void launch_finish(const FinishArgs& f, const DrawArgs* draw, hipStream_t st) {
+    const dim3 grid = flat_grid(f.in.rows);
+    if (draw) {
+        if (f.m <= 512) k_top_finish<DT, 1, true><<<grid, 1024, 0, st>>>(f, *draw);
+        else k_top_finish<DT, 2, true><<<grid, 1024, 0, st>>>(f, *draw);
+    } else {
+        if (f.m <= 512) k_top_finish<DT, 1, false><<<grid, 1024, 0, st>>>(f, DrawArgs());
+        else k_top_finish<DT, 2, false><<<grid, 1024, 0, st>>>(f, DrawArgs());
+    }
+}
+
 template <int DT>
 void launch_rows(const TopArgs& a, hipStream_t st) {
     const int64_t n = a.in.n, blocks = a.in.rows * a.segments;
@@ -143,14 +321,39 @@ void launch_rows(const TopArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// us per pass, segment by segment -> by tiles: TO BE MEASURED
+bool kge_top_by_tiles(int64_t n, int m) { return n > KGE_ROW_RESIDENT && n >= 512ll * m; }
+
 int64_t kge_top_workspace(int64_t rows, int64_t n, int m) {
     if (n <= KGE_ROW_RESIDENT) return 0;
+    if (kge_top_by_tiles(n, m)) {
+        const int64_t groups = rows * pieces(n, GROUP);
+        return up256(groups * GROUP_TILES * 4) + up256(groups * 4) + up256(groups * 8);
+    }
     const int64_t segments = pieces(n, KGE_ROW_SEGMENT), second = pieces(segments * m, KGE_ROW_SEGMENT);
     return up256(rows * segments * m * 8) + up256(rows * second * m * 8) + up256(rows * segments * 16);
 }
 
 void kge_launch_top(const RowScores& in, int m, float temperature, int64_t* ids, float* scores, uint64_t* entries, float* lse,
-                    void* workspace, hipStream_t st) {
+                    const DrawArgs* draw, void* workspace, hipStream_t st) {
+    if (kge_top_by_tiles(in.n, m)) {
+        TileArgs t = {};
+        t.in = in; t.inv_t = 1.0 / (double)temperature; t.groups = pieces(in.n, GROUP);
+        char* ws = static_cast<char*>(workspace);
+        t.tile_best = reinterpret_cast<float*>(ws);
+        ws += up256(in.rows * t.groups * GROUP_TILES * 4);
+        t.group_best = reinterpret_cast<float*>(ws);
+        t.group_sum = reinterpret_cast<double*>(ws + up256(in.rows * t.groups * 4));
+        kge_launch_tiles(t, lse ? TILES_BEST_SUMS : TILES_BEST, st);
+        FinishArgs f = {};
+        f.in = in; f.m = m; f.tiles = pieces(in.n, 256); f.pitch = t.groups * GROUP_TILES;
+        f.tile_best = t.tile_best; f.group_best = t.group_best; f.group_sum = t.group_sum;
+        f.inv_t = t.inv_t; f.ids = ids; f.scores = scores; f.lse = lse;
+        if (in.dtype == KGE_F32) launch_finish<KGE_F32>(f, draw, st);
+        else if (in.dtype == KGE_BF16) launch_finish<KGE_BF16>(f, draw, st);
+        else launch_finish<KGE_F16>(f, draw, st);
+        return;
+    }
     TopArgs a = {};
     a.in = in; a.m = m; a.inv_t = 1.0 / (double)temperature; a.want_lse = lse != nullptr;
     a.ids = ids; a.scores = scores; a.lse = lse;

@@ -910,7 +910,7 @@ int kge_top_scores(const void* scores, int32_t dtype, int64_t rows, int64_t n, i
     if (!ids_out || !scores_out) return fail(nullptr, KGE_ERR_INVALID_ARG, "null output%s");
     rc = check_workspace(workspace, workspace_bytes, kge_top_workspace(rows, n, m));
     if (rc != KGE_OK) return rc;
-    kge_launch_top({scores, dtype, rows, n, ld}, m, temperature, ids_out, scores_out, nullptr, lse_out, workspace, (hipStream_t)stream);
+    kge_launch_top({scores, dtype, rows, n, ld}, m, temperature, ids_out, scores_out, nullptr, lse_out, nullptr, workspace, (hipStream_t)stream);
     return launched("kge_top_scores: %s");
 }
 

@@ -74,7 +74,7 @@ def check_top(kge, x, m, T=1.0, **more):
 
 
 SIZES = [(1, 1, 1), (3, 2, 5), (1, 4, 4), (5, 63, 1), (5, 255, 10), (4, 256, 256), (3, 257, 300), (2, 1024, 1024), (4, 1025, 7), (3, 4096, 64),
-         (2, 4097, 1000), (2, 16384, 33), (2, 16385, 1024), (2, 32768, 5), (2, 32769, 1024), (2, 70001, 3), (1, 300_001, 1024)]
+         (2, 4097, 1000), (2, 16384, 33), (2, 16385, 1024), (2, 32768, 5), (2, 32769, 1024), (2, 70001, 3), (1, 300_001, 1024), (2, 300_001, 500), (1, 700_001, 1024)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
@@ -85,7 +85,7 @@ def test_top(kge, rows, n, m, dtype):
     check_top(kge, rows_of(x, dtype, pad=n % 5, offset=n % 3), m, T=0.7)
 
 
-@pytest.mark.parametrize("n,m", [(40, 10), (700, 100), (9000, 512), (20_000, 1024), (50_000, 300)])
+@pytest.mark.parametrize("n,m", [(40, 10), (700, 100), (9000, 512), (20_000, 1024), (50_000, 300), (50_000, 90), (1_300_000, 700)])
 def test_top_of_equal_and_extreme_scores(kge, n, m):
     g = np.random.default_rng(n)
     x = np.empty((9, n))
@@ -103,9 +103,9 @@ def test_top_of_equal_and_extreme_scores(kge, n, m):
 
 def test_sorted_rows(kge):
     """The best ones all in one wave's tiles, or in the last segment."""
-    for n in (5000, 30_000, 100_000):
+    for n, m in ((5000, 1000), (30_000, 1000), (100_000, 1000), (100_000, 100), (1_100_000, 1000)):
         x = torch.arange(n, dtype=torch.float32)[None] / 7
-        check_top(kge, rows_of(torch.cat([x, -x])), 1000, T=50.0)
+        check_top(kge, rows_of(torch.cat([x, -x])), m, T=50.0)
 
 
 # ---- sample
