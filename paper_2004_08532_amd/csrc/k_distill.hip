@@ -6,41 +6,45 @@
 //     grad_j = c T [ P - p_r Z / Z_r ] q_j             candidates that are not listed, where there is a rest
 // p_r = 1 - sum p is the mass that the teacher has outside of the list, q_r = Z_r / Z the student's, P = sum p + p_r.
 //
-// A row is read once and its gradient written once: the weights stay in registers between the sum and the gradient.  Long
-// rows are cut: one launch sums, a second one reads the row again.  What a list adds is little beside its row; its exponentials
-// and everything that is a difference of near values (logarithms of the loss, the rest) are formed in 64 bits.
+// A row that a workgroup holds is read once and its gradient written once: the weights stay in registers between the sum and the gradient.
+// Long rows: a pass for the sums, one workgroup per row for what their gradients have in common, a second pass for the gradient.  Bound by
+// the reads and writes, of long rows by the arithmetic of the weights as much.  A weight is formed in 32 bits from an argument in 64; what is a
+// difference of near values (logarithms of the loss, the rest) and all sums of weights are in 64.
 #include "k_rows.h"
 
 namespace {
+
+// What the gradients of a row have in common: grad_j = w_j * (listed or other) - p * unit, with w relative to `best`; p_e = exp(score / T - shift) * scale.
+struct RowGrad {
+    double best, shift, scale;
+    float listed, other, unit;
+};
 
 struct DistillArgs {
     RowScores in;
     TeacherLists t;
     double inv_t;
-    float grad_scale, loss_scale;  // loss_scale: T^2, and 1 / b in a step
+    float grad_scale, loss_scale;  // grad_scale: of the call times T; loss_scale: T^2, and 1 / b in a step
     float* loss;
     void* grad;
     int64_t ld_grad;
     StepRows step;
-    int segments;
-    double* parts;  // [rows][segments][3]: best score, Z and Z_r relative to it
-    double* lists;  // [rows][4]: see ListSums
+    // long rows
+    int64_t groups, per;  // groups of a row, and of a workgroup
+    double* sums;         // [rows][groups][3]: best score, sum of weights relative to it, of those that are not listed
+    RowGrad* rows;
 };
 
-struct ListSums {
-    double mass;      // sum p
-    double rest;      // p_r, 0 without one
-    double cross;     // sum_e p_e (log p_e - s_e / T)
-    double shift;     // p_e = exp(t_e / T - shift)
+// Weights relative to the largest score of their row (or of a part of it).  The argument of the exponential is formed in 64 bits and its fraction
+// taken in 32, so the weight is off by the roundings of exp2 alone, whatever the distance.  Masked: 0.
+struct Weight32 {
+    double best, per;  // log2(e) / T
+    __device__ __forceinline__ float of(float s) const {
+        const double x = fmax(((double)s - best) * per, -1000.0), shifted = x + 0x1.8p52;  // (NaN: -1000, see `odd`)
+        return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)(x - (shifted - 0x1.8p52))), __double2loint(shifted));
+    }
 };
-
-// Weight of a score relative to the largest of its row, which is finite (or NaN comes out).  The argument of the exponential is
-// formed in 64 bits and its fraction taken in 32: the weight is off by the roundings of exp2 alone, whatever the distance.
-__device__ __forceinline__ float weight32(float s, double best, double scale /* log2(e) / T */) {
-    const double x = ((double)s - best) * scale, n = rint(x);
-    const float e = __builtin_amdgcn_exp2f((float)(x - n));
-    return s > -INFINITY || s != s ? ldexpf(e, (int)fmax(n, -400.0)) : 0.f;
-}
+__device__ __forceinline__ bool odd(float s) { return !(s < INFINITY); }  // NaN or +inf: the row's sums are NaN
 
 template <int DT> struct RowAt {
     const typename Score<DT>::type* s;
@@ -51,57 +55,65 @@ template <int DT> struct RowAt {
     __device__ __forceinline__ float at(int64_t j) const { return of(widen<DT>(s[j])); }
 };
 
-// Sums over a row's list, by a workgroup.
-template <int DT, int WAVES>
-__device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, const RowAt<DT>& r, double* slot) {
-    const int64_t* ids = a.t.ids + row * a.t.m;
-    const float* ts = a.t.scores + row * a.t.m;
-    auto used = [&](int e) { return ids[e] >= 0 && ids[e] < r.n && !(ts[e] == -INFINITY); };
-    ListSums l;
-    if (a.t.lse) {
-        l.shift = (double)a.t.lse[row];
-    } else {
-        float best = -INFINITY;
-        for (int e = threadIdx.x; e < a.t.m; e += WAVES * 64) if (used(e)) best = fmaxf(best, ts[e]);
-        best = block_max<WAVES>(best, reinterpret_cast<float*>(slot));
-        l.shift = best > -INFINITY ? (double)best * a.inv_t : 0.0;
-        double z = 0.0;
-        for (int e = threadIdx.x; e < a.t.m; e += WAVES * 64) if (used(e)) z += exp((double)ts[e] * a.inv_t - l.shift);
-        z = block_sum64<WAVES>(z, slot);
-        if (z > 0.0 || z != z) l.shift += log(z);
+// An entry of a list: the candidate's position, -1 if the entry is not used.
+template <int DT> __device__ __forceinline__ int64_t list_position(const DistillArgs& a, int64_t row, int e, int64_t n) {
+    const int64_t id = a.t.ids[row * a.t.m + e];
+    return id >= 0 && id < n && a.t.scores[row * a.t.m + e] != -INFINITY ? id : -1;
+}
+
+struct ListSums { double a, b; };  // sum of p before it is scaled, sum of p * (log p - s / T)
+
+// A thread's part of the list's sums, with log p = score / T - shift.
+template <int DT, int THREADS>
+__device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, const RowAt<DT>& r, double shift) {
+    ListSums l = {0.0, 0.0};
+#pragma unroll 1
+    for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
+        const int64_t id = list_position<DT>(a, row, e, r.n);
+        if (id < 0) continue;
+        const double lp = (double)a.t.scores[row * a.t.m + e] * a.inv_t - shift, p = exp(lp);
+        l.a += p;
+        if (p > 0.0 || p != p) l.b += p * (lp - (double)r.at(id) * a.inv_t);
     }
-    double mass = 0.0, cross = 0.0;
-    for (int e = threadIdx.x; e < a.t.m; e += WAVES * 64) {
-        if (!used(e)) continue;
-        const double lp = (double)ts[e] * a.inv_t - l.shift, p = exp(lp);
-        mass += p;
-        cross += p > 0.0 || p != p ? p * (lp - (double)r.at(ids[e]) * a.inv_t) : 0.0;
-    }
-    l.mass = block_sum64<WAVES>(mass, slot);
-    l.cross = block_sum64<WAVES>(cross, slot);
-    l.rest = a.t.lse ? fmax(1.0 - l.mass, 0.0) : 0.0;
     return l;
 }
 
-struct RowSums { double best, z, rest; };  // best score; sum of all weights, and of those that are not listed
-
-// What the gradients of a row have in common: w * (listed or other) - p * unit
-struct RowGrad { double best; float listed, other, unit; };
-
-__device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, const RowSums& s, ListSums& l, double& loss) {
-    if (!(s.rest > 0.0)) l.rest = 0.0;  // no candidate that the rest could go to
-    const double mass = l.mass + l.rest;
-    loss = 0.0;
-    RowGrad g = {s.best, 0.f, 0.f, 0.f};
-    if (s.z != 0.0 && mass != 0.0) {
-        const double c = (double)a.grad_scale;
-        loss = l.cross + l.mass * (s.best * a.inv_t + log(s.z));
-        if (l.rest > 0.0) loss += l.rest * log(l.rest * s.z / s.rest);
-        g.listed = (float)(c * mass / s.z);
-        g.other = l.rest > 0.0 ? (float)(c * (mass / s.z - l.rest / s.rest)) : g.listed;
+// From the sums of a row (best score, sum of weights, of those not listed) and of its list.
+__device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, double best, double z, double z_rest, double shift, const ListSums& l) {
+    double mass = l.a, scale = 1.0, rest = 0.0;
+    if (a.t.lse) {
+        rest = fmax(1.0 - mass, 0.0);
+        if (!(z_rest > 0.0)) rest = 0.0;  // no candidate that it could go to
+    } else {
+        scale = mass > 0.0 || mass != mass ? 1.0 / mass : 0.0;
+        mass *= scale;
+    }
+    RowGrad g = {best, shift, scale, 0.f, 0.f, 0.f};
+    const double c = (double)a.grad_scale;
+    if (z != 0.0 && mass + rest != 0.0) {
+        g.listed = (float)(c * (mass + rest) / z);
+        g.other = rest > 0.0 ? (float)(c * ((mass + rest) / z - rest / z_rest)) : g.listed;
         g.unit = (float)c;
     }
     return g;
+}
+__device__ __forceinline__ double row_loss(const DistillArgs& a, double best, double z, double z_rest, const ListSums& l) {
+    double mass = l.a, cross = l.b, rest = 0.0;
+    if (a.t.lse) {
+        rest = z_rest > 0.0 ? fmax(1.0 - mass, 0.0) : 0.0;
+    } else if (mass > 0.0 || mass != mass) {  // log p has still to lose the logarithm of the sum
+        cross = cross / mass - log(mass);
+        mass /= mass;
+    }
+    if (z == 0.0 || mass + rest == 0.0) return 0.0;
+    double loss = cross + mass * (best * a.inv_t + log(z));
+    if (rest > 0.0) loss += rest * log(rest * z / z_rest);
+    return loss * (double)a.loss_scale;
+}
+
+// The list's shift: the teacher's log-sum-exp, or the largest score of the list.
+__device__ __forceinline__ double list_shift(const DistillArgs& a, int64_t row, float most) {
+    return a.t.lse ? (double)a.t.lse[row] : most > -INFINITY ? (double)most * a.inv_t : 0.0;
 }
 
 template <int DT>
@@ -122,154 +134,391 @@ __device__ __forceinline__ void store4(typename Score<DT>::type* row, int64_t j,
     }
 }
 
-enum { WHOLE_ROW, SEGMENT_SUMS, SEGMENT_GRAD };
-
-template <int DT, int WAVES, int TPW, int PASS, bool STEP>
+template <int DT, int WAVES, int TPW, bool STEP>
 __global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
     constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64, N = TPW * 4;
-    constexpr bool GRAD = PASS != SEGMENT_SUMS;
-    __shared__ uint32_t listed[CAP / 32];  // a bit per candidate of this row (segment)
-    __shared__ int32_t list_at[GRAD ? KGE_TOP_MAX : 1];
-    __shared__ float list_grad[GRAD ? KGE_TOP_MAX : 1];
-    __shared__ double slot[WAVES];
+    __shared__ uint32_t listed[CAP / 32];  // a bit per candidate
+    __shared__ int32_t list_at[KGE_TOP_MAX];
+    __shared__ float list_grad[KGE_TOP_MAX], maxima[3][WAVES];
+    __shared__ double parts[4][WAVES];
     __shared__ int twice;  // a candidate is listed more than once
-    const int64_t block = flat_block();
-    if (block >= a.in.rows * a.segments) return;
-    const int64_t row = PASS == WHOLE_ROW ? block : block / a.segments, seg = block - row * a.segments, first = seg * CAP;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row = flat_block();
+    if (row >= a.in.rows) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     RowAt<DT> r;
     r.s = static_cast<const typename Score<DT>::type*>(a.in.p) + row * a.in.ld;
     r.n = a.in.n;
     r.is_dist = STEP && a.step.is_dist; r.gamma = STEP ? a.step.gamma : 0.f;
 
-    float v[N];
-    float best = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < TPW; ++i) {
-        const int64_t tile = first + (int64_t)(i * WAVES + wave) * 256;
-        Quad<DT> x;
-        x.load(r.s, tile + lane * 4, r.n);
-        x.template values<false>(tile, r.n, v + 4 * i);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if constexpr (STEP) { if (tile + lane * 4 + q < r.n) v[4 * i + q] = r.of(v[4 * i + q]); }
-            best = fmaxf(best, v[4 * i + q]);
-        }
-    }
     for (int x = threadIdx.x; x < CAP / 32; x += THREADS) listed[x] = 0;
     if (threadIdx.x == 0) twice = 0;
-    __syncthreads();
-    // the list's candidates among these
-    const int64_t* ids = a.t.ids + row * a.t.m;
-    const float* ts = a.t.scores + row * a.t.m;
-    for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
-        const int64_t id = ids[e], at = id - first;
-        const bool in = id >= first && id < r.n && at < CAP && ts[e] != -INFINITY;
-        if (in) {
-            const uint32_t bit = 1u << (at & 31);
-            if (atomicOr(&listed[at >> 5], bit) & bit) twice = 1;
-        }
-        if constexpr (GRAD) list_at[e] = in ? (int)at : -1;
-    }
-    ListSums l = {};
-    if (PASS == WHOLE_ROW || (PASS == SEGMENT_SUMS && seg == 0)) l = sum_list<DT, WAVES>(a, row, r, slot);
-
-    const double scale = a.inv_t * 1.4426950408889634;
-    RowSums s = {};
-    if constexpr (PASS == SEGMENT_GRAD) {
-        const double* p = a.parts + 3 * row * a.segments;
-        float best = -INFINITY;
-        for (int g = threadIdx.x; g < a.segments; g += THREADS) best = fmaxf(best, (float)p[3 * g]);
-        const double top = (double)block_max<WAVES>(best, reinterpret_cast<float*>(slot));
-        for (int g = threadIdx.x; g < a.segments; g += THREADS) {
-            if (p[3 * g + 1] == 0.0) continue;
-            const double w = p[3 * g] == top ? 1.0 : exp((p[3 * g] - top) * a.inv_t);
-            s.z += p[3 * g + 1] * w;
-            s.rest += p[3 * g + 2] * w;
-        }
-        s.best = top;
-        const double* q = a.lists + 4 * row;
-        l.mass = q[0]; l.rest = q[1]; l.cross = q[2]; l.shift = q[3];
-    } else {
-        s.best = (double)block_max<WAVES>(best, reinterpret_cast<float*>(slot));
-    }
+    float v[N], best = -INFINITY, list_best = -INFINITY;
+    bool bad = false;
+    {
+        Quad<DT> x[TPW];
 #pragma unroll
-    for (int i = 0; i < TPW; ++i) {
-        const int at = (i * WAVES + wave) * 256 + lane * 4;
-        const uint32_t bits = a.t.lse ? listed[at >> 5] >> (at & 31) : 0u;
-        float z = 0.f, zr = 0.f;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            v[4 * i + q] = weight32(v[4 * i + q], s.best, scale);
-            z += v[4 * i + q];
-            zr += bits >> q & 1 ? 0.f : v[4 * i + q];
-        }
-        if constexpr (PASS != SEGMENT_GRAD) {
-            s.z += (double)z;
-            s.rest += (double)zr;
-        }
-    }
-    s.z = block_sum64<WAVES>(s.z, slot);
-    s.rest = a.t.lse ? block_sum64<WAVES>(s.rest, slot) : 0.0;
-
-    if constexpr (PASS == SEGMENT_SUMS) {
-        if (threadIdx.x == 0) {
-            double* p = a.parts + 3 * block;
-            p[0] = s.best; p[1] = s.z; p[2] = s.rest;
-            if (seg == 0) {
-                double* q = a.lists + 4 * row;
-                q[0] = l.mass; q[1] = l.rest; q[2] = l.cross; q[3] = l.shift;
-            }
-        }
-        return;
-    }
-    if constexpr (GRAD) {
-        double loss;
-        const RowGrad g = row_grad(a, s, l, loss);
-        if (threadIdx.x == 0 && seg == 0 && a.loss) a.loss[row] = (float)(loss * (double)a.loss_scale);
-        if constexpr (STEP) { if (threadIdx.x == 0) a.step.cpos[row] = 0.f; }
-        if (!a.grad) return;
-        auto* out = static_cast<typename Score<DT>::type*>(a.grad) + row * a.ld_grad + first;
-        const auto* in = r.s + first;
-        auto shape = [&](float x, float raw) {  // a gradient as the backward products of a step want it
-            if constexpr (STEP) {
-                if (r.is_dist) x = raw > 0.f ? x / raw : 0.f;
-                if (a.step.bf16) x = round_bf16(x);
-            }
-            return x;
-        };
-        auto p_of = [&](int e) { return exp((double)ts[e] * a.inv_t - l.shift); };
-        auto stands = [&](int e) {  // the first entry of a candidate stands for all of them
-            bool ok = true;
-            if (twice) for (int x = 0; x < e; ++x) ok = ok && list_at[x] != list_at[e];
-            return ok;
-        };
-        // the list's candidates: formed before any score is overwritten, stored behind the others
-        for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
-            const int at = list_at[e];
-            if (at < 0 || !stands(e)) continue;
-            double p = p_of(e);
-            if (twice) for (int x = e + 1; x < a.t.m; ++x) if (list_at[x] == at) p += p_of(x);
-            const float raw = widen<DT>(in[at]);
-            list_grad[e] = shape(fmaf(weight32(r.of(raw), s.best, scale), g.listed, -(float)p * g.unit), raw);
-        }
-        __syncthreads();
+        for (int i = 0; i < TPW; ++i) x[i].load(r.s, (i * WAVES + wave) * 256 + lane * 4, r.n);
 #pragma unroll
         for (int i = 0; i < TPW; ++i) {
-            const int64_t tile = (int64_t)(i * WAVES + wave) * 256, j = tile + lane * 4;
-            float x[4], raw[4] = {};
-            if constexpr (STEP) {
-                Quad<DT> again;
-                again.load(in, j, r.n);
-                again.template values<false>(tile, r.n, raw);
-            }
+            const int tile = (i * WAVES + wave) * 256;
+            x[i].template values<false>(tile, r.n, v + 4 * i);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) x[q] = shape(v[4 * i + q] * g.other, raw[q]);
-            if (j < r.n - first) store4<DT>(out, j, r.n - first, x);
+            for (int q = 4 * i; q < 4 * i + 4; ++q) {
+                if constexpr (STEP) { if (tile + lane * 4 + q % 4 < r.n) v[q] = r.of(v[q]); }
+                best = fmaxf(best, v[q]);
+                bad = bad || odd(v[q]);
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
+        const int at = (int)list_position<DT>(a, row, e, r.n);
+        list_at[e] = at;
+        if (at >= 0) {
+            const uint32_t bit = 1u << (at & 31);
+            if (atomicOr(&listed[at >> 5], bit) & bit) twice = 1;
+            list_best = fmaxf(list_best, a.t.scores[row * a.t.m + e]);
+        }
+    }
+    best = wave_most(best);
+    list_best = wave_most(list_best);
+    const float flag = __ballot(bad) ? 1.f : 0.f;
+    if (lane == 0) { maxima[0][wave] = best; maxima[1][wave] = list_best; maxima[2][wave] = flag; }
+    __syncthreads();
+    float any = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        best = fmaxf(best, maxima[0][w]);
+        list_best = fmaxf(list_best, maxima[1][w]);
+        any = fmaxf(any, maxima[2][w]);
+    }
+    const double shift = list_shift(a, row, list_best);
+    const Weight32 weight = {(double)best, a.inv_t * 1.4426950408889634};
+    double z = 0.0, z_rest = 0.0;
+    forget<N>(v);
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+#pragma unroll
+        for (int q = 4 * i; q < 4 * i + 4; ++q) v[q] = weight.of(v[q]);
+        const float four = (v[4 * i] + v[4 * i + 1]) + (v[4 * i + 2] + v[4 * i + 3]);
+        z += (double)four;
+        if (a.t.lse) {
+            const int at = (i * WAVES + wave) * 256 + lane * 4;
+            const uint32_t bits = listed[at >> 5] >> (at & 31) & 15u;
+            float rest = four;
+            if (bits) {
+                rest = 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) rest += bits >> q & 1 ? 0.f : v[4 * i + q];
+            }
+            z_rest += (double)rest;
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (tile by tile: the 64-bit halves of all weights at once would not fit the registers)
+    }
+    forget<N>(v);
+    ListSums l = sum_list<DT, THREADS>(a, row, r, shift);
+    z = wave_sum64(z);
+    l.a = wave_sum64(l.a);
+    l.b = wave_sum64(l.b);
+    if (a.t.lse) z_rest = wave_sum64(z_rest);
+    if constexpr (WAVES > 1) {
+        if (lane == 0) { parts[0][wave] = z; parts[1][wave] = z_rest; parts[2][wave] = l.a; parts[3][wave] = l.b; }
+        __syncthreads();
+        z = z_rest = l.a = l.b = 0.0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) { z += parts[0][w]; z_rest += parts[1][w]; l.a += parts[2][w]; l.b += parts[3][w]; }
+    }
+    if (any > 0.f) z = __longlong_as_double(0x7FF8000000000000ll);
+    if (threadIdx.x == 0) {
+        if (a.loss) a.loss[row] = (float)row_loss(a, weight.best, z, z_rest, l);
+        if constexpr (STEP) a.step.cpos[row] = 0.f;
+    }
+    if (!a.grad) return;
+    const RowGrad g = row_grad(a, weight.best, z, z_rest, shift, l);
+    auto* out = static_cast<typename Score<DT>::type*>(a.grad) + row * a.ld_grad;
+    auto shape = [&](float x, float raw) {  // a gradient as the backward products of a step want it
+        if constexpr (STEP) {
+            if (r.is_dist) x = raw > 0.f ? x / raw : 0.f;
+            if (a.step.bf16) x = round_bf16(x);
+        }
+        return x;
+    };
+    auto p_of = [&](int e) { return exp((double)a.t.scores[row * a.t.m + e] * a.inv_t - shift) * g.scale; };
+    auto stands = [&](int e) {  // the first entry of a candidate stands for all of them
+        bool ok = true;
+        if (twice) for (int x = 0; x < e; ++x) ok = ok && list_at[x] != list_at[e];
+        return ok;
+    };
+    // the list's candidates: formed before any score is overwritten, stored behind the others
+#pragma unroll 1
+    for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
+        const int at = list_at[e];
+        if (at < 0 || !stands(e)) continue;
+        double p = p_of(e);
+        if (twice) for (int x = e + 1; x < a.t.m; ++x) if (list_at[x] == at) p += p_of(x);
+        const float raw = widen<DT>(r.s[at]);
+        list_grad[e] = shape(fmaf(weight.of(r.of(raw)), g.listed, -(float)p * g.unit), raw);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+        const int tile = (i * WAVES + wave) * 256;
+        const int64_t j = tile + lane * 4;
+        float x[4], raw[4] = {};
+        if constexpr (STEP) {
+            Quad<DT> again;
+            again.load(r.s, j, r.n);
+            again.template values<false>(tile, r.n, raw);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[q] = shape(v[4 * i + q] * g.other, raw[q]);
+        if (j < r.n) store4<DT>(out, j, r.n, x);
+        if constexpr (STEP) __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int e = threadIdx.x; e < a.t.m; e += THREADS)
+        if (list_at[e] >= 0 && stands(e)) out[list_at[e]] = narrow<DT>(list_grad[e]);
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Long rows, groups of GROUP scores.  Workgroups go through ranges of groups as in k_tiles; the positions of a row's list stay in registers
+// while they do (up to 4 per thread), and those of a group become bits in LDS.
+// ---------------------------------------------------------------------------------------------------------
+constexpr int LIST_PER = KGE_TOP_MAX / 256, GROUP_WORDS = GROUP / 32;
+
+struct GroupWalk {
+    int64_t row, group;
+    __device__ __forceinline__ void step(int64_t groups) { if (++group == groups) { group = 0; ++row; } }
+};
+
+template <int DT>
+__device__ __forceinline__ void load_list(const DistillArgs& a, int64_t row, int64_t pos[LIST_PER]) {
+#pragma unroll
+    for (int k = 0; k < LIST_PER; ++k) {
+        const int e = k * 256 + threadIdx.x;
+        pos[k] = e < a.t.m ? list_position<DT>(a, row, e, a.in.n) : -1;
+    }
+}
+
+// Sums of groups, each wave's relative to the best of its scores.
+template <int DT>
+__global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
+    __shared__ uint32_t listed[3][GROUP_WORDS];  // of this group, of the next one, and cleared for the one after that
+    __shared__ double parts[2][3][4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t blocks = a.in.rows * a.groups, start = (int64_t)flat_block() * a.per, end = min(start + a.per, blocks);
+    if (start >= blocks) return;
+    GroupWalk at = {start / a.groups, 0};
+    at.group = start - at.row * a.groups;
+    const auto* scores = static_cast<const typename Score<DT>::type*>(a.in.p);
+    const double per = a.inv_t * 1.4426950408889634;
+    const bool rest = a.t.lse != nullptr;
+    Quad<DT> x[4];
+    auto load = [&](const GroupWalk& w) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i].load(scores + w.row * a.in.ld, w.group * GROUP + (wave * 4 + i) * 256 + lane * 4, a.in.n);
+    };
+    int64_t pos[LIST_PER];
+    auto mark = [&](const GroupWalk& w, uint32_t* bits) {
+#pragma unroll
+        for (int k = 0; k < LIST_PER; ++k) {
+            const int64_t p = pos[k] - w.group * GROUP;
+            if (pos[k] >= 0 && p >= 0 && p < GROUP) atomicOr(&bits[p >> 5], 1u << (p & 31));
+        }
+    };
+    load(at);
+    if (rest) {
+        load_list<DT>(a, at.row, pos);
+        for (int w = threadIdx.x; w < 3 * GROUP_WORDS; w += 256) listed[0][w] = 0;
+        __syncthreads();
+        mark(at, listed[0]);
+        __syncthreads();
+    }
+    for (int64_t block = start; block < end; ++block) {
+        const int64_t group = at.group;
+        const int turn = (int)((block - start) % 3), half = (int)(block - start) & 1;
+        float v[16], best = -INFINITY;
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i].template values<false>(group * GROUP + (wave * 4 + i) * 256, a.in.n, v + 4 * i);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            best = fmaxf(best, v[q]);
+            bad = bad || odd(v[q]);
+        }
+        const int64_t row = at.row;
+        at.step(a.groups);
+        if (block + 1 < end) {
+            load(at);
+            if (rest) {
+                if (at.row != row) load_list<DT>(a, at.row, pos);
+                mark(at, listed[(turn + 1) % 3]);
+                for (int w = threadIdx.x; w < GROUP_WORDS; w += 256) listed[(turn + 2) % 3][w] = 0;
+            }
+        }
+        best = wave_most(best);
+        const Weight32 weight = {(double)best, per};
+        double z = 0.0, z_rest = 0.0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[q] = weight.of(v[4 * i + q]);
+            const float four = (w[0] + w[1]) + (w[2] + w[3]);
+            z += (double)four;
+            if (rest) {
+                const int p = (wave * 4 + i) * 256 + lane * 4;
+                const uint32_t bits = listed[turn][p >> 5] >> (p & 31) & 15u;
+                float other = four;
+                if (bits) {
+                    other = 0.f;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) other += bits >> q & 1 ? 0.f : w[q];
+                }
+                z_rest += (double)other;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        z = wave_sum64(z);
+        if (rest) z_rest = wave_sum64(z_rest);
+        if (__ballot(bad)) z = __longlong_as_double(0x7FF8000000000000ll);
+        else if (!(best > -INFINITY)) z = z_rest = 0.0;
+        if (lane == 0) { parts[half][0][wave] = (double)best; parts[half][1][wave] = z; parts[half][2][wave] = z_rest; }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            double top = -INFINITY, s = 0.0, sr = 0.0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) top = fmax(top, parts[half][0][w]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const double b = parts[half][0][w], f = b == top ? 1.0 : exp2((b - top) * per);
+                if (parts[half][1][w] != 0.0) { s += parts[half][1][w] * f; sr += parts[half][2][w] * f; }
+            }
+            double* p = a.sums + 3 * block;
+            p[0] = top; p[1] = s; p[2] = sr;
+        }
+    }
+}
+
+// A row's loss, and what its gradients have in common.
+template <int DT>
+__global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
+    __shared__ double slot[4];
+    __shared__ float maxima[4];
+    const int64_t row = flat_block();
+    if (row >= a.in.rows) return;
+    RowAt<DT> r;
+    r.s = static_cast<const typename Score<DT>::type*>(a.in.p) + row * a.in.ld;
+    r.n = a.in.n; r.is_dist = false; r.gamma = 0.f;
+    const double* p = a.sums + 3 * row * a.groups;
+    const double per = a.inv_t * 1.4426950408889634;
+    float best = -INFINITY, list_best = -INFINITY;
+    for (int64_t g = threadIdx.x; g < a.groups; g += 256) best = fmaxf(best, (float)p[3 * g]);
+    for (int e = threadIdx.x; e < a.t.m; e += 256)
+        if (list_position<DT>(a, row, e, r.n) >= 0) list_best = fmaxf(list_best, a.t.scores[row * a.t.m + e]);
+    best = block_max<4>(best, maxima);
+    list_best = block_max<4>(list_best, maxima);
+    double z = 0.0, z_rest = 0.0;
+    for (int64_t g = threadIdx.x; g < a.groups; g += 256) {
+        if (p[3 * g + 1] == 0.0) continue;
+        const double w = p[3 * g] == (double)best ? 1.0 : exp2((p[3 * g] - (double)best) * per);
+        z += p[3 * g + 1] * w;
+        z_rest += p[3 * g + 2] * w;
+    }
+    z = block_sum64<4>(z, slot);
+    z_rest = block_sum64<4>(z_rest, slot);
+    const double shift = list_shift(a, row, list_best);
+    ListSums l = sum_list<DT, 256>(a, row, r, shift);
+    l.a = block_sum64<4>(l.a, slot);
+    l.b = block_sum64<4>(l.b, slot);
+    if (threadIdx.x == 0) {
+        if (a.loss) a.loss[row] = (float)row_loss(a, (double)best, z, z_rest, l);
+        a.rows[row] = row_grad(a, (double)best, z, z_rest, shift, l);
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
+    __shared__ uint32_t listed[3][GROUP_WORDS];
+    __shared__ float patch[2][GROUP];  // gradients of the list's candidates in the group
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t blocks = a.in.rows * a.groups, start = (int64_t)flat_block() * a.per, end = min(start + a.per, blocks);
+    if (start >= blocks) return;
+    GroupWalk at = {start / a.groups, 0};
+    at.group = start - at.row * a.groups;
+    const auto* scores = static_cast<const typename Score<DT>::type*>(a.in.p);
+    const double per = a.inv_t * 1.4426950408889634;
+    Quad<DT> x[4];
+    auto load = [&](const GroupWalk& w) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i].load(scores + w.row * a.in.ld, w.group * GROUP + (wave * 4 + i) * 256 + lane * 4, a.in.n);
+    };
+    int64_t pos[LIST_PER];
+    RowGrad g = a.rows[at.row];
+    // gradients of a group's listed candidates; an entry of a candidate that has been listed before leaves it to the first
+    auto patch_group = [&](const GroupWalk& w, const RowGrad& gr, uint32_t* bits, float* to) {
+#pragma unroll 1
+        for (int k = 0; k < LIST_PER; ++k) {
+            const int64_t p = pos[k] - w.group * GROUP;
+            if (pos[k] < 0 || p < 0 || p >= GROUP) continue;
+            atomicOr(&bits[p >> 5], 1u << (p & 31));
+            const int64_t* ids = a.t.ids + w.row * a.t.m;
+            const float* ts = a.t.scores + w.row * a.t.m;
+            bool first = true;
+            double sum = 0.0;
+            for (int e = 0; e < a.t.m; ++e) {
+                if (ids[e] != pos[k] || ts[e] == -INFINITY) continue;
+                if (e < k * 256 + (int)threadIdx.x) { first = false; break; }
+                sum += exp((double)ts[e] * a.inv_t - gr.shift);
+            }
+            if (!first) continue;
+            const Weight32 weight = {gr.best, per};
+            to[p] = fmaf(weight.of(widen<DT>(scores[w.row * a.in.ld + pos[k]])), gr.listed, -(float)(sum * gr.scale) * gr.unit);
+        }
+    };
+    load(at);
+    load_list<DT>(a, at.row, pos);
+    for (int w = threadIdx.x; w < 3 * GROUP_WORDS; w += 256) listed[0][w] = 0;
+    __syncthreads();
+    patch_group(at, g, listed[0], patch[0]);
+    __syncthreads();
+    for (int64_t block = start; block < end; ++block) {
+        const GroupWalk here = at;
+        const int turn = (int)((block - start) % 3), half = (int)(block - start) & 1;
+        const RowGrad now = g;
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i].template values<false>(here.group * GROUP + (wave * 4 + i) * 256, a.in.n, v + 4 * i);
+        at.step(a.groups);
+        if (block + 1 < end) {
+            load(at);
+            if (at.row != here.row) {
+                load_list<DT>(a, at.row, pos);
+                g = a.rows[at.row];
+            }
+            patch_group(at, g, listed[(turn + 1) % 3], patch[half ^ 1]);
+            for (int w = threadIdx.x; w < GROUP_WORDS; w += 256) listed[(turn + 2) % 3][w] = 0;
+        }
+        const Weight32 weight = {now.best, per};
+        auto* out = static_cast<typename Score<DT>::type*>(a.grad) + here.row * a.ld_grad;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int p = (wave * 4 + i) * 256 + lane * 4;
+            const int64_t j = here.group * GROUP + p;
+            const uint32_t bits = listed[turn][p >> 5] >> (p & 31) & 15u;
+            float y[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] = weight.of(v[4 * i + q]) * now.other;
+            if (bits) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) if (bits >> q & 1) y[q] = patch[half][p + q];
+            }
+            if (j < a.in.n) store4<DT>(out, j, a.in.n, y);
+            __builtin_amdgcn_sched_barrier(0);
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < a.t.m; e += THREADS)
-            if (list_at[e] >= 0 && stands(e)) out[list_at[e]] = narrow<DT>(list_grad[e]);
     }
 }
 
@@ -282,26 +531,27 @@ void launch_rows(kge_ctx* c, const DistillArgs& a, hipStream_t st) {
         if (c) KGE_LAUNCH(c, kernel, grid, dim3(threads), 0, st, a);
         else hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a);
     };
-    if (n <= 256) go(k_distill<DT, 1, 1, WHOLE_ROW, STEP>, 64);
-    else if (n <= 1024) go(k_distill<DT, 4, 1, WHOLE_ROW, STEP>, 256);
-    else if (n <= 4096) go(k_distill<DT, 4, 4, WHOLE_ROW, STEP>, 256);
-    else if (n <= 16384) go(k_distill<DT, 16, 4, WHOLE_ROW, STEP>, 1024);
-    else go(k_distill<DT, 16, 8, WHOLE_ROW, STEP>, 1024);
+    if (n <= 256) go(k_distill<DT, 1, 1, STEP>, 64);
+    else if (n <= 1024) go(k_distill<DT, 4, 1, STEP>, 256);
+    else if (n <= 4096) go(k_distill<DT, 4, 4, STEP>, 256);
+    else if (n <= 16384) go(k_distill<DT, 16, 4, STEP>, 1024);
+    else go(k_distill<DT, 16, 8, STEP>, 1024);
 }
 
 template <int DT>
 void launch(const DistillArgs& a, hipStream_t st) {
-    if (a.segments == 1) { launch_rows<DT, false>(nullptr, a, st); return; }
-    const dim3 grid = flat_grid(a.in.rows * a.segments);
-    k_distill<DT, 16, 4, SEGMENT_SUMS, false><<<grid, 1024, 0, st>>>(a);
-    k_distill<DT, 16, 4, SEGMENT_GRAD, false><<<grid, 1024, 0, st>>>(a);
+    if (a.groups == 0) { launch_rows<DT, false>(nullptr, a, st); return; }
+    const dim3 grid = flat_grid(pieces(a.in.rows * a.groups, a.per));
+    k_distill_sums<DT><<<grid, 256, 0, st>>>(a);
+    k_distill_finish<DT><<<flat_grid(a.in.rows), 256, 0, st>>>(a);
+    if (a.grad) k_distill_grad<DT><<<grid, 256, 0, st>>>(a);
 }
 
 }  // namespace
 
 int64_t kge_distill_workspace(int64_t rows, int64_t n) {
     if (n <= KGE_ROW_RESIDENT) return 0;
-    return up256(rows * pieces(n, KGE_ROW_SEGMENT) * 24) + up256(rows * 32);
+    return up256(rows * pieces(n, GROUP) * 24) + up256(rows * (int64_t)sizeof(RowGrad));
 }
 
 void kge_launch_distill(const RowScores& in, const TeacherLists& t, float grad_scale, float loss_scale, float* loss, void* grad, int64_t ld_grad,
@@ -312,15 +562,16 @@ void kge_launch_distill(const RowScores& in, const TeacherLists& t, float grad_s
     a.grad_scale = grad_scale * t.temperature;
     a.loss_scale = loss_scale * t.temperature * t.temperature;
     a.loss = loss; a.grad = grad; a.ld_grad = ld_grad;
-    a.segments = in.n <= KGE_ROW_RESIDENT ? 1 : (int)pieces(in.n, KGE_ROW_SEGMENT);
     if (step) {
         a.step = *step;
         launch_rows<KGE_F32, true>(step->c, a, st);
         return;
     }
-    if (a.segments > 1) {
-        a.parts = static_cast<double*>(workspace);
-        a.lists = reinterpret_cast<double*>(static_cast<char*>(workspace) + up256(in.rows * a.segments * 24));
+    if (in.n > KGE_ROW_RESIDENT) {
+        a.groups = pieces(in.n, GROUP);
+        a.per = groups_per_workgroup(in.rows * a.groups);
+        a.sums = static_cast<double*>(workspace);
+        a.rows = reinterpret_cast<RowGrad*>(static_cast<char*>(workspace) + up256(in.rows * a.groups * 24));
     }
     if (in.dtype == KGE_F32) launch<KGE_F32>(a, st);
     else if (in.dtype == KGE_BF16) launch<KGE_BF16>(a, st);

@@ -275,12 +275,6 @@ __device__ __forceinline__ int find_bin(const uint64_t* bins, const BinRule<LOG_
     return b;
 }
 
-// (what has been formed from these is formed again: kept for every score, the parts of its weight would not fit the registers)
-template <int N> __device__ __forceinline__ void forget(float v[N]) {
-#pragma unroll
-    for (int q = 0; q < N; ++q) asm volatile("" : "+v"(v[q]));
-}
-
 template <int WAVES, int TPW> struct CutScratch {
     static constexpr int ROOM = WAVES * TPW * 256 < 1024 ? WAVES * TPW * 256 : 1024, LOG_BINS = WAVES * TPW <= 4 ? 8 : 10, BINS = 1 << LOG_BINS;
     uint64_t bins[BINS > ROOM ? BINS : ROOM];  // then the list

@@ -327,6 +327,12 @@ template <int WAVES> __device__ __forceinline__ float block_max(float v, float* 
     return v;
 }
 
+// What has been formed from these is formed again, and not kept in registers from one place to the other.
+template <int N> __device__ __forceinline__ void forget(float v[N]) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) asm volatile("" : "+v"(v[q]));
+}
+
 // The tiles of a workgroup in registers; returns this thread's largest score.
 template <int DT, int WAVES, int TPW>
 __device__ __forceinline__ float load_tiles(const typename Score<DT>::type* row, int64_t first, int64_t n, float v[TPW * 4]) {
