@@ -16,7 +16,7 @@ namespace {
 
 // What the gradients of a row have in common: grad_j = w_j * (listed or other) - p * unit, with w relative to `best`; p_e = exp(score / T - shift) * scale.
 struct RowGrad {
-    double best, shift, scale;
+    double best, scale;
     float listed, other, unit;
 };
 
@@ -31,20 +31,38 @@ struct DistillArgs {
     StepRows step;
     // long rows
     int64_t groups, per;  // groups of a row, and of a workgroup
-    double* sums;         // [rows][groups][3]: best score, sum of weights relative to it, of those that are not listed
+    double* sums;         // [rows][groups][3]: a score, the weights' sum relative to it, that of the listed ones where there is a rest
     RowGrad* rows;
 };
 
-// Weights relative to the largest score of their row (or of a part of it).  The argument of the exponential is formed in 64 bits and its fraction
-// taken in 32, so the weight is off by the roundings of exp2 alone, whatever the distance.  Masked: 0.
+__device__ __forceinline__ float larger(float a, float b) {  // NaN: the other (as fmaxf, without a step that quiets signalling ones)
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ float largest(float a, float b, float c) {  // NaN if one of them is
+    float r;
+    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// Weights relative to `best`.  The argument of the exponential is formed in 64 bits and its fraction taken in 32, so the weight is off by
+// the roundings of exp2 alone, whatever the distance.  Masked: 0.
 struct Weight32 {
-    double best, per;  // log2(e) / T
+    double best, per;  // per: log2(e) / T, or less where neighbouring numbers are so far apart that all weights but the best's are 0
+    float floor;       // a weight of 0, below the best
+    __device__ __forceinline__ Weight32(float b, double p) {
+        const float at = fabsf(b) < INFINITY ? b : 0.f;  // (no candidate)
+        best = (double)at;
+        per = fmin(p, 0x1p43 / fmax(fabs(best), 1e-300));
+        const float far = at - (float)fmin(1024.0 / per, 3e38);
+        floor = far < at ? far : score_below(at);
+    }
     __device__ __forceinline__ float of(float s) const {
-        const double x = fmax(((double)s - best) * per, -1000.0), shifted = x + 0x1.8p52;  // (NaN: -1000, see `odd`)
-        return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)(x - (shifted - 0x1.8p52))), __double2loint(shifted));
+        const double d = (double)larger(s, floor) - best, shifted = fma(d, per, 0x1.8p52), f = fma(d, per, -(shifted - 0x1.8p52));
+        return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)f), __double2loint(shifted));
     }
 };
-__device__ __forceinline__ bool odd(float s) { return !(s < INFINITY); }  // NaN or +inf: the row's sums are NaN
 
 template <int DT> struct RowAt {
     const typename Score<DT>::type* s;
@@ -79,7 +97,7 @@ __device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, 
 }
 
 // From the sums of a row (best score, sum of weights, of those not listed) and of its list.
-__device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, double best, double z, double z_rest, double shift, const ListSums& l) {
+__device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, double best, double z, double z_rest, const ListSums& l) {
     double mass = l.a, scale = 1.0, rest = 0.0;
     if (a.t.lse) {
         rest = fmax(1.0 - mass, 0.0);
@@ -88,7 +106,7 @@ __device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, double best, d
         scale = mass > 0.0 || mass != mass ? 1.0 / mass : 0.0;
         mass *= scale;
     }
-    RowGrad g = {best, shift, scale, 0.f, 0.f, 0.f};
+    RowGrad g = {best, scale, 0.f, 0.f, 0.f};
     const double c = (double)a.grad_scale;
     if (z != 0.0 && mass + rest != 0.0) {
         g.listed = (float)(c * (mass + rest) / z);
@@ -116,9 +134,10 @@ __device__ __forceinline__ double list_shift(const DistillArgs& a, int64_t row, 
     return a.t.lse ? (double)a.t.lse[row] : most > -INFINITY ? (double)most * a.inv_t : 0.0;
 }
 
+// Gradients j .. j + 3 of a row of n, but those of candidates whose bit is set.
 template <int DT>
-__device__ __forceinline__ void store4(typename Score<DT>::type* row, int64_t j, int64_t n, const float v[4]) {
-    if (j + 4 <= n) {
+__device__ __forceinline__ void store_unlisted(typename Score<DT>::type* row, int64_t j, int64_t n, const float v[4], uint32_t bits) {
+    if (j + 4 <= n && bits == 0) {
         if constexpr (DT == KGE_F32) {
             f32x4u x;
             x.x = v[0]; x.y = v[1]; x.z = v[2]; x.w = v[3];
@@ -130,7 +149,7 @@ __device__ __forceinline__ void store4(typename Score<DT>::type* row, int64_t j,
         }
     } else {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) if (j + q < n) row[j + q] = narrow<DT>(v[q]);
+        for (int q = 0; q < 4; ++q) if (j + q < n && !(bits >> q & 1)) row[j + q] = narrow<DT>(v[q]);
     }
 }
 
@@ -139,7 +158,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
     constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64, N = TPW * 4;
     __shared__ uint32_t listed[CAP / 32];  // a bit per candidate
     __shared__ int32_t list_at[KGE_TOP_MAX];
-    __shared__ float list_grad[KGE_TOP_MAX], maxima[3][WAVES];
+    __shared__ float maxima[2][WAVES];
     __shared__ double parts[4][WAVES];
     __shared__ int twice;  // a candidate is listed more than once
     const int64_t row = flat_block();
@@ -153,7 +172,6 @@ __global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
     for (int x = threadIdx.x; x < CAP / 32; x += THREADS) listed[x] = 0;
     if (threadIdx.x == 0) twice = 0;
     float v[N], best = -INFINITY, list_best = -INFINITY;
-    bool bad = false;
     {
         Quad<DT> x[TPW];
 #pragma unroll
@@ -162,14 +180,14 @@ __global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
         for (int i = 0; i < TPW; ++i) {
             const int tile = (i * WAVES + wave) * 256;
             x[i].template values<false>(tile, r.n, v + 4 * i);
+            if constexpr (STEP) {
 #pragma unroll
-            for (int q = 4 * i; q < 4 * i + 4; ++q) {
-                if constexpr (STEP) { if (tile + lane * 4 + q % 4 < r.n) v[q] = r.of(v[q]); }
-                best = fmaxf(best, v[q]);
-                bad = bad || odd(v[q]);
+                for (int q = 0; q < 4; ++q) if (tile + lane * 4 + q < r.n) v[4 * i + q] = r.of(v[4 * i + q]);
             }
+            best = largest(largest(best, v[4 * i], v[4 * i + 1]), v[4 * i + 2], v[4 * i + 3]);
         }
     }
+    const bool bad = __ballot(!(best < INFINITY)) != 0;  // NaN or +inf: the row's sums are NaN
     __syncthreads();
 #pragma unroll 1
     for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
@@ -181,39 +199,37 @@ __global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
             list_best = fmaxf(list_best, a.t.scores[row * a.t.m + e]);
         }
     }
-    best = wave_most(best);
+    best = bad ? INFINITY : wave_most(best);
     list_best = wave_most(list_best);
-    const float flag = __ballot(bad) ? 1.f : 0.f;
-    if (lane == 0) { maxima[0][wave] = best; maxima[1][wave] = list_best; maxima[2][wave] = flag; }
+    if (lane == 0) { maxima[0][wave] = best; maxima[1][wave] = list_best; }
     __syncthreads();
-    float any = 0.f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
         best = fmaxf(best, maxima[0][w]);
         list_best = fmaxf(list_best, maxima[1][w]);
-        any = fmaxf(any, maxima[2][w]);
     }
     const double shift = list_shift(a, row, list_best);
-    const Weight32 weight = {(double)best, a.inv_t * 1.4426950408889634};
-    double z = 0.0, z_rest = 0.0;
+    const Weight32 weight(best, a.inv_t * 1.4426950408889634);
+    // sums of the weights: with a rest, of the candidates that are not listed, and of the few others
+    double z = 0.0, z_listed = 0.0;
     forget<N>(v);
 #pragma unroll
     for (int i = 0; i < TPW; ++i) {
+        const int at = (i * WAVES + wave) * 256 + lane * 4;
+        const uint32_t bits = a.t.lse ? listed[at >> 5] >> (at & 31) & 15u : 0u;
+        float four;
 #pragma unroll
         for (int q = 4 * i; q < 4 * i + 4; ++q) v[q] = weight.of(v[q]);
-        const float four = (v[4 * i] + v[4 * i + 1]) + (v[4 * i + 2] + v[4 * i + 3]);
-        z += (double)four;
-        if (a.t.lse) {
-            const int at = (i * WAVES + wave) * 256 + lane * 4;
-            const uint32_t bits = listed[at >> 5] >> (at & 31) & 15u;
-            float rest = four;
-            if (bits) {
-                rest = 0.f;
+        four = (v[4 * i] + v[4 * i + 1]) + (v[4 * i + 2] + v[4 * i + 3]);
+        if (bits) {
+            four = 0.f;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) rest += bits >> q & 1 ? 0.f : v[4 * i + q];
+            for (int q = 0; q < 4; ++q) {
+                if (bits >> q & 1) z_listed += (double)v[4 * i + q];
+                else four += v[4 * i + q];
             }
-            z_rest += (double)rest;
         }
+        z += (double)four;
         __builtin_amdgcn_sched_barrier(0);  // (tile by tile: the 64-bit halves of all weights at once would not fit the registers)
     }
     forget<N>(v);
@@ -221,21 +237,23 @@ __global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
     z = wave_sum64(z);
     l.a = wave_sum64(l.a);
     l.b = wave_sum64(l.b);
-    if (a.t.lse) z_rest = wave_sum64(z_rest);
+    if (a.t.lse) z_listed = wave_sum64(z_listed);
     if constexpr (WAVES > 1) {
-        if (lane == 0) { parts[0][wave] = z; parts[1][wave] = z_rest; parts[2][wave] = l.a; parts[3][wave] = l.b; }
+        if (lane == 0) { parts[0][wave] = z; parts[1][wave] = z_listed; parts[2][wave] = l.a; parts[3][wave] = l.b; }
         __syncthreads();
-        z = z_rest = l.a = l.b = 0.0;
+        z = z_listed = l.a = l.b = 0.0;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) { z += parts[0][w]; z_rest += parts[1][w]; l.a += parts[2][w]; l.b += parts[3][w]; }
+        for (int w = 0; w < WAVES; ++w) { z += parts[0][w]; z_listed += parts[1][w]; l.a += parts[2][w]; l.b += parts[3][w]; }
     }
-    if (any > 0.f) z = __longlong_as_double(0x7FF8000000000000ll);
+    const double z_rest = z;
+    z += z_listed;
+    if (best == INFINITY) z = __longlong_as_double(0x7FF8000000000000ll);
     if (threadIdx.x == 0) {
         if (a.loss) a.loss[row] = (float)row_loss(a, weight.best, z, z_rest, l);
         if constexpr (STEP) a.step.cpos[row] = 0.f;
     }
     if (!a.grad) return;
-    const RowGrad g = row_grad(a, weight.best, z, z_rest, shift, l);
+    const RowGrad g = row_grad(a, weight.best, z, z_rest, l);
     auto* out = static_cast<typename Score<DT>::type*>(a.grad) + row * a.ld_grad;
     auto shape = [&](float x, float raw) {  // a gradient as the backward products of a step want it
         if constexpr (STEP) {
@@ -244,47 +262,42 @@ __global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
         }
         return x;
     };
-    auto p_of = [&](int e) { return exp((double)a.t.scores[row * a.t.m + e] * a.inv_t - shift) * g.scale; };
-    auto stands = [&](int e) {  // the first entry of a candidate stands for all of them
-        bool ok = true;
-        if (twice) for (int x = 0; x < e; ++x) ok = ok && list_at[x] != list_at[e];
-        return ok;
-    };
-    // the list's candidates: formed before any score is overwritten, stored behind the others
+    // The list's candidates are stored here and left out below, so that neither has to wait for the other.  The first entry of a candidate
+    // stands for all of them.
 #pragma unroll 1
     for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
         const int at = list_at[e];
-        if (at < 0 || !stands(e)) continue;
+        if (at < 0) continue;
+        auto p_of = [&](int x) { return exp((double)a.t.scores[row * a.t.m + x] * a.inv_t - shift) * g.scale; };
         double p = p_of(e);
-        if (twice) for (int x = e + 1; x < a.t.m; ++x) if (list_at[x] == at) p += p_of(x);
+        bool stands = true;
+        if (twice) {
+            for (int x = 0; x < e; ++x) stands = stands && list_at[x] != at;
+            for (int x = e + 1; stands && x < a.t.m; ++x) if (list_at[x] == at) p += p_of(x);
+        }
+        if (!stands) continue;
         const float raw = widen<DT>(r.s[at]);
-        list_grad[e] = shape(fmaf(weight.of(r.of(raw)), g.listed, -(float)p * g.unit), raw);
+        out[at] = narrow<DT>(shape(fmaf(weight.of(r.of(raw)), g.listed, -(float)p * g.unit), raw));
     }
-    __syncthreads();
 #pragma unroll
     for (int i = 0; i < TPW; ++i) {
-        const int tile = (i * WAVES + wave) * 256;
-        const int64_t j = tile + lane * 4;
+        const int tile = (i * WAVES + wave) * 256, at = tile + lane * 4;
         float x[4], raw[4] = {};
         if constexpr (STEP) {
             Quad<DT> again;
-            again.load(r.s, j, r.n);
+            again.load(r.s, at, r.n);
             again.template values<false>(tile, r.n, raw);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[q] = shape(v[4 * i + q] * g.other, raw[q]);
-        if (j < r.n) store4<DT>(out, j, r.n, x);
+        if (at < r.n) store_unlisted<DT>(out, at, r.n, x, listed[at >> 5] >> (at & 31) & 15u);
         if constexpr (STEP) __builtin_amdgcn_sched_barrier(0);
     }
-    __syncthreads();
-#pragma unroll 1
-    for (int e = threadIdx.x; e < a.t.m; e += THREADS)
-        if (list_at[e] >= 0 && stands(e)) out[list_at[e]] = narrow<DT>(list_grad[e]);
 }
 
 // ---------------------------------------------------------------------------------------------------------
 // Long rows, groups of GROUP scores.  Workgroups go through ranges of groups as in k_tiles; the positions of a row's list stay in registers
-// while they do (up to 4 per thread), and those of a group become bits in LDS.
+// while they do (up to 4 per thread), and those in a group become bits in LDS.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int LIST_PER = KGE_TOP_MAX / 256, GROUP_WORDS = GROUP / 32;
 
@@ -293,20 +306,35 @@ struct GroupWalk {
     __device__ __forceinline__ void step(int64_t groups) { if (++group == groups) { group = 0; ++row; } }
 };
 
-template <int DT>
-__device__ __forceinline__ void load_list(const DistillArgs& a, int64_t row, int64_t pos[LIST_PER]) {
+// The bits of the listed candidates of a group.  Three sets: this group's, the next one's, and one that is cleared for the group after that, so
+// that one barrier per group is enough.
+template <int DT> struct GroupMarks {
+    int64_t pos[LIST_PER];
+    __device__ __forceinline__ void load(const DistillArgs& a, int64_t row) {
 #pragma unroll
-    for (int k = 0; k < LIST_PER; ++k) {
-        const int e = k * 256 + threadIdx.x;
-        pos[k] = e < a.t.m ? list_position<DT>(a, row, e, a.in.n) : -1;
+        for (int k = 0; k < LIST_PER; ++k) {
+            const int e = k * 256 + threadIdx.x;
+            pos[k] = e < a.t.m ? list_position<DT>(a, row, e, a.in.n) : -1;
+        }
     }
-}
+    __device__ __forceinline__ void set(const DistillArgs& a, int64_t group, uint32_t* bits) const {
+#pragma unroll
+        for (int k = 0; k < LIST_PER; ++k) {
+            if (k * 256 >= a.t.m) break;
+            const int64_t p = pos[k] - group * GROUP;
+            if (pos[k] >= 0 && p >= 0 && p < GROUP) atomicOr(&bits[p >> 5], 1u << (p & 31));
+        }
+    }
+};
+__device__ __forceinline__ void clear_marks(uint32_t* bits) { if (threadIdx.x < GROUP_WORDS) bits[threadIdx.x] = 0; }
+__device__ __forceinline__ uint32_t marks_of(const uint32_t* bits, int p) { return bits[p >> 5] >> (p & 31) & 15u; }
 
-// Sums of groups, each wave's relative to the best of its scores.
+// Sums of the weights of a workgroup's part of a row, noted with its last group; its other groups note none.  A wave adds up relative to a score of
+// its own, the best of the first scores it meets, and takes another one only when a score lies 2^40 above (in weights).
 template <int DT>
 __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
-    __shared__ uint32_t listed[3][GROUP_WORDS];  // of this group, of the next one, and cleared for the one after that
-    __shared__ double parts[2][3][4];
+    __shared__ uint32_t listed[3][GROUP_WORDS];
+    __shared__ double parts[3][4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t blocks = a.in.rows * a.groups, start = (int64_t)flat_block() * a.per, end = min(start + a.per, blocks);
     if (start >= blocks) return;
@@ -320,93 +348,108 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i].load(scores + w.row * a.in.ld, w.group * GROUP + (wave * 4 + i) * 256 + lane * 4, a.in.n);
     };
-    int64_t pos[LIST_PER];
-    auto mark = [&](const GroupWalk& w, uint32_t* bits) {
-#pragma unroll
-        for (int k = 0; k < LIST_PER; ++k) {
-            const int64_t p = pos[k] - w.group * GROUP;
-            if (pos[k] >= 0 && p >= 0 && p < GROUP) atomicOr(&bits[p >> 5], 1u << (p & 31));
-        }
-    };
+    GroupMarks<DT> marks;
     load(at);
     if (rest) {
-        load_list<DT>(a, at.row, pos);
-        for (int w = threadIdx.x; w < 3 * GROUP_WORDS; w += 256) listed[0][w] = 0;
+        marks.load(a, at.row);
+        for (int k = 0; k < 3; ++k) clear_marks(listed[k]);
         __syncthreads();
-        mark(at, listed[0]);
+        marks.set(a, at.group, listed[0]);
         __syncthreads();
     }
+    float base = -INFINITY, limit = -INFINITY;
+    double z = 0.0, z_listed = 0.0;  // of this lane
+    Weight32 weight(base, per);
+    int turn = 0;
     for (int64_t block = start; block < end; ++block) {
-        const int64_t group = at.group;
-        const int turn = (int)((block - start) % 3), half = (int)(block - start) & 1;
+        const GroupWalk here = at;
         float v[16], best = -INFINITY;
-        bool bad = false;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i].template values<false>(group * GROUP + (wave * 4 + i) * 256, a.in.n, v + 4 * i);
-#pragma unroll
-        for (int q = 0; q < 16; ++q) {
-            best = fmaxf(best, v[q]);
-            bad = bad || odd(v[q]);
-        }
-        const int64_t row = at.row;
-        at.step(a.groups);
-        if (block + 1 < end) {
-            load(at);
-            if (rest) {
-                if (at.row != row) load_list<DT>(a, at.row, pos);
-                mark(at, listed[(turn + 1) % 3]);
-                for (int w = threadIdx.x; w < GROUP_WORDS; w += 256) listed[(turn + 2) % 3][w] = 0;
-            }
-        }
-        best = wave_most(best);
-        const Weight32 weight = {(double)best, per};
-        double z = 0.0, z_rest = 0.0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float w[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) w[q] = weight.of(v[4 * i + q]);
-            const float four = (w[0] + w[1]) + (w[2] + w[3]);
-            z += (double)four;
+            x[i].template values<false>(here.group * GROUP + (wave * 4 + i) * 256, a.in.n, v + 4 * i);
+            best = largest(largest(best, v[4 * i], v[4 * i + 1]), v[4 * i + 2], v[4 * i + 3]);
+        }
+        at.step(a.groups);
+        const int next = turn == 2 ? 0 : turn + 1;
+        if (block + 1 < end) {
+            load(at);  // (arrives while these are worked on)
             if (rest) {
-                const int p = (wave * 4 + i) * 256 + lane * 4;
-                const uint32_t bits = listed[turn][p >> 5] >> (p & 31) & 15u;
-                float other = four;
-                if (bits) {
-                    other = 0.f;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) other += bits >> q & 1 ? 0.f : w[q];
-                }
-                z_rest += (double)other;
+                if (at.row != here.row) marks.load(a, at.row);
+                marks.set(a, at.group, listed[next]);
+                clear_marks(listed[next == 2 ? 0 : next + 1]);
             }
+        }
+        if (__ballot(!(best <= limit))) {  // far above what the sums are relative to, or NaN
+            const bool bad = __ballot(!(best < INFINITY)) != 0;
+            const float top = wave_most(best);
+            if (bad) {
+                z = __longlong_as_double(0x7FF8000000000000ll);
+                limit = INFINITY;  // (NaN comes back here, and is NaN again)
+            } else if (top > limit) {
+                const double f = base > -INFINITY ? exp2(((double)base - (double)top) * per) : 0.0;
+                z = f == 0.0 && !(z != z) ? 0.0 : z * f;
+                z_listed = f == 0.0 ? 0.0 : z_listed * f;
+                base = top;
+                limit = top + (float)fmin(40.0 / per, 3e38);
+                weight = Weight32(base, per);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t bits = rest ? marks_of(listed[turn], (wave * 4 + i) * 256 + lane * 4) : 0u;
+#pragma unroll
+            for (int q = 4 * i; q < 4 * i + 4; ++q) v[q] = weight.of(v[q]);
+            float four = (v[4 * i] + v[4 * i + 1]) + (v[4 * i + 2] + v[4 * i + 3]);
+            if (bits) {
+                four = 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (bits >> q & 1) z_listed += (double)v[4 * i + q];
+                    else four += v[4 * i + q];
+                }
+            }
+            z += (double)four;
             __builtin_amdgcn_sched_barrier(0);
         }
-        z = wave_sum64(z);
-        if (rest) z_rest = wave_sum64(z_rest);
-        if (__ballot(bad)) z = __longlong_as_double(0x7FF8000000000000ll);
-        else if (!(best > -INFINITY)) z = z_rest = 0.0;
-        if (lane == 0) { parts[half][0][wave] = (double)best; parts[half][1][wave] = z; parts[half][2][wave] = z_rest; }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            double top = -INFINITY, s = 0.0, sr = 0.0;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) top = fmax(top, parts[half][0][w]);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const double b = parts[half][0][w], f = b == top ? 1.0 : exp2((b - top) * per);
-                if (parts[half][1][w] != 0.0) { s += parts[half][1][w] * f; sr += parts[half][2][w] * f; }
-            }
-            double* p = a.sums + 3 * block;
-            p[0] = top; p[1] = s; p[2] = sr;
+        turn = next;
+        const bool last = block + 1 == end || at.row != here.row;
+        if (last) {
+            z = wave_sum64(z);
+            if (rest) z_listed = wave_sum64(z_listed);
+            if (lane == 0) { parts[0][wave] = (double)base; parts[1][wave] = z; parts[2][wave] = z_listed; }
+            base = limit = -INFINITY;
+            z = z_listed = 0.0;
         }
+        if (last || rest) __syncthreads();
+        if (threadIdx.x == 0) {
+            double* p = a.sums + 3 * block;
+            double top = -INFINITY, s = 0.0, sl = 0.0;
+            if (last) {
+#pragma unroll 1
+                for (int w = 0; w < 4; ++w) top = fmax(top, parts[0][w]);
+#pragma unroll 1
+                for (int w = 0; w < 4; ++w) {
+                    const double b = parts[0][w], f = b == top ? 1.0 : exp2((b - top) * per);
+                    if (parts[1][w] != 0.0) s += parts[1][w] * f;
+                    if (parts[2][w] != 0.0) sl += parts[2][w] * f;
+                }
+            }
+            p[0] = top; p[1] = s; p[2] = sl;
+        }
+        if (last) __syncthreads();
     }
 }
 
-// A row's loss, and what its gradients have in common.
+// A row's loss, what its gradients have in common, and the gradients of its listed candidates: k_distill_grad leaves these out, and what it reads in
+// their place (where gradients replace the scores) does not matter to it.
 template <int DT>
 __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
+    constexpr int SLOTS = 2 * KGE_TOP_MAX;
     __shared__ double slot[4];
     __shared__ float maxima[4];
+    __shared__ uint32_t key[SLOTS], first[SLOTS], times[SLOTS];  // candidates of the list, its first entry and their number
+    __shared__ uint16_t entry_slot[KGE_TOP_MAX];
+    __shared__ RowGrad shared_grad;
     const int64_t row = flat_block();
     if (row >= a.in.rows) return;
     RowAt<DT> r;
@@ -414,35 +457,67 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     r.n = a.in.n; r.is_dist = false; r.gamma = 0.f;
     const double* p = a.sums + 3 * row * a.groups;
     const double per = a.inv_t * 1.4426950408889634;
+    constexpr uint32_t NONE = 0xFFFFFFFFu;  // (not a position: rows have fewer than 2^32 candidates)
+    for (int x = threadIdx.x; x < SLOTS; x += 256) { key[x] = NONE; first[x] = NONE; times[x] = 0; }
     float best = -INFINITY, list_best = -INFINITY;
     for (int64_t g = threadIdx.x; g < a.groups; g += 256) best = fmaxf(best, (float)p[3 * g]);
-    for (int e = threadIdx.x; e < a.t.m; e += 256)
-        if (list_position<DT>(a, row, e, r.n) >= 0) list_best = fmaxf(list_best, a.t.scores[row * a.t.m + e]);
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.t.m; e += 256) {
+        const int64_t id = list_position<DT>(a, row, e, r.n);
+        if (id < 0) { entry_slot[e] = 0xFFFF; continue; }
+        list_best = fmaxf(list_best, a.t.scores[row * a.t.m + e]);
+        uint32_t x = ((uint32_t)id * 2654435761u) >> 21;  // (2^11 slots for up to 2^10 candidates: there is always a free one)
+        while (true) {
+            const uint32_t was = atomicCAS(&key[x], NONE, (uint32_t)id);
+            if (was == NONE || was == (uint32_t)id) break;
+            x = (x + 1) & (SLOTS - 1);
+        }
+        atomicMin(&first[x], (uint32_t)e);
+        atomicAdd(&times[x], 1u);
+        entry_slot[e] = (uint16_t)x;
+    }
     best = block_max<4>(best, maxima);
     list_best = block_max<4>(list_best, maxima);
-    double z = 0.0, z_rest = 0.0;
+    double z = 0.0, z_listed = 0.0;
     for (int64_t g = threadIdx.x; g < a.groups; g += 256) {
-        if (p[3 * g + 1] == 0.0) continue;
-        const double w = p[3 * g] == (double)best ? 1.0 : exp2((p[3 * g] - (double)best) * per);
-        z += p[3 * g + 1] * w;
-        z_rest += p[3 * g + 2] * w;
+        const double b = p[3 * g], f = b == (double)best ? 1.0 : exp2((b - (double)best) * per);
+        if (p[3 * g + 1] != 0.0) z += p[3 * g + 1] * f;
+        if (p[3 * g + 2] != 0.0) z_listed += p[3 * g + 2] * f;
     }
     z = block_sum64<4>(z, slot);
-    z_rest = block_sum64<4>(z_rest, slot);
-    const double shift = list_shift(a, row, list_best);
+    z_listed = block_sum64<4>(z_listed, slot);
+    const double shift = list_shift(a, row, list_best), z_rest = z;
+    z += z_listed;
     ListSums l = sum_list<DT, 256>(a, row, r, shift);
     l.a = block_sum64<4>(l.a, slot);
     l.b = block_sum64<4>(l.b, slot);
     if (threadIdx.x == 0) {
-        if (a.loss) a.loss[row] = (float)row_loss(a, (double)best, z, z_rest, l);
-        a.rows[row] = row_grad(a, (double)best, z, z_rest, shift, l);
+        const double b = best > -INFINITY ? (double)best : 0.0;
+        if (a.loss) a.loss[row] = (float)row_loss(a, b, z, z_rest, l);
+        a.rows[row] = shared_grad = row_grad(a, b, z, z_rest, l);
+    }
+    __syncthreads();
+    if (!a.grad) return;
+    const RowGrad g = shared_grad;
+    const Weight32 weight(best, per);
+    auto* out = static_cast<typename Score<DT>::type*>(a.grad) + row * a.ld_grad;
+    for (int e = threadIdx.x; e < a.t.m; e += 256) {
+        const uint32_t x = entry_slot[e];
+        if (x == 0xFFFF || first[x] != (uint32_t)e) continue;
+        double sum = exp((double)a.t.scores[row * a.t.m + e] * a.inv_t - shift);
+        uint32_t left = times[x] - 1;
+        for (int y = e + 1; left; ++y) {
+            if (entry_slot[y] != x) continue;
+            sum += exp((double)a.t.scores[row * a.t.m + y] * a.inv_t - shift);
+            --left;
+        }
+        out[key[x]] = narrow<DT>(fmaf(weight.of(r.at(key[x])), g.listed, -(float)(sum * g.scale) * g.unit));
     }
 }
 
 template <int DT>
 __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
     __shared__ uint32_t listed[3][GROUP_WORDS];
-    __shared__ float patch[2][GROUP];  // gradients of the list's candidates in the group
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t blocks = a.in.rows * a.groups, start = (int64_t)flat_block() * a.per, end = min(start + a.per, blocks);
     if (start >= blocks) return;
@@ -455,68 +530,44 @@ __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i].load(scores + w.row * a.in.ld, w.group * GROUP + (wave * 4 + i) * 256 + lane * 4, a.in.n);
     };
-    int64_t pos[LIST_PER];
-    RowGrad g = a.rows[at.row];
-    // gradients of a group's listed candidates; an entry of a candidate that has been listed before leaves it to the first
-    auto patch_group = [&](const GroupWalk& w, const RowGrad& gr, uint32_t* bits, float* to) {
-#pragma unroll 1
-        for (int k = 0; k < LIST_PER; ++k) {
-            const int64_t p = pos[k] - w.group * GROUP;
-            if (pos[k] < 0 || p < 0 || p >= GROUP) continue;
-            atomicOr(&bits[p >> 5], 1u << (p & 31));
-            const int64_t* ids = a.t.ids + w.row * a.t.m;
-            const float* ts = a.t.scores + w.row * a.t.m;
-            bool first = true;
-            double sum = 0.0;
-            for (int e = 0; e < a.t.m; ++e) {
-                if (ids[e] != pos[k] || ts[e] == -INFINITY) continue;
-                if (e < k * 256 + (int)threadIdx.x) { first = false; break; }
-                sum += exp((double)ts[e] * a.inv_t - gr.shift);
-            }
-            if (!first) continue;
-            const Weight32 weight = {gr.best, per};
-            to[p] = fmaf(weight.of(widen<DT>(scores[w.row * a.in.ld + pos[k]])), gr.listed, -(float)(sum * gr.scale) * gr.unit);
-        }
-    };
+    GroupMarks<DT> marks;
     load(at);
-    load_list<DT>(a, at.row, pos);
-    for (int w = threadIdx.x; w < 3 * GROUP_WORDS; w += 256) listed[0][w] = 0;
+    marks.load(a, at.row);
+    for (int k = 0; k < 3; ++k) clear_marks(listed[k]);
     __syncthreads();
-    patch_group(at, g, listed[0], patch[0]);
+    marks.set(a, at.group, listed[0]);
     __syncthreads();
+    Weight32 weight((float)a.rows[at.row].best, per);
+    float other = a.rows[at.row].other;
+    int turn = 0;
     for (int64_t block = start; block < end; ++block) {
         const GroupWalk here = at;
-        const int turn = (int)((block - start) % 3), half = (int)(block - start) & 1;
-        const RowGrad now = g;
         float v[16];
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i].template values<false>(here.group * GROUP + (wave * 4 + i) * 256, a.in.n, v + 4 * i);
         at.step(a.groups);
+        const int next = turn == 2 ? 0 : turn + 1;
         if (block + 1 < end) {
             load(at);
-            if (at.row != here.row) {
-                load_list<DT>(a, at.row, pos);
-                g = a.rows[at.row];
-            }
-            patch_group(at, g, listed[(turn + 1) % 3], patch[half ^ 1]);
-            for (int w = threadIdx.x; w < GROUP_WORDS; w += 256) listed[(turn + 2) % 3][w] = 0;
+            if (at.row != here.row) marks.load(a, at.row);
+            marks.set(a, at.group, listed[next]);
+            clear_marks(listed[next == 2 ? 0 : next + 1]);
         }
-        const Weight32 weight = {now.best, per};
         auto* out = static_cast<typename Score<DT>::type*>(a.grad) + here.row * a.ld_grad;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int p = (wave * 4 + i) * 256 + lane * 4;
             const int64_t j = here.group * GROUP + p;
-            const uint32_t bits = listed[turn][p >> 5] >> (p & 31) & 15u;
             float y[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) y[q] = weight.of(v[4 * i + q]) * now.other;
-            if (bits) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) if (bits >> q & 1) y[q] = patch[half][p + q];
-            }
-            if (j < a.in.n) store4<DT>(out, j, a.in.n, y);
+            for (int q = 0; q < 4; ++q) y[q] = weight.of(v[4 * i + q]) * other;
+            if (j < a.in.n) store_unlisted<DT>(out, j, a.in.n, y, marks_of(listed[turn], p));
             __builtin_amdgcn_sched_barrier(0);
+        }
+        turn = next;
+        if (block + 1 < end && at.row != here.row) {
+            weight = Weight32((float)a.rows[at.row].best, per);
+            other = a.rows[at.row].other;
         }
         __syncthreads();
     }

@@ -227,8 +227,8 @@ __device__ __forceinline__ float score_below(float s) {
 
 // Sums and maxima of a wave by moves within rows of 16 lanes and from row to row: no LDS on the way.
 template <int CTRL, int ROWS> __device__ __forceinline__ double moved64(double v) {  // lanes without a source: 0
-    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, ROWS, 0xf, false);
-    const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, ROWS, 0xf, false);
+    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, ROWS, 0xf, ROWS == 0xf);
+    const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, ROWS, 0xf, ROWS == 0xf);
     return __hiloint2double(hi, lo);
 }
 constexpr int ROW_SHR = 0x110, BCAST_15 = 0x142, BCAST_31 = 0x143;
