@@ -154,7 +154,7 @@ __device__ __forceinline__ void store_unlisted(typename Score<DT>::type* row, in
 }
 
 template <int DT, int WAVES, int TPW, bool STEP>
-__global__ __launch_bounds__(WAVES * 64) void k_distill(DistillArgs a) {
+__global__ __launch_bounds__(WAVES * 64, WAVES == 16 && TPW == 4 ? 8 : 1) void k_distill(DistillArgs a) {
     constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64, N = TPW * 4;
     __shared__ uint32_t listed[CAP / 32];  // a bit per candidate
     __shared__ int32_t list_at[KGE_TOP_MAX];
