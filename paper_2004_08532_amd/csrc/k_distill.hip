@@ -154,12 +154,13 @@ __device__ __forceinline__ void store_unlisted(typename Score<DT>::type* row, in
 }
 
 template <int DT, int WAVES, int TPW, bool STEP>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 16 && TPW == 4 ? 8 : 1) void k_distill(DistillArgs a) {
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 6 : WAVES == 16 && TPW == 4 ? 8 : 1) void k_distill(DistillArgs a) {
     constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64, N = TPW * 4;
     __shared__ uint32_t listed[CAP / 32];  // a bit per candidate
     __shared__ int32_t list_at[KGE_TOP_MAX];
     __shared__ float maxima[2][WAVES];
     __shared__ double parts[4][WAVES];
+    __shared__ RowGrad shared_grad;
     __shared__ int twice;  // a candidate is listed more than once
     const int64_t row = flat_block();
     if (row >= a.in.rows) return;
@@ -233,27 +234,31 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 16 && TPW == 4 ? 8 : 1) void k
         __builtin_amdgcn_sched_barrier(0);  // (tile by tile: the 64-bit halves of all weights at once would not fit the registers)
     }
     forget<N>(v);
-    ListSums l = sum_list<DT, THREADS>(a, row, r, shift);
+    ListSums l = {0.0, 0.0};
     z = wave_sum64(z);
-    l.a = wave_sum64(l.a);
-    l.b = wave_sum64(l.b);
-    if (a.t.lse) z_listed = wave_sum64(z_listed);
-    if constexpr (WAVES > 1) {
-        if (lane == 0) { parts[0][wave] = z; parts[1][wave] = z_listed; parts[2][wave] = l.a; parts[3][wave] = l.b; }
-        __syncthreads();
-        z = z_listed = l.a = l.b = 0.0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) { z += parts[0][w]; z_listed += parts[1][w]; l.a += parts[2][w]; l.b += parts[3][w]; }
+    if (wave * 64 < a.t.m) {
+        l = sum_list<DT, THREADS>(a, row, r, shift);
+        l.a = wave_sum64(l.a);
+        l.b = wave_sum64(l.b);
     }
-    const double z_rest = z;
-    z += z_listed;
-    if (best == INFINITY) z = __longlong_as_double(0x7FF8000000000000ll);
-    if (threadIdx.x == 0) {
-        if (a.loss) a.loss[row] = (float)row_loss(a, weight.best, z, z_rest, l);
-        if constexpr (STEP) a.step.cpos[row] = 0.f;
+    if (__ballot(z_listed != 0.0)) z_listed = wave_sum64(z_listed);
+    if (lane == 0) { parts[0][wave] = z; parts[1][wave] = z_listed; parts[2][wave] = l.a; parts[3][wave] = l.b; }
+    __syncthreads();
+    if (wave == 0) {  // (one wave for all: the divisions and logarithms of a row are as much work as a tile)
+        double sum[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum[k] = wave_sum64(lane < WAVES ? parts[k][lane] : 0.0);
+        const double z_rest = sum[0], all = best == INFINITY ? __longlong_as_double(0x7FF8000000000000ll) : sum[0] + sum[1];
+        l = {sum[2], sum[3]};
+        if (lane == 0) {
+            if (a.loss) a.loss[row] = (float)row_loss(a, weight.best, all, z_rest, l);
+            if constexpr (STEP) a.step.cpos[row] = 0.f;
+            shared_grad = row_grad(a, weight.best, all, z_rest, l);
+        }
     }
     if (!a.grad) return;
-    const RowGrad g = row_grad(a, weight.best, z, z_rest, l);
+    __syncthreads();
+    const RowGrad g = shared_grad;
     auto* out = static_cast<typename Score<DT>::type*>(a.grad) + row * a.ld_grad;
     auto shape = [&](float x, float raw) {  // a gradient as the backward products of a step want it
         if constexpr (STEP) {
@@ -585,6 +590,7 @@ void launch_rows(kge_ctx* c, const DistillArgs& a, hipStream_t st) {
     if (n <= 256) go(k_distill<DT, 1, 1, STEP>, 64);
     else if (n <= 1024) go(k_distill<DT, 4, 1, STEP>, 256);
     else if (n <= 4096) go(k_distill<DT, 4, 4, STEP>, 256);
+    else if (n <= 16384 && a.in.rows > 512) go(k_distill<DT, 8, 8, STEP>, 512);
     else if (n <= 16384) go(k_distill<DT, 16, 4, STEP>, 1024);
     else go(k_distill<DT, 16, 8, STEP>, 1024);
 }

@@ -360,7 +360,7 @@ __device__ __forceinline__ Kept cut_by_weight(float v[TPW * 4], const L& low, fl
 enum { CUT_MIN, CUT_WEIGHT, CUT_LIST };  // min-p alone; top-p and min-p; top-k and what follows it
 
 template <int DT, int WAVES, int TPW, int CUT>
-__global__ __launch_bounds__(WAVES * 64) void k_draw_rows(DrawArgs a) {
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 6 : 1) void k_draw_rows(DrawArgs a) {
     constexpr int THREADS = WAVES * 64, N = TPW * 4, TILES = WAVES * TPW;
     __shared__ float maxima[WAVES];
     const int64_t row = flat_block();
@@ -783,6 +783,7 @@ void launch_rows(const DrawArgs& a, hipStream_t st) {
     if (n <= 256) k_draw_rows<DT, 1, 1, CUT><<<grid, 64, 0, st>>>(a);
     else if (n <= 1024) k_draw_rows<DT, 4, 1, CUT><<<grid, 256, 0, st>>>(a);
     else if (n <= 4096) k_draw_rows<DT, 4, 4, CUT><<<grid, 256, 0, st>>>(a);
+    else if (n <= 16384 && a.in.rows > 512) k_draw_rows<DT, 8, 8, CUT><<<grid, 512, 0, st>>>(a);
     else if (n <= 16384) k_draw_rows<DT, 16, 4, CUT><<<grid, 1024, 0, st>>>(a);
     else k_draw_rows<DT, 16, 8, CUT><<<grid, 1024, 0, st>>>(a);
 }

@@ -34,7 +34,7 @@ __device__ __forceinline__ float lse_of(double best, double sum, double inv_t) {
 }
 
 template <int DT, int WAVES, int TPW>
-__global__ __launch_bounds__(WAVES * 64) void k_top_rows(TopArgs a) {
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 8 : 1) void k_top_rows(TopArgs a) {
     constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64;
     __shared__ BestList<WAVES, TPW> s;
     __shared__ double sums[WAVES];
@@ -52,8 +52,15 @@ __global__ __launch_bounds__(WAVES * 64) void k_top_rows(TopArgs a) {
         if (!empty) {
             const Scale scale(a.inv_t);
             const Weights w(best, scale);
+            if (best == INFINITY) {
+                z = 1.0;
+            } else {
 #pragma unroll
-            for (int q = 0; q < TPW * 4; ++q) z += w.of(v[q]);
+                for (int q = 0; q < TPW * 4; ++q) {
+                    z += w.loose(v[q], v[q] >= w.floor);
+                    if (q % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
             z = block_sum64<WAVES>(z, sums);
         }
         if (threadIdx.x == 0) {
@@ -315,6 +322,7 @@ void launch_rows(const TopArgs& a, hipStream_t st) {
     else if (n <= 256) k_top_rows<DT, 1, 1><<<flat_grid(blocks), 64, 0, st>>>(a);
     else if (n <= 1024) k_top_rows<DT, 4, 1><<<flat_grid(blocks), 256, 0, st>>>(a);
     else if (n <= 4096) k_top_rows<DT, 4, 4><<<flat_grid(blocks), 256, 0, st>>>(a);
+    else if (n <= 16384 && blocks > 512) k_top_rows<DT, 8, 8><<<flat_grid(blocks), 512, 0, st>>>(a);
     else if (n <= 16384) k_top_rows<DT, 16, 4><<<flat_grid(blocks), 1024, 0, st>>>(a);
     else k_top_rows<DT, 16, 8><<<flat_grid(blocks), 1024, 0, st>>>(a);
 }
