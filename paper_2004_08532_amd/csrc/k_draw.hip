@@ -451,7 +451,7 @@ __global__ __launch_bounds__(256) void k_draw_lists(DrawArgs a, const uint64_t* 
 // ---------------------------------------------------------------------------------------------------------
 constexpr int LOG_BINS = 11, BINS = 1 << LOG_BINS;
 constexpr int ROUNDS = 4;  // bins of equal width, then 2^32 keys in three rounds
-constexpr int PART_GROUPS = 16, NOTES = 1024;  // groups per workgroup of k_draw_bins, scores that it can note
+constexpr int PART_GROUPS = 4, NOTES = 1024;  // groups per workgroup of k_draw_bins, scores that it can note
 
 struct RowCut {
     BinRule<LOG_BINS> rule;

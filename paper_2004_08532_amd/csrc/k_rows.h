@@ -441,6 +441,7 @@ __device__ __forceinline__ uint32_t select_equal(const float v[N], float t, cons
 // number of those that there are.
 template <int N, typename L>
 __device__ __forceinline__ void append_marked(const float v[N], uint32_t marked, const L& low, uint64_t* list, uint32_t room, uint32_t* n) {
+    static_assert(N <= 32, "a bit per score");
     if (!__ballot(marked != 0)) return;
     const uint32_t own = (uint32_t)__popc(marked), upto = wave_scan_u32(own);
     uint32_t at = 0;
