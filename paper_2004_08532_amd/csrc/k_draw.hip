@@ -173,13 +173,15 @@ template <int LOG_BINS> struct BinRule {
     static constexpr int BINS = 1 << LOG_BINS;
     uint32_t lo, hi;   // interval of keys
     int shift;         // keys per bin: 2^shift; negative: bins of equal width
-    float best, per;   // bins per unit of the score
+    float unit, best;  // scores are taken times this power of two, the best one already is
+    float per;         // bins per one of these
     float drop;        // exponents per bin
     int top;           // exponent at the interval's upper end
+    __device__ __forceinline__ float place(float s) const { return fmaf(s, -unit, best) * per; }  // (the sum is exact but for its last bit)
     __device__ __forceinline__ int bin(float s) const {
         if (shift < 0) {
-            const float x = s < best ? (best - s) * per : 0.f;
-            return x < (float)(BINS - 1) ? (int)x : BINS - 1;
+            const float x = place(s);  // (NaN: both are +inf)
+            return x < (float)(BINS - 1) ? (int)x : x >= 0.f ? BINS - 1 : 0;
         }
         return (int)((hi - order_key(s)) >> shift);
     }
@@ -192,10 +194,15 @@ template <int LOG_BINS> __device__ __forceinline__ BinRule<LOG_BINS> first_bins(
     constexpr int BINS = 1 << LOG_BINS;
     BinRule<LOG_BINS> r;
     r.lo = LOWEST_KEY; r.hi = order_key(best);
-    r.shift = -1; r.best = best;
-    const float range = fminf(best - worst, (float)fmin(40.0 / inv_t, 3e38));
-    r.per = range > 0.f ? (float)BINS / range : 0.f;
-    r.drop = r.per > 0.f ? (float)(inv_t * 1.4426950408889634 / (double)r.per) : 0.f;
+    r.shift = -1;
+    // The unit keeps differences finite and the bins per unit a normal number: 1 unless scores are further apart than the type's largest value, or
+    // those that matter are closer than 2^-60.  (Then either the best is below 2^-20, or all others are too far from it to matter.)
+    float range = fminf(best - worst, (float)fmin(40.0 / inv_t, 3.4e38));
+    r.unit = best - worst == INFINITY ? 0.5f : range < 0x1p-60f && fabsf(best) < 0x1p-20f ? 0x1p60f : 1.f;
+    r.best = best * r.unit;
+    range = fminf(fmaf(worst, -r.unit, r.best), (float)fmin(40.0 / inv_t * (double)r.unit, 3.4e38));
+    r.per = range > 0.f ? fminf((float)BINS * (1.f - 0x1p-12f) / range, 1e38f) : 0.f;  // (the lowest score is inside the last bin)
+    r.drop = r.per > 0.f ? (float)(inv_t * 1.4426950408889634 / ((double)r.per * (double)r.unit)) : 0.f;
     r.top = 0;
     return r;
 }

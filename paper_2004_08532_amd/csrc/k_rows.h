@@ -151,10 +151,10 @@ __device__ __forceinline__ int64_t entry_position(uint64_t e) { return (int64_t)
 // kernels that form a weight per score they are what bounds it beside the reads: 64 scores take a SIMD some 90 cycles.
 struct Scale {  // what all weights of a kernel have in common
     double per, c[9];  // log2(e) / T; coefficients
-    float far;         // a weight 2^-1000 lies that far below the best score
+    double far;        // a weight 2^-1000 lies that far below the best score
     __device__ __forceinline__ explicit Scale(double inv_t) : per(inv_t * 1.4426950408889634),
         c{0x1.62e42fefa39f7p-1, 0x1.ebfbdff8149f2p-3, 0x1.c6b08d7044119p-5, 0x1.3b2ab72b175eep-7, 0x1.5d87fe908f88ap-10, 0x1.43088e257f341p-13,
-          0x1.ffcb76789860fp-17, 0x1.63ef969a64d3cp-20, 0x1.b6571de2f2351p-24}, far((float)fmin(1000.0 / per, 3.4e38)) {
+          0x1.ffcb76789860fp-17, 0x1.63ef969a64d3cp-20, 0x1.b6571de2f2351p-24}, far(1000.0 / per) {
         // (in scalar registers: a coefficient in a vector register is copied for every step, the instruction adds to its own output)
 #pragma unroll
         for (int i = 0; i < 9; ++i) asm("" : "+s"(c[i]));
@@ -165,8 +165,8 @@ struct Weights {
     double best;
     float floor;  // scores below have a weight of 0: 2^-1000 and less, or that of no number between the floor and the best
     __device__ __forceinline__ Weights(float b, const Scale& s) : scale(s) {
-        const float f = b - s.far;
-        floor = fmaxf(fminf(b, fmaf(fabsf(f), 0x1p-22f, f)), -3.402823466e38f);  // (rounded up; b = +inf: above every number)
+        const double f = (double)b - s.far;
+        floor = fmaxf(fminf(b, (float)fma(fabs(f), 0x1p-22, f)), -3.402823466e38f);  // (rounded up; b = +inf: above every number)
         best = (double)fminf(b, 3.402823466e38f);
     }
     // (of a score at or above the floor; something else below it)

@@ -198,6 +198,28 @@ def test_sample_of_equal_and_extreme_scores(kge, n, setting):
     check_sample(kge, rows_of(torch.from_numpy(x).float()), u, **SETTINGS[setting])
 
 
+@pytest.mark.parametrize("top_p", [1e-7, 0.3, 0.9, 0.9999, 1.0 - 2.0 ** -23])
+@pytest.mark.parametrize("n", [700, 6000, 20_000, 33_001, 270_000])
+def test_where_top_p_ends(kge, n, top_p):
+    """Scores as they come, few different ones, one far above many equal ones, all but a few masked; differences below the normal numbers and
+    above the largest one."""
+    g = np.random.default_rng(n)
+    u = g.random((6, 6))
+    x = np.full((6, n), -math.inf)
+    x[0] = g.normal(0, 3, n)
+    x[1] = np.round(g.normal(0, 2, n))
+    x[2] = 0.125
+    x[3] = np.where(np.arange(n) == n // 3, 7.0, -2.5)
+    x[4, ::97] = g.normal(0, 1, x[4, ::97].size)
+    x[5] = np.where(g.random(n) < 0.5, 1.0, g.normal(1.0, 2.0 ** -9, n))
+    check_sample(kge, rows_of(torch.from_numpy(x).float()), u, top_p=top_p)
+    check_sample(kge, rows_of(torch.from_numpy(x).float(), torch.bfloat16), u, T=0.5, top_p=top_p, min_p=1e-4)
+    check_sample(kge, rows_of(torch.from_numpy(x).float()), u, T=1e-4, top_p=top_p)
+    # (weights from 1 to exp(-8.4) in steps of 2^-149; then to exp(-6.8), whose scores are further apart than any number)
+    check_sample(kge, rows_of(torch.from_numpy(2.0 ** -149 * g.integers(-3000, 3000, (6, n))).float()), u, T=1e-42, top_p=top_p)
+    check_sample(kge, rows_of(torch.from_numpy(3.4e38 * g.uniform(-1, 1, (6, n))).float()), u, T=1e38, top_p=top_p)
+
+
 def test_numbers_outside_of_the_unit_interval(kge):
     for n in (100, 2000, 50_000):
         x = normal(2, n, n)
