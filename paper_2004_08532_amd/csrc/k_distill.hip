@@ -14,7 +14,7 @@
 
 namespace {
 
-// What the gradients of a row have in common: grad_j = w_j * (listed or other) - p * unit, with w relative to `best`; p_e = exp(score / T - shift) * scale.
+// What the gradients of a row have in common: grad_j = w_j * (listed or other) - p * unit, with w relative to `best`; p_e = exp(Teacher::log_p) * scale.
 struct RowGrad {
     double best, scale;
     float listed, other, unit;
@@ -35,31 +35,22 @@ struct DistillArgs {
     RowGrad* rows;
 };
 
-__device__ __forceinline__ float larger(float a, float b) {  // NaN: the other (as fmaxf, without a step that quiets signalling ones)
-    float r;
-    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-    return r;
-}
 __device__ __forceinline__ float largest(float a, float b, float c) {  // NaN if one of them is
     float r;
     asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
 
+// The same for all lanes: in a scalar register.
+__device__ __forceinline__ float scalar(float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v))); }
+
 // Weights relative to `best`.  The argument of the exponential is formed in 64 bits and its fraction taken in 32, so the weight is off by
 // the roundings of exp2 alone, whatever the distance.  Masked: 0.
 struct Weight32 {
-    double best, per;  // per: log2(e) / T, or less where neighbouring numbers are so far apart that all weights but the best's are 0
-    float floor;       // a weight of 0, below the best
-    __device__ __forceinline__ Weight32(float b, double p) {
-        const float at = fabsf(b) < INFINITY ? b : 0.f;  // (no candidate)
-        best = (double)at;
-        per = fmin(p, 0x1p43 / fmax(fabs(best), 1e-300));
-        const float far = at - (float)fmin(1024.0 / per, 3e38);
-        floor = far < at ? far : score_below(at);
-    }
+    double best, per, far;  // per: log2(e) / T; 2^1024 times less than the best's: 0
+    __device__ __forceinline__ Weight32(float b, double p) : best(fabsf(b) < INFINITY ? (double)b : 0.0 /* no candidate */), per(p), far(-1024.0 / p) {}
     __device__ __forceinline__ float of(float s) const {
-        const double d = (double)larger(s, floor) - best, shifted = fma(d, per, 0x1.8p52), f = fma(d, per, -(shifted - 0x1.8p52));
+        const double d = fmax((double)s - best, far), shifted = fma(d, per, 0x1.8p52), f = fma(d, per, -(shifted - 0x1.8p52));
         return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)f), __double2loint(shifted));
     }
 };
@@ -79,19 +70,28 @@ template <int DT> __device__ __forceinline__ int64_t list_position(const Distill
     return id >= 0 && id < n && a.t.scores[row * a.t.m + e] != -INFINITY ? id : -1;
 }
 
-struct ListSums { double a, b; };  // sum of p before it is scaled, sum of p * (log p - s / T)
+// log p of an entry before p is scaled: relative to the teacher's log-sum-exp, or to the largest score of the list.
+struct Teacher {
+    const float* scores;
+    double inv_t, best, lse;
+    __device__ __forceinline__ Teacher(const DistillArgs& a, int64_t row, float most)
+        : scores(a.t.scores + row * a.t.m), inv_t(a.inv_t), best(a.t.lse || !(most > -INFINITY) ? 0.0 : (double)most), lse(a.t.lse ? (double)a.t.lse[row] : 0.0) {}
+    __device__ __forceinline__ double log_p(int e) const { return ((double)scores[e] - best) * inv_t - lse; }
+};
 
-// A thread's part of the list's sums, with log p = score / T - shift.
+struct ListSums { double a, b; };  // sum of p before it is scaled, sum of p * (log p - (s - best) / T)
+
+// A thread's part of the list's sums.
 template <int DT, int THREADS>
-__device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, const RowAt<DT>& r, double shift) {
+__device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, const RowAt<DT>& r, const Teacher& teacher, double best) {
     ListSums l = {0.0, 0.0};
 #pragma unroll 1
     for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
         const int64_t id = list_position<DT>(a, row, e, r.n);
         if (id < 0) continue;
-        const double lp = (double)a.t.scores[row * a.t.m + e] * a.inv_t - shift, p = exp(lp);
+        const double lp = teacher.log_p(e), p = exp(lp);
         l.a += p;
-        if (p > 0.0 || p != p) l.b += p * (lp - (double)r.at(id) * a.inv_t);
+        if (p > 0.0 || p != p) l.b += p * (lp - ((double)r.at(id) - best) * a.inv_t);
     }
     return l;
 }
@@ -115,7 +115,7 @@ __device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, double best, d
     }
     return g;
 }
-__device__ __forceinline__ double row_loss(const DistillArgs& a, double best, double z, double z_rest, const ListSums& l) {
+__device__ __forceinline__ double row_loss(const DistillArgs& a, double z, double z_rest, const ListSums& l) {
     double mass = l.a, cross = l.b, rest = 0.0;
     if (a.t.lse) {
         rest = z_rest > 0.0 ? fmax(1.0 - mass, 0.0) : 0.0;
@@ -124,14 +124,9 @@ __device__ __forceinline__ double row_loss(const DistillArgs& a, double best, do
         mass /= mass;
     }
     if (z == 0.0 || mass + rest == 0.0) return 0.0;
-    double loss = cross + mass * (best * a.inv_t + log(z));
+    double loss = cross + mass * log(z);
     if (rest > 0.0) loss += rest * log(rest * z / z_rest);
     return loss * (double)a.loss_scale;
-}
-
-// The list's shift: the teacher's log-sum-exp, or the largest score of the list.
-__device__ __forceinline__ double list_shift(const DistillArgs& a, int64_t row, float most) {
-    return a.t.lse ? (double)a.t.lse[row] : most > -INFINITY ? (double)most * a.inv_t : 0.0;
 }
 
 // Gradients j .. j + 3 of a row of n, but those of candidates whose bit is set.
@@ -209,7 +204,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 6 : WAVES == 16 && TPW == 
         best = fmaxf(best, maxima[0][w]);
         list_best = fmaxf(list_best, maxima[1][w]);
     }
-    const double shift = list_shift(a, row, list_best);
+    best = scalar(best);
+    const Teacher teacher(a, row, scalar(list_best));
     const Weight32 weight(best, a.inv_t * 1.4426950408889634);
     // sums of the weights: with a rest, of the candidates that are not listed, and of the few others
     double z = 0.0, z_listed = 0.0;
@@ -237,7 +233,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 6 : WAVES == 16 && TPW == 
     ListSums l = {0.0, 0.0};
     z = wave_sum64(z);
     if (wave * 64 < a.t.m) {
-        l = sum_list<DT, THREADS>(a, row, r, shift);
+        l = sum_list<DT, THREADS>(a, row, r, teacher, weight.best);
         l.a = wave_sum64(l.a);
         l.b = wave_sum64(l.b);
     }
@@ -251,7 +247,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 6 : WAVES == 16 && TPW == 
         const double z_rest = sum[0], all = best == INFINITY ? __longlong_as_double(0x7FF8000000000000ll) : sum[0] + sum[1];
         l = {sum[2], sum[3]};
         if (lane == 0) {
-            if (a.loss) a.loss[row] = (float)row_loss(a, weight.best, all, z_rest, l);
+            if (a.loss) a.loss[row] = (float)row_loss(a, all, z_rest, l);
             if constexpr (STEP) a.step.cpos[row] = 0.f;
             shared_grad = row_grad(a, weight.best, all, z_rest, l);
         }
@@ -273,7 +269,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 6 : WAVES == 16 && TPW == 
     for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
         const int at = list_at[e];
         if (at < 0) continue;
-        auto p_of = [&](int x) { return exp((double)a.t.scores[row * a.t.m + x] * a.inv_t - shift) * g.scale; };
+        auto p_of = [&](int x) { return exp(teacher.log_p(x)) * g.scale; };
         double p = p_of(e);
         bool stands = true;
         if (twice) {
@@ -491,14 +487,14 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     }
     z = block_sum64<4>(z, slot);
     z_listed = block_sum64<4>(z_listed, slot);
-    const double shift = list_shift(a, row, list_best), z_rest = z;
+    const Teacher teacher(a, row, list_best);
+    const double b = best > -INFINITY ? (double)best : 0.0, z_rest = z;
     z += z_listed;
-    ListSums l = sum_list<DT, 256>(a, row, r, shift);
+    ListSums l = sum_list<DT, 256>(a, row, r, teacher, b);
     l.a = block_sum64<4>(l.a, slot);
     l.b = block_sum64<4>(l.b, slot);
     if (threadIdx.x == 0) {
-        const double b = best > -INFINITY ? (double)best : 0.0;
-        if (a.loss) a.loss[row] = (float)row_loss(a, b, z, z_rest, l);
+        if (a.loss) a.loss[row] = (float)row_loss(a, z, z_rest, l);
         a.rows[row] = shared_grad = row_grad(a, b, z, z_rest, l);
     }
     __syncthreads();
@@ -509,11 +505,11 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     for (int e = threadIdx.x; e < a.t.m; e += 256) {
         const uint32_t x = entry_slot[e];
         if (x == 0xFFFF || first[x] != (uint32_t)e) continue;
-        double sum = exp((double)a.t.scores[row * a.t.m + e] * a.inv_t - shift);
+        double sum = exp(teacher.log_p(e));
         uint32_t left = times[x] - 1;
         for (int y = e + 1; left; ++y) {
             if (entry_slot[y] != x) continue;
-            sum += exp((double)a.t.scores[row * a.t.m + y] * a.inv_t - shift);
+            sum += exp(teacher.log_p(y));
             --left;
         }
         out[key[x]] = narrow<DT>(fmaf(weight.of(r.at(key[x])), g.listed, -(float)(sum * g.scale) * g.unit));

@@ -346,6 +346,30 @@ def test_distill_in_place_with_masks_and_repeated_entries(kge, n, m, rest):
     check_distill(kge, rows_of(x, pad=5), ids, t, lse if rest else None, grad=False)
 
 
+@pytest.mark.parametrize("n", [60, 1000, 20_000, 50_000])
+def test_distill_of_extreme_scores_and_temperatures(kge, n):
+    """Rows of the type's lowest value, alone and beside masked ones; scores as far apart as the type allows and 2^-83 apart, T with them."""
+    low, g = torch.finfo(torch.float32).min, np.random.default_rng(n)
+    x = np.full((5, n), low)
+    x[1, ::2] = -math.inf
+    x[2, 1::3] = g.normal(0, 3, x[2, 1::3].size)
+    x[3] = 1e30 * (1 + 2.0 ** -23 * g.integers(-3, 4, n))
+    x[4] = -x[3]
+    ids = np.stack([g.permutation(n)[:20] for _ in range(5)])
+    ids[1] = ids[1] // 2 * 2 + 1 - 2 * (ids[1] >= n - n % 2)  # not masked
+    t = g.normal(0, 1, ids.shape)
+    check_distill(kge, rows_of(torch.from_numpy(x).float()), ids, t)
+    for size, T in ((3.4e38, 1e18), (2.0 ** -60, 2.0 ** -60)):
+        x = size * np.floor(g.uniform(-1, 1, (5, n)) * 2.0 ** 23) * 2.0 ** -23
+        x[0, ::2] = -math.inf
+        t = size * g.uniform(-1, 1, ids.shape)
+        if size < 1:
+            ids[0] = ids[1]
+            check_distill(kge, rows_of(torch.from_numpy(x).float()), ids, t, T=T)
+        else:  # far beyond each other: the best has all of the mass
+            check_distill(kge, rows_of(torch.from_numpy(x).float()), np.argsort(-x, axis=1)[:, :20], np.sort(t, axis=1)[:, ::-1].copy(), T=T)
+
+
 def test_a_rest_that_has_nowhere_to_go(kge):
     for n in (8, 300, 1024):
         x = normal(2, n, n)
