@@ -288,7 +288,104 @@ template <int WAVES, int TPW> struct CutScratch {
     uint64_t sorted[256];
     double sums[ROOM], part[WAVES + 1];
     uint32_t slots[2 * WAVES], rank[256], found[2], count;
+    uint64_t more[WAVES * TPW];
 };
+
+// The bins in which the weights of a row reach top-p, as an interval of keys, from weights in 32 bits: a score's is that at its bin's upper end
+// times a whole number of 32768ths, by two terms of the exponential (a bin has at most 0.04 T).  Sums of these are off by less than a
+// 16,000th: 2^-16 from rounding, 1e-5 from the third term, 5e-6 from a score's place, 5e-6 from the bins' exponents; and 2^15 scores
+// 40 T below the best, which are left out, have 2e-13.  A sum reaches top_p of the whole where what is behind it is at most the rest of 1: the closer
+// of the two bounds is taken.
+constexpr double ENCLOSE = 1.0 / 16000.0, LEFT_OUT = 2e-13;
+template <int WAVES, int TPW>
+__device__ __forceinline__ void enclose(const float v[TPW * 4], float best, float worst, double inv_t, double top_p, CutScratch<WAVES, TPW>& s, uint32_t& lo, uint32_t& hi) {
+    constexpr int THREADS = WAVES * 64, LOG_BINS = CutScratch<WAVES, TPW>::LOG_BINS, BINS = 1 << LOG_BINS, PER = BINS / THREADS;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const BinRule<LOG_BINS> r = first_bins<LOG_BINS>(best, worst, inv_t);
+    uint32_t* bins = reinterpret_cast<uint32_t*>(s.bins);
+    for (int b = threadIdx.x; b < BINS; b += THREADS) bins[b] = 0;
+    if (threadIdx.x < 2) s.found[threadIdx.x] = BINS;
+    __syncthreads();
+    const bool infinite = best == INFINITY;
+    const float top = infinite ? 0.f : r.best, y = r.drop * 0.69314718f, c1 = -y * 32768.f, c2 = 0.5f * y * y * 32768.f;
+#pragma unroll
+    for (int q = 0; q < TPW * 4; ++q) {
+        const float x = infinite ? (v[q] == INFINITY ? 0.f : -INFINITY) : v[q], at = fmaf(x, -r.unit, top) * r.per, part = __builtin_amdgcn_fractf(at);
+        const uint32_t number = (uint32_t)fmaf(part, fmaf(part, c2, c1), 32768.5f);
+        const bool counts = at < (float)BINS;  // neither masked nor too far; the others add 0, at places that do not collide
+        atomicAdd(&bins[counts ? (int)at : lane], counts ? number : 0u);
+        if (q % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();
+    double x[PER], sum = 0.0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        const float e = (float)(threadIdx.x * PER + q) * r.drop, whole = floorf(e);
+        x[q] = ldexp((double)bins[threadIdx.x * PER + q] * (double)__builtin_amdgcn_exp2f(whole - e), -(int)whole);
+        sum += x[q];
+    }
+    const double incl = wave_scan64(sum, lane);
+    if (lane == 63) s.part[wave] = incl;
+    __syncthreads();
+    double run = incl - sum, all = 0.0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) run += s.part[w];
+        all += s.part[w];
+    }
+    const double reach = top_p * all, behind = (1.0 - top_p) * all, off = 2.0 * ENCLOSE, left = LEFT_OUT * all;
+    int first = BINS, last = BINS;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        run += x[q];
+        if (!(x[q] > 0.0)) continue;
+        const double rest = all - run;
+        const int b = threadIdx.x * PER + q;
+        if (first == BINS && run >= reach * (1.0 - off) && rest <= behind * (1.0 + off) + left) first = b;
+        if (last == BINS && (run >= reach * (1.0 + off) || rest <= behind * (1.0 - off) - left)) last = b;
+    }
+    if (first < BINS) atomicMin(&s.found[0], (uint32_t)first);
+    if (last < BINS) atomicMin(&s.found[1], (uint32_t)last);
+    __syncthreads();
+    if (wave == 0) {  // (one wave for all; a larger key never has a larger bin; no bin: all that is left)
+        const int from = min((int)s.found[0], BINS - 1), to = min((int)s.found[1], BINS - 1);
+        const uint32_t low = order_key(worst), high = order_key(best);
+        lo = lowest_key(low, high, [&](uint32_t key) { return r.bin(key_score(key)) <= to; });
+        hi = from > 0 ? lowest_key(low, high, [&](uint32_t key) { return r.bin(key_score(key)) < from; }) - 1 : high;
+        if (lane == 0) { s.slots[0] = lo; s.slots[1] = hi; s.count = 0; }
+    }
+    for (int t = threadIdx.x; t < WAVES * TPW; t += THREADS) s.more[t] = 0;
+    __syncthreads();
+    lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)s.slots[0]);
+    hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)s.slots[1]);
+}
+
+// The first entry of a list in LDS at which `above` and the sum of the weights reach the target, and what that keeps.
+template <int WAVES, int TPW>
+__device__ __forceinline__ Kept cut_list(int count, double target, double above, const Weights& w, CutScratch<WAVES, TPW>& s) {
+    constexpr int THREADS = WAVES * 64;
+    const int lane = threadIdx.x & 63;
+    const uint64_t* list = order_list<THREADS>(s.bins, s.sorted, s.rank, count);
+    for (int e = threadIdx.x; e < count; e += THREADS) s.sums[e] = w.of(key_score((uint32_t)(list[e] >> 32)));
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        double carry = above;
+        int cut = count - 1;
+        for (int e0 = 0; e0 < count; e0 += 64) {
+            const double x = carry + wave_scan64(e0 + lane < count ? s.sums[e0 + lane] : 0.0, lane);
+            const uint64_t there = __ballot(e0 + lane < count && x >= target);
+            if (there) { cut = e0 + __ffsll((unsigned long long)there) - 1; break; }
+            carry = lane64(x, 63);
+        }
+        if (lane == 0) {  // (no other score like it behind the cut: all of them are kept)
+            s.found[0] = (uint32_t)(list[cut] >> 32);
+            s.found[1] = cut + 1 < count && (uint32_t)(list[cut + 1] >> 32) == s.found[0] ? (uint32_t)list[cut] : 0u;
+        }
+    }
+    __syncthreads();
+    const float t = key_score(s.found[0]);
+    return {s.found[1] == 0 ? score_below(t) : t, t, s.found[1], 0u};
+}
 
 // What top-p keeps of a workgroup's scores.
 template <int WAVES, int TPW, typename L>
@@ -296,7 +393,6 @@ __device__ __forceinline__ Kept cut_by_weight(float v[TPW * 4], const L& low, fl
                                               CutScratch<WAVES, TPW>& s) {
     constexpr int N = TPW * 4, THREADS = WAVES * 64, BITS = 46;  // 2^15 scores of up to 2^47.5
     constexpr int ROOM = CutScratch<WAVES, TPW>::ROOM, LOG_BINS = CutScratch<WAVES, TPW>::LOG_BINS, BINS = 1 << LOG_BINS;
-    const int lane = threadIdx.x & 63;
     BinRule<LOG_BINS> r = first_bins<LOG_BINS>(best, worst, inv_t);
     double target = 0.0, above = 0.0;
     int count = 0;
@@ -340,34 +436,79 @@ __device__ __forceinline__ Kept cut_by_weight(float v[TPW * 4], const L& low, fl
     for (int q = 0; q < N; ++q) marked |= (uint32_t)(v[q] >= t0 && v[q] <= t1) << q;
     append_marked<N>(v, marked, low, s.bins, ROOM, &s.count);
     __syncthreads();
-    const uint64_t* list = order_list<THREADS>(s.bins, s.sorted, s.rank, count);
-    for (int e = threadIdx.x; e < count; e += THREADS) s.sums[e] = w.of(key_score((uint32_t)(list[e] >> 32)));
+    return cut_list(count, target, above, w, s);
+}
+
+// The cut and the tiles' sums of what it keeps in one pass with weights in 64 bits, once few scores are left between those that are surely kept and
+// those that are not; false where too many are left (equal scores, top-p close to 1).
+template <int DT, int WAVES, int TPW, typename L>
+__device__ __forceinline__ bool cut_enclosed(float v[TPW * 4], const L& low, float best, float worst, const Weights& w, const DrawArgs& a,
+                                             CutScratch<WAVES, TPW>& s, double* sums, Kept& kept) {
+    constexpr int N = TPW * 4, THREADS = WAVES * 64, TILES = WAVES * TPW, BITS = 46;
+    constexpr int ROOM = CutScratch<WAVES, TPW>::ROOM;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t lo, hi;
+    enclose<WAVES, TPW>(v, best, worst, a.inv_t, a.top_p, s, lo, hi);
+    forget<N>(v);
+    const float from = key_score(lo), to = key_score(hi);
+    kept = {to, __uint_as_float(0x7FC00000u), 0u, 0u};
+    keep_from_min_p(kept, w, best, a.min_p);
+    const bool refine = !(kept.over > to);  // (else min-p leaves less than top-p)
+    uint32_t marked = 0;
+    double all = 0.0;
+#pragma unroll
+    for (int i = 0; i < TPW; i += 4) {
+        double z[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            z[k] = 0.0;
+            double sum = 0.0;
+#pragma unroll
+            for (int q = 4 * (i + k); q < 4 * (i + k) + 4; ++q) {
+                const double y = best == INFINITY ? (v[q] == INFINITY ? 1.0 : 0.0) : w.loose(v[q], v[q] >= w.floor);
+                sum += y;
+                z[k] += __hiloint2double(v[q] > kept.over ? __double2hiint(y) : 0, __double2loint(y));
+                marked |= (uint32_t)(v[q] >= from && v[q] <= to) << q;
+            }
+            all += sum;
+        }
+        const double sum = Weights::some_weight(sum_four(z));
+        if ((lane & 15) == 15) sums[(i + tile_of_row(lane >> 4)) * WAVES + wave] = sum;
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    all = wave_sum64(all);
+    if (lane == 0) s.part[wave] = all;
+    if (!refine) { __syncthreads(); return true; }
+    append_marked<N>(v, marked, low, s.bins, ROOM, &s.count);
     __syncthreads();
-    if (threadIdx.x < 64) {  // the first entry at which the sum reaches the target
-        double carry = above;
-        int cut = count - 1;
-        for (int e0 = 0; e0 < count; e0 += 64) {
-            const double x = carry + wave_scan64(e0 + lane < count ? s.sums[e0 + lane] : 0.0, lane);
-            const uint64_t there = __ballot(e0 + lane < count && x >= target);
-            if (there) { cut = e0 + __ffsll((unsigned long long)there) - 1; break; }
-            carry = lane64(x, 63);
-        }
-        if (lane == 0) {  // (no other score like it behind the cut: all of them are kept)
-            s.found[0] = (uint32_t)(list[cut] >> 32);
-            s.found[1] = cut + 1 < count && (uint32_t)(list[cut + 1] >> 32) == s.found[0] ? (uint32_t)list[cut] : 0u;
-        }
+    const int count = (int)s.count;
+    if (count > ROOM || count == 0) return false;
+    all = wave_sum64(lane < WAVES ? s.part[lane] : 0.0);
+    double above = lane < TILES ? sums[lane] : 0.0;
+#pragma unroll
+    for (int t = 64; t < TILES; t += 64) above += sums[t + lane];
+    above = wave_sum64(above);
+    kept = cut_list<WAVES, TPW>(count, a.top_p * all, above, w, s);
+    keep_from_min_p(kept, w, best, a.min_p);
+    int top;
+    double p;
+    w.split(to, p, top);
+    const uint64_t* list = count <= 256 ? s.sorted : s.bins;
+    for (int e = threadIdx.x; e < count; e += THREADS) {
+        const float x = key_score((uint32_t)(list[e] >> 32));
+        const uint32_t position = ~(uint32_t)list[e];
+        if (x > kept.over || (x == kept.t && (uint32_t)list[e] >= kept.least))
+            atomicAdd(reinterpret_cast<unsigned long long*>(&s.more[position / 256]), (unsigned long long)whole_weight(w, x, top, BITS));
     }
     __syncthreads();
-    kept.t = kept.over = key_score(s.found[0]);
-    kept.least = s.found[1];
-    if (kept.least == 0) kept.over = score_below(kept.t);
-    return kept;
+    for (int t = threadIdx.x; t < TILES; t += THREADS) sums[t] += ldexp((double)s.more[t], top - BITS);
+    return true;
 }
 
 enum { CUT_MIN, CUT_WEIGHT, CUT_LIST };  // min-p alone; top-p and min-p; top-k and what follows it
 
 template <int DT, int WAVES, int TPW, int CUT>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 6 : 1) void k_draw_rows(DrawArgs a) {
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? (CUT == CUT_WEIGHT ? 4 : 6) : 1) void k_draw_rows(DrawArgs a) {
     constexpr int THREADS = WAVES * 64, N = TPW * 4, TILES = WAVES * TPW;
     __shared__ float maxima[WAVES];
     const int64_t row = flat_block();
@@ -398,6 +539,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 6 : 1) void k_draw_rows(Dr
 #pragma unroll
             for (int q = 0; q < N; ++q) worst = v[q] > -INFINITY ? fminf(worst, v[q]) : worst;
             worst = -block_max<WAVES>(-worst, maxima);
+            if constexpr (TPW % 4 == 0) {
+                if (cut_enclosed<DT, WAVES, TPW>(v, low, best, worst, weights, a, scratch, sums, kept)) {
+                    draw_from_tiles<DT, WAVES, TILES>(a, row, s, TILES, sums, nullptr, kept, weights);
+                    return;
+                }
+            }
             kept = cut_by_weight<WAVES, TPW>(v, low, best, worst, weights, a.inv_t, a.top_p, scratch);
             forget<N>(v);
         }
