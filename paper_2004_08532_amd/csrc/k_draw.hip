@@ -298,7 +298,7 @@ template <int WAVES, int TPW> struct CutScratch {
 // of the two bounds is taken.
 constexpr double ENCLOSE = 1.0 / 16000.0, LEFT_OUT = 2e-13;
 template <int WAVES, int TPW>
-__device__ __forceinline__ void enclose(const float v[TPW * 4], float best, float worst, double inv_t, double top_p, CutScratch<WAVES, TPW>& s, uint32_t& lo, uint32_t& hi) {
+__device__ __forceinline__ void enclose(const float v[TPW * 4], int64_t n, float best, float worst, double inv_t, double top_p, CutScratch<WAVES, TPW>& s, uint32_t& lo, uint32_t& hi) {
     constexpr int THREADS = WAVES * 64, LOG_BINS = CutScratch<WAVES, TPW>::LOG_BINS, BINS = 1 << LOG_BINS, PER = BINS / THREADS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const BinRule<LOG_BINS> r = first_bins<LOG_BINS>(best, worst, inv_t);
@@ -310,6 +310,7 @@ __device__ __forceinline__ void enclose(const float v[TPW * 4], float best, floa
     const float top = infinite ? 0.f : r.best, y = r.drop * 0.69314718f, c1 = -y * 32768.f, c2 = 0.5f * y * y * 32768.f;
 #pragma unroll
     for (int q = 0; q < TPW * 4; ++q) {
+        if (q % 16 == 0 && q > 0 && q * WAVES * 64 >= n) break;
         const float x = infinite ? (v[q] == INFINITY ? 0.f : -INFINITY) : v[q], at = fmaf(x, -r.unit, top) * r.per, part = __builtin_amdgcn_fractf(at);
         const uint32_t number = (uint32_t)fmaf(part, fmaf(part, c2, c1), 32768.5f);
         const bool counts = at < (float)BINS;  // neither masked nor too far; the others add 0, at places that do not collide
@@ -448,7 +449,7 @@ __device__ __forceinline__ bool cut_enclosed(float v[TPW * 4], const L& low, flo
     constexpr int ROOM = CutScratch<WAVES, TPW>::ROOM;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t lo, hi;
-    enclose<WAVES, TPW>(v, best, worst, a.inv_t, a.top_p, s, lo, hi);
+    enclose<WAVES, TPW>(v, a.in.n, best, worst, a.inv_t, a.top_p, s, lo, hi);
     forget<N>(v);
     const float from = key_score(lo), to = key_score(hi);
     kept = {to, __uint_as_float(0x7FC00000u), 0u, 0u};
@@ -458,6 +459,10 @@ __device__ __forceinline__ bool cut_enclosed(float v[TPW * 4], const L& low, flo
     double all = 0.0;
 #pragma unroll
     for (int i = 0; i < TPW; i += 4) {
+        if (i > 0 && i * WAVES * 256 >= a.in.n) {
+            if ((lane & 15) == 15) sums[(i + tile_of_row(lane >> 4)) * WAVES + wave] = 0.0;
+            continue;
+        }
         double z[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -493,7 +498,7 @@ __device__ __forceinline__ bool cut_enclosed(float v[TPW * 4], const L& low, flo
     int top;
     double p;
     w.split(to, p, top);
-    const uint64_t* list = count <= 256 ? s.sorted : s.bins;
+    const uint64_t* list = by_counting<THREADS>(count) ? s.sorted : s.bins;
     for (int e = threadIdx.x; e < count; e += THREADS) {
         const float x = key_score((uint32_t)(list[e] >> 32));
         const uint32_t position = ~(uint32_t)list[e];
@@ -539,6 +544,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? (CUT == CUT_WEIGHT ? 4 : 6
 #pragma unroll
             for (int q = 0; q < N; ++q) worst = v[q] > -INFINITY ? fminf(worst, v[q]) : worst;
             worst = -block_max<WAVES>(-worst, maxima);
+            // us, bins of 64-bit weights alone -> this first, 1 / 1024 rows: of 2000 16.9 -> 16.2 / 26.2 -> 22.8, of 15,000 26 -> 22 / 72 -> 60, of 30,000
+            // 39 -> 32 / 163 -> 138; about equal whatever top_p and the temperature.  (Rows of up to 1024 have 4 scores per thread: no pass to save.)
             if constexpr (TPW % 4 == 0) {
                 if (cut_enclosed<DT, WAVES, TPW>(v, low, best, worst, weights, a, scratch, sums, kept)) {
                     draw_from_tiles<DT, WAVES, TILES>(a, row, s, TILES, sums, nullptr, kept, weights);
@@ -553,7 +560,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? (CUT == CUT_WEIGHT ? 4 : 6
         if constexpr (TPW % 4 == 0) {
 #pragma unroll
             for (int i = 0; i < TPW; i += 4) {
-                const double z = sum_of_tiles(v + 4 * i, weights, kept.over);
+                const double z = i * WAVES * 256 < a.in.n ? sum_of_tiles(v + 4 * i, weights, kept.over) : 0.0;
                 if ((lane & 15) == 15) sums[(i + tile_of_row(lane >> 4)) * WAVES + wave] = z;
             }
         } else {
@@ -937,8 +944,9 @@ void launch_rows(const DrawArgs& a, hipStream_t st) {
     if (n <= 256) k_draw_rows<DT, 1, 1, CUT><<<grid, 64, 0, st>>>(a);
     else if (n <= 1024) k_draw_rows<DT, 4, 1, CUT><<<grid, 256, 0, st>>>(a);
     else if (n <= 4096) k_draw_rows<DT, 4, 4, CUT><<<grid, 256, 0, st>>>(a);
-    else if (n <= 16384 && a.in.rows > 512) k_draw_rows<DT, 8, 8, CUT><<<grid, 512, 0, st>>>(a);
-    else if (n <= 16384) k_draw_rows<DT, 16, 4, CUT><<<grid, 1024, 0, st>>>(a);
+    // (1024 threads of half as many scores are as fast up to 256 rows.  us, 512 / 4096 rows of 15,000, 1024 -> 512 threads: top-p 46 -> 32 / 360 -> 221,
+    // min-p 17.3 -> 12.7 / 122 -> 73, top-k 50 22.6 -> 13.8 / 165 -> 72)
+    else if (n <= 16384) k_draw_rows<DT, 8, 8, CUT><<<grid, 512, 0, st>>>(a);
     else k_draw_rows<DT, 16, 8, CUT><<<grid, 1024, 0, st>>>(a);
 }
 
@@ -946,8 +954,10 @@ template <int DT>
 void launch_whole(const DrawArgs& a, hipStream_t st) {
     const int64_t tiles = pieces(a.in.n, 256);
     const dim3 grid = flat_grid(a.in.rows);
+    // us, 4 draws, 16 -> 4 waves: rows of 4000, 256 / 512 of them 7.8 -> 8.3 / 11.5 -> 8.2; rows of 15,000 9.9 -> 11.1 / 15.9 -> 14.2, 4096 of
+    // them 95 -> 64; rows of 32,768 13.7 -> 16.9 / 26.7 -> 24.5
     if (tiles <= 4) k_draw_whole<DT, 1><<<grid, 64, 0, st>>>(a);
-    else if (tiles <= 16 || a.in.rows >= 512) k_draw_whole<DT, 4><<<grid, 256, 0, st>>>(a);
+    else if (tiles <= 16 || a.in.rows > 256) k_draw_whole<DT, 4><<<grid, 256, 0, st>>>(a);
     else k_draw_whole<DT, 16><<<grid, 1024, 0, st>>>(a);
 }
 

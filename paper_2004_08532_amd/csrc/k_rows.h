@@ -475,10 +475,9 @@ __device__ __forceinline__ int power_of_two(int x) { return x <= 1 ? 1 : 1 << (3
 
 // The best of a workgroup's scores, as entries in an LDS list, best first.  A score that at least m of the workgroup's groups (its
 // threads, or the threads' vectors of 4) reach with their largest is reached by at least m scores, and by few more than m if
-// not many more groups reach it: -groups ln(1 - m / groups) where scores lie as they come, 1.4 m at m = groups / 2.  So it is enough to look for such a score among the groups' largest, 1024 instead of 16,384, and only until at most a quarter too many
-// reach it; the candidates are then put in order by counting (up to 256: a position is the number of entries
-// above) or by a sorting network.  Where they do not fit the list (equal scores, orders made for it) the threshold is found among all
-// scores.
+// not many more groups reach it: -groups ln(1 - m / groups) where scores lie as they come, 1.4 m at m = groups / 2.  So it is enough
+// to look for such a score among the groups' largest, 1024 instead of 16,384, and only until at most a quarter too many reach it; the
+// candidates are then put in order.  Where they do not fit the list (equal scores, orders made for it) the threshold is found among all scores.
 constexpr int BEST_ROOM = 2048;
 template <int WAVES, int TPW> struct BestList {
     static constexpr int ROOM = WAVES * TPW * 256 < BEST_ROOM ? WAVES * TPW * 256 : BEST_ROOM;
@@ -508,9 +507,15 @@ template <int PER> __device__ __forceinline__ uint32_t wave_bound(const float v[
     return lo;
 }
 
+// Whether a list is put in order by counting for each entry those above it, count^2 comparisons in few steps, or by a sorting network, which has
+// log^2 steps with a barrier each.  us, best m of 1000 scores (256 threads) by counting -> by the network: m = 60 8.0 -> 8.1, m = 100 12.3 -> 10.0,
+// m = 128 15.3 -> 9.8; of 15,000 scores, 1024 rows of 512 threads: m = 100 28.8 -> 30.5, m = 128 31.2 -> 30.8, m = 190 35.7 -> 35.1; one row,
+// 1024 threads: m = 60 8.3 -> 11.8, m = 190 10.9 -> 13.6.  (The lists have up to m / 4 entries more.)
+template <int THREADS> __device__ __forceinline__ bool by_counting(int count) { return count <= (THREADS >= 1024 ? 256 : 32 + THREADS / 4); }
+
 // Sorts the list's first `count` entries, the largest first; returns where they are.
 template <int THREADS> __device__ __forceinline__ uint64_t* order_list(uint64_t* list, uint64_t* sorted, uint32_t* rank, int count) {
-    if (count <= 256) {
+    if (by_counting<THREADS>(count)) {
         const int width = count <= 64 ? 64 : power_of_two(count), parts = THREADS > width ? THREADS / width : 1;
         for (int e = threadIdx.x; e < width; e += THREADS) rank[e] = 0;
         __syncthreads();

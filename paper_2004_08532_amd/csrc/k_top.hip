@@ -322,14 +322,18 @@ void launch_rows(const TopArgs& a, hipStream_t st) {
     else if (n <= 256) k_top_rows<DT, 1, 1><<<flat_grid(blocks), 64, 0, st>>>(a);
     else if (n <= 1024) k_top_rows<DT, 4, 1><<<flat_grid(blocks), 256, 0, st>>>(a);
     else if (n <= 4096) k_top_rows<DT, 4, 4><<<flat_grid(blocks), 256, 0, st>>>(a);
-    else if (n <= 16384 && blocks > 512) k_top_rows<DT, 8, 8><<<flat_grid(blocks), 512, 0, st>>>(a);
+    // 16,384 scores in 1024 threads, or in 512 where a CU would get more than one row.  us, best 64, 1024 -> 512 threads: 256 rows of 5000 / 15,000
+    // 9.4 -> 11.1 / 9.5 -> 11.1, 512 rows 17.0 -> 14.5 / 17.1 -> 17.0, 4096 rows 122 -> 63 / 125 -> 82
+    else if (n <= 16384 && blocks > 256) k_top_rows<DT, 8, 8><<<flat_grid(blocks), 512, 0, st>>>(a);
     else if (n <= 16384) k_top_rows<DT, 16, 4><<<flat_grid(blocks), 1024, 0, st>>>(a);
     else k_top_rows<DT, 16, 8><<<flat_grid(blocks), 1024, 0, st>>>(a);
 }
 
 }  // namespace
 
-// us per pass, segment by segment -> by tiles: TO BE MEASURED
+// The best tiles bound the scores from below only where there are more than enough of them.  us, segment by segment -> by tiles, at m = n / 512: n = 40,943,
+// 4 / 256 rows 17.3 -> 14.6 / 35 -> 22; n = 300,000 54 -> 51 / 503 -> 112; at m = n / 2000: 16.9 -> 11.5 / 32.6 -> 17.3 and 22 -> 20 / 206 -> 73.  At m = n / 300 the
+// candidates do not fit the list: 21 -> 73 / 41 -> 85.
 bool kge_top_by_tiles(int64_t n, int m) { return n > KGE_ROW_RESIDENT && n >= 512ll * m; }
 
 int64_t kge_top_workspace(int64_t rows, int64_t n, int m) {
