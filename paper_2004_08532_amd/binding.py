@@ -181,6 +181,7 @@ def kge_sample_steps(seed, triples, num_entities, batch, n_chunks, neg_per_chunk
 
 # ---- rows of scores: two-dimensional tensors [rows, n] whose rows are contiguous, any distance apart
 KGE_F32, KGE_BF16, KGE_F16 = 0, 1, 2
+_RESIDENT = 32_768  # candidates; longer rows need a workspace
 _DTYPES = {torch.float32: KGE_F32, torch.bfloat16: KGE_BF16, torch.float16: KGE_F16}
 
 
@@ -194,45 +195,44 @@ def _rows(x: torch.Tensor, name: str):
     if x.dim() != 2:
         raise ValueError(f"{name} must have two dimensions")
     rows, n = x.shape
-    ld = x.stride(0) if rows > 1 else n
-    if (n > 1 and x.stride(1) != 1) or ld < n:
+    ld, step = x.stride()
+    if rows <= 1:
+        ld = n
+    if (step != 1 and n > 1) or ld < n:
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
     return x.data_ptr(), dtype, rows, n, ld
 
 
-def _shaped(x, dtype, shape, like, name: str):
-    """Address of a contiguous tensor of this shape on the device of `like`, or None."""
+def _shaped(x, dtype, shape, device: int, name: str):
+    """Address of a contiguous tensor of this shape on the device of the scores, or None."""
     if x is None:
         return None
-    p = _dev_ptr(x, dtype, name)
+    if isinstance(x, _Tensor) and x.dtype is dtype and x.shape == shape and x.get_device() == device and x.is_contiguous():
+        return x.data_ptr()
+    _dev_ptr(x, dtype, name)
     if tuple(x.shape) != shape:
         raise ValueError(f"{name} must have the shape {shape}, got {tuple(x.shape)}")
-    if x.device != like.device:
-        raise ValueError(f"{name} must be on the device of the scores")
-    return p
+    raise ValueError(f"{name} must be on the device of the scores")
 
 
-def _on_device(call, like, hip_stream):
-    """call(stream) with the device of `like` current, as calls without a context need it."""
-    device = like.device.index
-    if device == torch.cuda.current_device():
-        return call(_stream(hip_stream))
-    with torch.cuda.device(device):
-        return call(_stream(hip_stream))
-
-
-def _workspace(given, needed: int, like, hip_stream):
-    """The caller's workspace, or one that lives until the work that has been enqueued on the stream is over."""
+def _rows_call(f, args, given, needed, device: int, hip_stream):
+    """f(*args, workspace, its size, stream) with the device of the scores current, as calls without a context need it.  The workspace is the
+    caller's, or one from the stream's own memory, which nothing else gets before the work enqueued here is over."""
+    if device != torch._C._cuda_getDevice():
+        with torch.cuda.device(device):
+            return _rows_call(f, args, given, needed, device, hip_stream)
+    stream = torch._C._cuda_getCurrentRawStream(device) if hip_stream is None else hip_stream.cuda_stream
     if given is not None:
-        if given.device != like.device:
+        at, size = _dev_ptr(given, torch.uint8, "workspace"), given.numel()
+        if given.get_device() != device:
             raise ValueError("workspace must be on the device of the scores")
-        return given
-    if needed == 0:
-        return None
-    ws = torch.empty(needed, dtype=torch.uint8, device=like.device)
-    if hip_stream is not None:
-        ws.record_stream(hip_stream)
-    return ws
+    else:
+        at, size = None, needed() if args[3] > _RESIDENT else 0
+        if size:
+            with torch.cuda.stream(hip_stream):  # (None: the current one)
+                given = torch.empty(size, dtype=torch.uint8, device=device)
+            at = given.data_ptr()
+    _check(None, f(*args, at, size, stream))
 
 
 def kge_top_scores_workspace(rows, n, m) -> int:
@@ -242,13 +242,11 @@ def kge_top_scores_workspace(rows, n, m) -> int:
 def kge_top_scores(scores, m, temperature, ids_out, scores_out, lse_out=None, workspace=None, hip_stream=None) -> None:
     """scores [rows, n] float32, bfloat16 or float16; ids_out int64 and scores_out float32 [rows, m], lse_out float32 [rows] or None."""
     p, dtype, rows, n, ld = _rows(scores, "scores")
-    m, f = int(m), torch.float32
-    ids, tops = _shaped(ids_out, torch.int64, (rows, m), scores, "ids_out"), _shaped(scores_out, f, (rows, m), scores, "scores_out")
-    lse = _shaped(lse_out, f, (rows,), scores, "lse_out")
-    ws = _workspace(workspace, kge_top_scores_workspace(rows, n, m), scores, hip_stream)
-    at, size = _dev_ptr(ws, torch.uint8, "workspace"), 0 if ws is None else ws.numel()
-    _check(None, _on_device(lambda st: _lib.kge_top_scores(p, dtype, rows, n, ld, m, float(temperature), ids, tops, lse, at, size, st),
-                            scores, hip_stream))
+    m, f, on = int(m), torch.float32, scores.get_device()
+    ids, tops = _shaped(ids_out, torch.int64, (rows, m), on, "ids_out"), _shaped(scores_out, f, (rows, m), on, "scores_out")
+    lse = _shaped(lse_out, f, (rows,), on, "lse_out")
+    _rows_call(_lib.kge_top_scores, (p, dtype, rows, n, ld, m, float(temperature), ids, tops, lse),
+               workspace, lambda: kge_top_scores_workspace(rows, n, m), on, hip_stream)
 
 
 def kge_sample_scores_workspace(rows, n, draws, top_k=0, top_p=1.0) -> int:
@@ -260,26 +258,24 @@ def kge_sample_scores(scores, u, temperature, top_k, top_p, min_p, ids_out, logp
     p, dtype, rows, n, ld = _rows(scores, "scores")
     if not isinstance(u, _Tensor) or u.dim() != 2 or u.shape[0] != rows:
         raise ValueError("u must be a tensor [rows, draws]")
-    draws = u.shape[1]
-    un = _shaped(u, torch.float64, (rows, draws), scores, "u")
-    ids = _shaped(ids_out, torch.int64, (rows, draws), scores, "ids_out")
-    logp = _shaped(logp_out, torch.float32, (rows, draws), scores, "logp_out")
-    ws = _workspace(workspace, kge_sample_scores_workspace(rows, n, draws, top_k, top_p), scores, hip_stream)
-    at, size = _dev_ptr(ws, torch.uint8, "workspace"), 0 if ws is None else ws.numel()
-    _check(None, _on_device(lambda st: _lib.kge_sample_scores(p, dtype, rows, n, ld, un, draws, float(temperature), int(top_k),
-                                                              float(top_p), float(min_p), ids, logp, at, size, st), scores, hip_stream))
+    draws, on = u.shape[1], scores.get_device()
+    un = _shaped(u, torch.float64, (rows, draws), on, "u")
+    ids = _shaped(ids_out, torch.int64, (rows, draws), on, "ids_out")
+    logp = _shaped(logp_out, torch.float32, (rows, draws), on, "logp_out")
+    _rows_call(_lib.kge_sample_scores, (p, dtype, rows, n, ld, un, draws, float(temperature), int(top_k), float(top_p), float(min_p), ids, logp),
+               workspace, lambda: kge_sample_scores_workspace(rows, n, draws, top_k, top_p), on, hip_stream)
 
 
 def kge_distill_loss_workspace(rows, n) -> int:
     return int(_lib.kge_distill_loss_workspace(int(rows), int(n)))
 
 
-def _teacher(ids, scores, lse, rows, like):
+def _teacher(ids, scores, lse, rows, on):
     if not isinstance(ids, _Tensor) or ids.dim() != 2:
         raise ValueError("teacher_ids must be a tensor [rows, m]")
     m, f = ids.shape[1], torch.float32
-    return (_shaped(ids, torch.int64, (rows, m), like, "teacher_ids"), _shaped(scores, f, (rows, m), like, "teacher_scores"),
-            _shaped(lse, f, (rows,), like, "teacher_lse"), m)
+    return (_shaped(ids, torch.int64, (rows, m), on, "teacher_ids"), _shaped(scores, f, (rows, m), on, "teacher_scores"),
+            _shaped(lse, f, (rows,), on, "teacher_lse"), m)
 
 
 def kge_distill_loss(scores, teacher_ids, teacher_scores, teacher_lse, temperature, grad_scale, loss_out=None, grad_out=None,
@@ -287,23 +283,21 @@ def kge_distill_loss(scores, teacher_ids, teacher_scores, teacher_lse, temperatu
     """scores [rows, n]; teacher_ids int64 and teacher_scores float32 [rows, m], teacher_lse float32 [rows] or None; loss_out
     float32 [rows] or None; grad_out [rows, n] of the scores' dtype, or the scores themselves, or None."""
     p, dtype, rows, n, ld = _rows(scores, "scores")
-    grad, ld_grad = None, n
+    on, grad, ld_grad = scores.get_device(), None, n
     if grad_out is not None:
         grad, g_dtype, g_rows, g_n, ld_grad = _rows(grad_out, "grad_out")
-        if (g_dtype, g_rows, g_n, grad_out.device) != (dtype, rows, n, scores.device):
+        if (g_dtype, g_rows, g_n, grad_out.get_device()) != (dtype, rows, n, on):
             raise ValueError("grad_out must have the shape, dtype and device of the scores")
-    ids, tops, lse, m = _teacher(teacher_ids, teacher_scores, teacher_lse, rows, scores)
-    loss = _shaped(loss_out, torch.float32, (rows,), scores, "loss_out")
-    ws = _workspace(workspace, kge_distill_loss_workspace(rows, n), scores, hip_stream)
-    at, size = _dev_ptr(ws, torch.uint8, "workspace"), 0 if ws is None else ws.numel()
-    _check(None, _on_device(lambda st: _lib.kge_distill_loss(p, dtype, rows, n, ld, ids, tops, lse, m, float(temperature), float(grad_scale),
-                                                             loss, grad, ld_grad, at, size, st), scores, hip_stream))
+    ids, tops, lse, m = _teacher(teacher_ids, teacher_scores, teacher_lse, rows, on)
+    loss = _shaped(loss_out, torch.float32, (rows,), on, "loss_out")
+    _rows_call(_lib.kge_distill_loss, (p, dtype, rows, n, ld, ids, tops, lse, m, float(temperature), float(grad_scale), loss, grad, ld_grad),
+               workspace, lambda: kge_distill_loss_workspace(rows, n), on, hip_stream)
 
 
 def kge_distill_step(ctx, ent, ent_state, rel, rel_state, h, r, t, b, neg, k, chunk, neg_side, gamma, lr, teacher_ids, teacher_scores,
                      teacher_lse, temperature, hip_stream=None, loss_out=None) -> None:
     f, i = torch.float32, torch.int64
-    ids, tops, lse, m = _teacher(teacher_ids, teacher_scores, teacher_lse, int(b), ent)
+    ids, tops, lse, m = _teacher(teacher_ids, teacher_scores, teacher_lse, int(b), ent.get_device())
     rc = _lib.kge_distill_step(ctx, _dev_ptr(ent, f, "ent"), _dev_ptr(ent_state, f, "ent_state"),
                                _dev_ptr(rel, f, "rel"), _dev_ptr(rel_state, f, "rel_state"),
                                _dev_ptr(h, i, "h"), _dev_ptr(r, i, "r"), _dev_ptr(t, i, "t"), int(b),

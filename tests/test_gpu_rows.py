@@ -472,6 +472,26 @@ def test_two_streams_at_once(kge):
             assert torch.equal(a[k], b[k]), k
 
 
+def test_workspace_of_another_stream(kge):
+    """Memory that the current stream still writes to is free for it, not for the stream of the call."""
+    x = rows_of(normal(2, 200_000, 3))
+    alone = {k: v.clone() for k, v in all_three(kge, x).items()}
+    out = {k: torch.empty_like(v) if k != "u" else v for k, v in alone.items()}
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    sizes = {f(2, 200_000, *rest) for f, rest in ((kge.kge_top_scores_workspace, (40,)), (kge.kge_sample_scores_workspace, (6, 0, 0.9)),
+                                                  (kge.kge_sample_scores_workspace, (6, 30, 0.9)), (kge.kge_distill_loss_workspace, ()))}
+    held = [torch.empty(size, dtype=torch.uint8, device="cuda") for size in sizes for _ in range(4)]
+    for _ in range(200):
+        for y in held:
+            y.fill_(255)
+    del held, y
+    all_three(kge, x, stream=side, out=out)
+    torch.cuda.synchronize()
+    for k in alone:
+        assert torch.equal(alone[k], out[k]), k
+
+
 def test_same_call_same_bits(kge):
     for rows, n in [(3, 700), (5, 14_951), (2, 200_000)]:
         x = rows_of(normal(rows, n, n))
