@@ -149,7 +149,7 @@ __device__ __forceinline__ void store_unlisted(typename Score<DT>::type* row, in
 }
 
 template <int DT, int WAVES, int TPW, bool STEP>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 6 : 1) void k_distill(DistillArgs a) {
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? 6 : 1) void k_distill(DistillArgs a) {
     constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64, N = TPW * 4;
     __shared__ uint32_t listed[CAP / 32];  // a bit per candidate
     __shared__ int32_t list_at[KGE_TOP_MAX];
@@ -586,6 +586,8 @@ void launch_rows(kge_ctx* c, const DistillArgs& a, hipStream_t st) {
     if (n <= 256) go(k_distill<DT, 1, 1, STEP>, 64);
     else if (n <= 1024) go(k_distill<DT, 4, 1, STEP>, 256);
     else if (n <= 4096) go(k_distill<DT, 4, 4, STEP>, 256);
+    // (us, 16 / 1024 / 4096 rows of 5000, by the kernel for 16,384 -> by this: 9.0 -> 7.5 / 23.9 -> 17.6 / 71 -> 55)
+    else if (n <= 8192) go(k_distill<DT, 8, 4, STEP>, 512);
     // (us, 16 / 256 / 4096 rows of 15,000, 1024 threads -> these 512: 9.4 -> 9.3 / 13.5 -> 11.9 / 168 -> 132)
     else if (n <= 16384) go(k_distill<DT, 8, 8, STEP>, 512);
     else go(k_distill<DT, 16, 8, STEP>, 1024);

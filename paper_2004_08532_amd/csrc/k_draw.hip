@@ -513,7 +513,7 @@ __device__ __forceinline__ bool cut_enclosed(float v[TPW * 4], const L& low, flo
 enum { CUT_MIN, CUT_WEIGHT, CUT_LIST };  // min-p alone; top-p and min-p; top-k and what follows it
 
 template <int DT, int WAVES, int TPW, int CUT>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? (CUT == CUT_WEIGHT ? 4 : 6) : 1) void k_draw_rows(DrawArgs a) {
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? (CUT == CUT_WEIGHT ? 4 : 6) : 1) void k_draw_rows(DrawArgs a) {
     constexpr int THREADS = WAVES * 64, N = TPW * 4, TILES = WAVES * TPW;
     __shared__ float maxima[WAVES];
     const int64_t row = flat_block();
@@ -944,6 +944,9 @@ void launch_rows(const DrawArgs& a, hipStream_t st) {
     if (n <= 256) k_draw_rows<DT, 1, 1, CUT><<<grid, 64, 0, st>>>(a);
     else if (n <= 1024) k_draw_rows<DT, 4, 1, CUT><<<grid, 256, 0, st>>>(a);
     else if (n <= 4096) k_draw_rows<DT, 4, 4, CUT><<<grid, 256, 0, st>>>(a);
+    // us, 16 / 1024 / 4096 rows of 5000, by the kernel for 16,384 -> by this: top-p 20 -> 17.6 / 48 -> 41 / 181 -> 154, min-p 7.9 -> 7.0 / 18.3 -> 16.2 /
+    // 61 -> 52, top-k 50 12.0 -> 10.5 / 23.5 -> 20.5 / 70 -> 60
+    else if (n <= 8192) k_draw_rows<DT, 8, 4, CUT><<<grid, 512, 0, st>>>(a);
     // (1024 threads of half as many scores are as fast up to 256 rows.  us, 512 / 4096 rows of 15,000, 1024 -> 512 threads: top-p 46 -> 32 / 360 -> 221,
     // min-p 17.3 -> 12.7 / 122 -> 73, top-k 50 22.6 -> 13.8 / 165 -> 72)
     else if (n <= 16384) k_draw_rows<DT, 8, 8, CUT><<<grid, 512, 0, st>>>(a);

@@ -322,6 +322,8 @@ void launch_rows(const TopArgs& a, hipStream_t st) {
     else if (n <= 256) k_top_rows<DT, 1, 1><<<flat_grid(blocks), 64, 0, st>>>(a);
     else if (n <= 1024) k_top_rows<DT, 4, 1><<<flat_grid(blocks), 256, 0, st>>>(a);
     else if (n <= 4096) k_top_rows<DT, 4, 4><<<flat_grid(blocks), 256, 0, st>>>(a);
+    // us, best 64 of 5000, by the kernels for 16,384 -> by this: 16 / 1024 / 4096 rows 9.0 -> 7.8 / 18.9 -> 11.8 / 63 -> 38.5
+    else if (n <= 8192) k_top_rows<DT, 8, 4><<<flat_grid(blocks), 512, 0, st>>>(a);
     // 16,384 scores in 1024 threads, or in 512 where a CU would get more than one row.  us, best 64, 1024 -> 512 threads: 256 rows of 5000 / 15,000
     // 9.4 -> 11.1 / 9.5 -> 11.1, 512 rows 17.0 -> 14.5 / 17.1 -> 17.0, 4096 rows 122 -> 63 / 125 -> 82
     else if (n <= 16384 && blocks > 256) k_top_rows<DT, 8, 8><<<flat_grid(blocks), 512, 0, st>>>(a);

@@ -74,7 +74,8 @@ def check_top(kge, x, m, T=1.0, **more):
 
 
 SIZES = [(1, 1, 1), (3, 2, 5), (1, 4, 4), (5, 63, 1), (5, 255, 10), (4, 256, 256), (3, 257, 300), (2, 1024, 1024), (4, 1025, 7), (3, 4096, 64),
-         (2, 4097, 1000), (2, 16384, 33), (2, 16385, 1024), (2, 32768, 5), (2, 32769, 1024), (2, 70001, 3), (1, 300_001, 1024), (2, 300_001, 500), (1, 700_001, 1024)]
+         (2, 4097, 1000), (2, 8192, 40), (300, 8193, 300), (2, 16384, 33),
+         (2, 16385, 1024), (2, 32768, 5), (2, 32769, 1024), (2, 70001, 3), (1, 300_001, 1024), (2, 300_001, 500), (1, 700_001, 1024)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
@@ -156,7 +157,7 @@ SETTINGS = [dict(), dict(T=0.0), dict(T=0.6, min_p=0.05), dict(top_p=0.9), dict(
 
 
 @pytest.mark.parametrize("setting", range(len(SETTINGS)))
-@pytest.mark.parametrize("rows,n,draws", [(1, 1, 1), (3, 5, 2), (5, 255, 7), (2, 256, 64), (3, 1000, 3), (2, 4096, 5), (2, 5000, 100), (3, 16384, 2), (1, 16385, 70),
+@pytest.mark.parametrize("rows,n,draws", [(1, 1, 1), (3, 5, 2), (5, 255, 7), (2, 256, 64), (3, 1000, 3), (2, 4096, 5), (2, 5000, 100), (2, 8192, 3), (300, 8193, 4), (3, 16384, 2), (1, 16385, 70),
                                           (2, 32768, 4), (2, 32769, 9), (1, 70_001, 3), (1, 1_000_003, 33)])
 def test_sample(kge, rows, n, draws, setting):
     dtype = [torch.float32, torch.bfloat16, torch.float16][(n + setting) % 3]
@@ -322,7 +323,7 @@ def teacher_lists(x, m, seed, T, unused=True):
 @pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("rows,n,m", [(1, 1, 1), (3, 2, 5), (5, 255, 10), (4, 256, 256), (3, 257, 300), (2, 1024, 1024), (4, 1025, 7), (3, 4096, 64), (2, 4097, 1000),
-                                      (2, 16384, 33), (2, 16385, 1024), (2, 32768, 5), (2, 32769, 1024), (2, 70001, 3), (1, 300_001, 100)])
+                                      (2, 8192, 40), (300, 8193, 20), (2, 16384, 33), (2, 16385, 1024), (2, 32768, 5), (2, 32769, 1024), (2, 70001, 3), (1, 300_001, 100)])
 def test_distill(kge, rows, n, m, dtype, rest):
     x = normal(rows, n, n + m, dtype=dtype)
     T = 2.0 if n % 2 else 0.75
