@@ -172,12 +172,13 @@ __global__ __launch_bounds__(1024) void k_top_finish(FinishArgs a, DrawArgs draw
     float mine[PER], best = -INFINITY;
 #pragma unroll
     for (int g = 0; g < PER; ++g) mine[g] = -INFINITY;
-    for (int64_t t0 = threadIdx.x; t0 < a.tiles; t0 += PER * THREADS) {
+    constexpr int READS = 8;  // of a thread at once
+    for (int64_t t0 = threadIdx.x; t0 < a.tiles; t0 += READS * THREADS) {
+        float x[READS];
 #pragma unroll
-        for (int g = 0; g < PER; ++g) {
-            const int64_t t = t0 + g * THREADS;
-            mine[g] = fmaxf(mine[g], t < a.tiles ? bests[t] : -INFINITY);
-        }
+        for (int k = 0; k < READS; ++k) x[k] = bests[min(t0 + k * THREADS, a.tiles - 1)];
+#pragma unroll
+        for (int k = 0; k < READS; ++k) mine[k % PER] = fmaxf(mine[k % PER], t0 + k * THREADS < a.tiles ? x[k] : -INFINITY);
     }
 #pragma unroll
     for (int g = 0; g < PER; ++g) {
@@ -201,15 +202,18 @@ __global__ __launch_bounds__(1024) void k_top_finish(FinishArgs a, DrawArgs draw
     }
     __syncthreads();
     float t = key_score(shared_bound);
-    for (int64_t i0 = 0; i0 < a.tiles; i0 += THREADS) {
-        const int64_t i = i0 + threadIdx.x;
-        const bool in = i < a.tiles && bests[i] >= t;
-        const uint64_t who = __ballot(in);
-        if (!who) continue;
-        uint32_t at = 0;
-        if (lane == 0) at = atomicAdd(&n_tiles, (uint32_t)__popcll(who));
-        at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + (uint32_t)__popcll(who & (((uint64_t)1 << lane) - 1));
-        if (in && at < TILE_ROOM) tile_list[at] = (uint32_t)i;
+    for (int64_t i0 = threadIdx.x; i0 < a.tiles; i0 += READS * THREADS) {
+        float x[READS];
+#pragma unroll
+        for (int k = 0; k < READS; ++k) x[k] = bests[min(i0 + k * THREADS, a.tiles - 1)];
+#pragma unroll
+        for (int k = 0; k < READS; ++k) {
+            const int64_t i = i0 + k * THREADS;
+            if (i < a.tiles && x[k] >= t) {  // (few)
+                const uint32_t at = atomicAdd(&n_tiles, 1u);
+                if (at < TILE_ROOM) tile_list[at] = (uint32_t)i;
+            }
+        }
     }
     __syncthreads();
     const uint32_t found = n_tiles;
