@@ -300,8 +300,8 @@ int kge_top_scores(const void* scores, int32_t dtype, int64_t rows, int64_t n, i
                    void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
- * Draws from every row by given random numbers.  With w_j = exp((s_j - best) / temperature) (masked candidates, -inf and NaN: 0) the
- * candidates kept are the first K in order, K the least of
+ * Draws from every row by given random numbers.  With w_j = exp((s_j - best) / temperature) (0 for masked candidates, -inf and NaN,
+ * and where it is less than 2^-1000) the candidates kept are the first K in order, K the least of
  *     top_k (0, or n and more: all; else at most 1024),
  *     the fewest whose w sum to top_p times the sum over those first top_k or more (1: all; at least one), and
  *     the number with w_j >= min_p (0: all);

@@ -7,9 +7,14 @@
 // p_r = 1 - sum p is the mass that the teacher has outside of the list, q_r = Z_r / Z the student's, P = sum p + p_r.
 //
 // A row that a workgroup holds is read once and its gradient written once: the weights stay in registers between the sum and the gradient.
-// Long rows: a pass for the sums, one workgroup per row for what their gradients have in common, a second pass for the gradient.  Bound by
-// the reads and writes, of long rows by the arithmetic of the weights as much.  A weight is formed in 32 bits from an argument in 64; what is a
-// difference of near values (logarithms of the loss, the rest) and all sums of weights are in 64.
+// Long rows: a pass for the sums, one workgroup per row for what their gradients have in common, a second pass for the gradient.  A weight is
+// formed in 32 bits from an argument in 64; what is a difference of near values (logarithms of the loss, the rest) and all sums of weights are
+// in 64.
+//
+// 1024 rows of 14,951 fp32, lists of 64 and a rest: 36 us, 3.4 TB/s read and written (a large copy: 24 us); the vector units work for 19, and the
+// phases of a row (reads, sums, list, writes) overlap only with those of two other rows on the CU.  16 rows of 2.5 M bf16, lists of 256 and a
+// rest: sums 33 us (2.4 TB/s; 12.2 M wave instructions, 25 us of the vector units), lists 9, gradient 32 (5 TB/s).  690 rows of 40,943 fp16, loss
+// alone: sums 24, lists 7.  1024 rows of 256, lists of 16: 7 us.
 #include "k_rows.h"
 
 namespace {

@@ -6,6 +6,13 @@
 //
 // Sums are kept per tile of 256 scores; a draw is a wave that finds its tile among the sums and its position in the tile.  All sums are
 // formed in 64 bits, in a fixed order or as whole numbers, so a draw depends on the row and its number alone.
+//
+// What bounds them (fp32; a large copy takes 12 us for the first and 16 us for the last of these):
+//     1024 rows of 14,951, 16 draws, nothing cut   k_draw_whole 30 us: a weight in 64 bits per score, 13 M wave instructions, 26 us of the vector units
+//     the same, top-p 0.9, 1 draw                  k_draw_rows 63 us: bins, then weights in 64 bits, 23 M wave instructions, 47 us of the vector units
+//     one such row                                 k_draw_rows 22 us: a chain of some twenty steps between barriers, on one CU
+//     2 rows of 10 M, top-p 0.95, 64 draws         143 us in 9 launches: best and lowest score 16, bins 43, 29, 13 and 6, the cut 5, sums of what is
+//                                                  kept 26, running sums 8, draws 6; the first bins and the sums are bound by their weights
 #include "k_draw_list.h"
 
 namespace {
@@ -612,7 +619,7 @@ __global__ __launch_bounds__(256) void k_draw_lists(DrawArgs a, const uint64_t* 
 // ---------------------------------------------------------------------------------------------------------
 constexpr int LOG_BINS = 11, BINS = 1 << LOG_BINS;
 constexpr int ROUNDS = 4;  // bins of equal width, then 2^32 keys in three rounds
-constexpr int PART_GROUPS = 4, NOTES = 1024;  // groups per workgroup of k_draw_bins, scores that it can note
+constexpr int PART_GROUPS = 4, NOTES = 1024;  // groups per workgroup of k_draw_bins (16: 178 us for 2 x 10 M where 4 took 148), scores that it can note
 
 struct RowCut {
     BinRule<LOG_BINS> rule;
@@ -711,7 +718,22 @@ __global__ __launch_bounds__(256) void k_draw_bins(LongArgs a, int round) {
         for (int64_t g = part * PART_GROUPS; g < last; ++g) {
             float v[16];
             load_tiles<DT, 4, 4>(s, g * GROUP, a.d.in.n, v);
-            if (round == 0) {
+            if (round == 0 && c.best < INFINITY) {  // (as add, without a branch per score)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    const float at = floorf(fminf(c.rule.place(v[q]), (float)(BINS - 1)));
+                    const double d = (double)v[q] - w.best, shifted = fma(d, scale.per, 0x1.8p52), f = fma(d, scale.per, -(shifted - 0x1.8p52));
+                    double p = scale.c[8];
+#pragma unroll
+                    for (int i = 7; i >= 0; --i) p = fma(p, f, scale.c[i]);
+                    const int up = __double2loint(shifted) - (int)floorf(-at * c.rule.drop) + a.bits;
+                    const double x = Weights::scaled(fma(p, f, 1.0), up) + 0x1p52;
+                    const bool some = v[q] >= w.floor && up >= -2;  // the others add 0, at places that do not collide
+                    atomicAdd(&bins[some ? (int)at : (int)(threadIdx.x & 63)],
+                              some ? (unsigned long long)__double_as_longlong(x) & (((uint64_t)1 << 52) - 1) : 0ull);
+                    if (q % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+            } else if (round == 0) {
 #pragma unroll
                 for (int q = 0; q < 16; ++q) if (v[q] > -INFINITY) add(v[q]);
             } else {

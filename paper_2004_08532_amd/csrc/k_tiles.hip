@@ -3,7 +3,8 @@
 //
 // Weights are relative to the best score of the four tiles that a wave has at a time, so that waves work for themselves: no score has to be known
 // before the others are read.  Every workgroup goes through a range of groups and has the next one's scores on their way while it works on one's: reads and
-// arithmetic take about the same time (20 M fp32 scores: 16 us each).
+// arithmetic take about the same time: 20 M fp32 scores with best and lowest alone 16 us (5 TB/s, the rate of a large copy), 40 M bf16 scores with the
+// tiles' best 15 us (5.3 TB/s).
 #include "k_rows.h"
 
 namespace {
