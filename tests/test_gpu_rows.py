@@ -221,6 +221,18 @@ def test_where_top_p_ends(kge, n, top_p):
     check_sample(kge, rows_of(torch.from_numpy(3.4e38 * g.uniform(-1, 1, (6, n))).float()), u, T=1e38, top_p=top_p)
 
 
+@pytest.mark.parametrize("top_k", [300, 1024])
+@pytest.mark.parametrize("n", [1100, 6000, 12_000, 30_000, 40_000, 120_000, 600_000])
+def test_sample_of_long_lists(kge, n, top_k):
+    g = np.random.default_rng(n)
+    x = g.normal(0, 2, (3, n))
+    x[1] = np.round(x[1])
+    x[2, n // 7:] = -math.inf
+    for dtype in (torch.float32, torch.float16):
+        check_sample(kge, rows_of(torch.from_numpy(x), dtype), g.random((3, 20)), top_k=top_k)
+        check_sample(kge, rows_of(torch.from_numpy(x), dtype), g.random((3, 20)), T=3.0, top_k=top_k, top_p=0.95, min_p=1e-3)
+
+
 def test_numbers_outside_of_the_unit_interval(kge):
     for n in (100, 2000, 50_000):
         x = normal(2, n, n)
@@ -263,7 +275,7 @@ def distill64(x, ids, t, lse, T):
         target = np.bincount(listed, p, x.shape[1])
         with np.errstate(divide="ignore"):
             logs = np.log(p) - ((row[listed] - row[row > -np.inf].max()) / T - np.log(w.sum()))
-        loss[i] = (p * logs)[p > 0].sum()
+        loss[i] = (p[p > 0] * logs[p > 0]).sum()
         rest = 0.0 if lse is None else max(0.0, 1.0 - p.sum())
         other = w.copy()
         other[listed] = 0.0
@@ -297,7 +309,8 @@ def check_distill(kge, x, ids, t, lse=None, T=1.0, c=1.0, in_place=False, grad=T
     got = loss[:rows].double().cpu().numpy()
     finite = np.isfinite(want)
     assert np.array_equal(got[~finite], want[~finite])
-    assert (np.abs(got - want)[finite] <= (1.01 * U32 * np.abs(want) + mass * 2 * W_ERR)[finite]).all(), np.abs(got - want).max()
+    got, want = got[finite], want[finite]
+    assert (np.abs(got - want) <= 1.01 * U32 * np.abs(want) + mass * 2 * W_ERR).all(), np.abs(got - want).max()
     if grad:
         got = out.double().cpu().numpy()
         limit = abs(c) * (scale * (Q_ERR + 4 * U32)) + 1.01 * HALF_STEP[dtype] * np.abs(c * g) + TINY[dtype]
@@ -500,6 +513,17 @@ def test_same_call_same_bits(kge):
         for _ in range(3):
             again = all_three(kge, x)
             assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+@pytest.mark.parametrize("rows,n", [(70_001, 5), (66_000, 300)])
+def test_many_rows(kge, rows, n):
+    """A row's results do not depend on how many rows the call has."""
+    x = torch.randn(rows, n, generator=torch.Generator("cuda").manual_seed(n), device="cuda")
+    all_at_once = {k: v.clone() for k, v in all_three(kge, x).items()}
+    for first in (0, 40_000, rows - 500):
+        part = x[first:first + 500]
+        some = all_three(kge, part, out={k: torch.empty_like(v[:500]) if k != "u" else v[first:first + 500].contiguous() for k, v in all_at_once.items()})
+        assert all(torch.equal(some[k], all_at_once[k][first:first + 500]) for k in some), first
 
 
 def test_positions_past_31_bits(kge):
