@@ -508,10 +508,10 @@ template <int PER> __device__ __forceinline__ uint32_t wave_bound(const float v[
 }
 
 // Whether a list is put in order by counting for each entry those above it, count^2 comparisons in few steps, or by a sorting network, which has
-// log^2 steps with a barrier each.  us, best m of 1000 scores (256 threads) by counting -> by the network: m = 60 8.0 -> 8.1, m = 100 12.3 -> 10.0,
-// m = 128 15.3 -> 9.8; of 15,000 scores, 1024 rows of 512 threads: m = 100 28.8 -> 30.5, m = 128 31.2 -> 30.8, m = 190 35.7 -> 35.1; one row,
-// 1024 threads: m = 60 8.3 -> 11.8, m = 190 10.9 -> 13.6.  (The lists have up to m / 4 entries more.)
-template <int THREADS> __device__ __forceinline__ bool by_counting(int count) { return count <= (THREADS >= 1024 ? 256 : 32 + THREADS / 4); }
+// log^2 steps with a barrier each.  us, best m of 1565 scores (256 threads), 14 / 1024 rows, by the network -> by counting: m = 80 10.8 -> 7.3 /
+// 12.8 -> 9.5, m = 150 14.2 -> 10.8 / 19.0 -> 16.1; of 6000 (512 threads): m = 150 12.6 -> 9.3 / 17.6 -> 15.3; of 15,000 (1024 threads, 14 rows): m = 60
+// 11.8 -> 8.9.  One wave, of 250 scores: m = 30 6.7 -> 6.0, m = 100 (all 250 are candidates) 12 -> 20.  (The lists have up to m / 4 entries more.)
+template <int THREADS> __device__ __forceinline__ bool by_counting(int count) { return count <= (THREADS == 64 ? 64 : 256); }
 
 // Sorts the list's first `count` entries, the largest first; returns where they are.
 template <int THREADS> __device__ __forceinline__ uint64_t* order_list(uint64_t* list, uint64_t* sorted, uint32_t* rank, int count) {
@@ -524,7 +524,15 @@ template <int THREADS> __device__ __forceinline__ uint64_t* order_list(uint64_t*
             if (e < count) {
                 const uint64_t own = list[e];
                 uint32_t above = 0;
-                for (int j = part; j < count; j += parts) above += list[j] > own;
+                int j = part;
+                for (; j + 7 * parts < count; j += 8 * parts) {
+                    uint64_t y[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = list[j + i * parts];  // (all reads at once)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) above += y[i] > own;
+                }
+                for (; j < count; j += parts) above += list[j] > own;
                 if (parts > 1) atomicAdd(&rank[e], above);
                 else rank[e] = above;
             }
