@@ -456,15 +456,23 @@ __device__ __forceinline__ void append_marked(const float v[N], uint32_t marked,
     }
 }
 
-// Sorts the first `size` (a power of two) entries of a list in LDS, the largest first.
+// Sorts the first `size` entries (a power of two, 128 or more) of a list in LDS, the largest first.
 template <int THREADS> __device__ __forceinline__ void sort_descending(uint64_t* list, int size) {
+    constexpr int PAIRS = THREADS == 64 ? 2 : 1024 / THREADS;  // of a thread (one wave: lists of up to 256)
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63u), lane = threadIdx.x & 63;
     for (int k = 2; k <= size; k *= 2) {
         for (int j = k / 2; j > 0; j /= 2) {
             __syncthreads();
-            for (int p = threadIdx.x; p < size / 2; p += THREADS) {
-                const int x = 2 * p - (p & (j - 1)), y = x + j;
-                const uint64_t a = list[x], b = list[y];
-                if ((a < b) == ((x & k) == 0)) { list[x] = b; list[y] = a; }
+            uint64_t a[PAIRS], b[PAIRS];
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {  // (all reads at once)
+                const int p = wave + i * THREADS + lane, x = 2 * p - (p & (j - 1));
+                if (wave + i * THREADS < size / 2) { a[i] = list[x]; b[i] = list[x + j]; }
+            }
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                const int p = wave + i * THREADS + lane, x = 2 * p - (p & (j - 1));
+                if (wave + i * THREADS < size / 2 && (a[i] < b[i]) == ((x & k) == 0)) { list[x] = b[i]; list[x + j] = a[i]; }
             }
         }
     }
@@ -542,7 +550,7 @@ template <int THREADS> __device__ __forceinline__ uint64_t* order_list(uint64_t*
         __syncthreads();
         return sorted;
     }
-    const int size = power_of_two(count);
+    const int size = power_of_two(max(count, 128));
     for (int e = count + threadIdx.x; e < size; e += THREADS) list[e] = 0;
     sort_descending<THREADS>(list, size);
     return list;
