@@ -516,9 +516,10 @@ template <int PER> __device__ __forceinline__ uint32_t wave_bound(const float v[
 }
 
 // Whether a list is put in order by counting for each entry those above it, count^2 comparisons in few steps, or by a sorting network, which has
-// log^2 steps with a barrier each.  us, best m of 1565 scores (256 threads), 14 / 1024 rows, by the network -> by counting: m = 80 10.8 -> 7.3 /
-// 12.8 -> 9.5, m = 150 14.2 -> 10.8 / 19.0 -> 16.1; of 6000 (512 threads): m = 150 12.6 -> 9.3 / 17.6 -> 15.3; of 15,000 (1024 threads, 14 rows): m = 60
-// 11.8 -> 8.9.  One wave, of 250 scores: m = 30 6.7 -> 6.0, m = 100 (all 250 are candidates) 12 -> 20.  (The lists have up to m / 4 entries more.)
+// log^2 steps with a barrier each.  us, best m of 1565 scores (256 threads), 14 / 1024 rows, by the network -> by counting: m = 80 11.2 -> 6.9 /
+// 14.2 -> 9.7, m = 150 14.5 -> 10.7 / 19.7 -> 16.5; of 6000 (512 threads): m = 60 10.5 -> 7.4 / 16.0 -> 11.4, m = 150 12.2 -> 9.4 / 17.8 -> 15.4; of 15,000
+// (1024 threads, 14 rows): m = 60 12.4 -> 8.8, m = 150 14.0 -> 10.2.  One wave, of 250 scores: m = 100 (all 250 are candidates) 9.2 -> 20.  (The
+// lists have up to m / 4 entries more.)
 template <int THREADS> __device__ __forceinline__ bool by_counting(int count) { return count <= (THREADS == 64 ? 64 : 256); }
 
 // Sorts the list's first `count` entries, the largest first; returns where they are.
