@@ -14,6 +14,7 @@
 //     2 rows of 10 M, top-p 0.95, 64 draws         143 us in 9 launches: best and lowest score 16, bins 43, 29, 13 and 6, the cut 5, sums of what is
 //                                                  kept 26, running sums 8, draws 6; the first bins and the sums are bound by their weights
 #include "k_draw_list.h"
+#include "k_probe.h"
 
 namespace {
 
@@ -920,14 +921,12 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
         return;
     }
     const double want = unit_number(a.d.u[d]) * total;
-    int64_t lo = 0, hi = a.groups - 1;  // the first group whose sum exceeds `want` is in lo .. hi (or none does)
-    while (lo < hi) {
-        const int64_t step = (hi - lo + 63) / 64, at = min(lo + (lane + 1) * step - 1, hi);
-        const uint64_t past = __ballot(sums[at] > want);
-        const int first = past ? __ffsll((unsigned long long)past) - 1 : 63;
-        hi = min(lo + (first + 1) * step - 1, hi);
-        lo = min(lo + first * step, hi);
+    Probes groups = {0, a.groups - 1};  // the first group whose sum exceeds `want`
+    while (groups.open()) {
+        const uint64_t past = __ballot(sums[groups.at(lane)] > want);
+        groups.narrow(past ? __ffsll((unsigned long long)past) - 1 : 63);
     }
+    int64_t lo = groups.lo;
     while (lo > 0 && !(sums[lo] > sums[lo - 1])) --lo;  // (never a group without weight)
     const int64_t group = row * a.groups + lo;
     const Scale scale(a.d.inv_t);
