@@ -79,6 +79,8 @@ __device__ __forceinline__ void draw_in_tile(const Quad<DT>& x, int64_t first, i
 template <int DT, int WAVES, int TILES>
 __device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, const typename Score<DT>::type* s, int tiles, double* sums,
                                                 const float* tile_best, const Kept& kept, const Weights& weights) {
+    constexpr int WORDS = (TILES + 63) / 64;
+    __shared__ uint64_t weighted[WORDS];  // tiles with a weight (the running sums differ by roundings also where nothing was added)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     __syncthreads();
     if (wave == 0) {  // running sums
@@ -88,6 +90,8 @@ __device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, 
             const int t = t0 + lane;
             double x = t < tiles ? sums[t] : 0.0;
             if (tile_best && t < tiles) x = tile_best[t] > -INFINITY ? x * weights.of(tile_best[t]) : 0.0;
+            const uint64_t some = __ballot(x > 0.0);
+            if (lane == 0) weighted[t0 / 64] = some;
             x = carry + wave_scan64(x, lane);
             if (t < tiles) sums[t] = x;
             carry = lane64(x, 63);
@@ -95,13 +99,12 @@ __device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, 
     }
     __syncthreads();
     const double total = sums[tiles - 1];
-    double x[TILES / 64 + 1];
+    double x[WORDS];
     int last = 0;  // tile with a weight
 #pragma unroll
-    for (int k = 0; k * 64 < TILES; ++k) {
-        const int t = k * 64 + lane;
-        x[k] = t < tiles ? sums[t] : INFINITY;
-        const uint64_t some = __ballot(t < tiles && x[k] > (t > 0 ? sums[t - 1] : 0.0));
+    for (int k = 0; k < WORDS; ++k) {
+        const uint64_t some = weighted[k];
+        x[k] = some >> lane & 1 ? sums[k * 64 + lane] : -INFINITY;
         if (some) last = k * 64 + 63 - __clzll(some);
     }
     constexpr int AT_ONCE = 4;  // draws of a wave whose tiles are read together
@@ -113,10 +116,12 @@ __device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, 
 #pragma unroll
         for (int d = 0; d < AT_ONCE; ++d) {
             const double want = lane64(own, d);
-            int at = 0;
+            tile[d] = last;  // the first tile with a weight whose running sum exceeds `want`
 #pragma unroll
-            for (int k = 0; k * 64 < TILES; ++k) at += __popcll(__ballot(x[k] <= want));  // (running sums: the tiles in front)
-            tile[d] = min(at, last);
+            for (int k = WORDS - 1; k >= 0; --k) {
+                const uint64_t past = __ballot(x[k] > want);
+                if (past) tile[d] = k * 64 + __ffsll((unsigned long long)past) - 1;
+            }
             quad[d].load(s, (int64_t)tile[d] * 256 + lane * 4, a.in.n);
         }
 #pragma unroll
@@ -927,25 +932,35 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
         groups.narrow(past ? __ffsll((unsigned long long)past) - 1 : 63);
     }
     int64_t lo = groups.lo;
-    while (lo > 0 && !(sums[lo] > sums[lo - 1])) --lo;  // (never a group without weight)
-    const int64_t group = row * a.groups + lo;
     const Scale scale(a.d.inv_t);
     const Weights weights(best, scale);
-    double base = lo > 0 ? sums[lo - 1] : 0.0, v = 0.0;
-    uint32_t e = 0, before = 0;
-    if (lane < GROUP_TILES) {
-        const float own = a.tile_best[group * GROUP_TILES + lane];
-        v = own > -INFINITY ? a.tile_sum[group * GROUP_TILES + lane] * weights.of(own) : 0.0;
-        if (kept.ties) e = a.tile_ties[group * GROUP_TILES + lane];
+    double base, incl;
+    uint32_t before;
+    int tile;
+    for (;; --lo) {  // (never a group without weight, whose running sum may be a rounding above the one before it)
+        const int64_t group = row * a.groups + lo;
+        base = lo > 0 ? sums[lo - 1] : 0.0;
+        before = 0;
+        double v = 0.0;
+        uint32_t e = 0;
+        if (lane < GROUP_TILES) {
+            const float own = a.tile_best[group * GROUP_TILES + lane];
+            v = own > -INFINITY ? a.tile_sum[group * GROUP_TILES + lane] * weights.of(own) : 0.0;
+            if (kept.ties) e = a.tile_ties[group * GROUP_TILES + lane];
+        }
+        if (kept.ties) {
+            before = a.group_ties[group] + wave_scan_u32(e) - e;
+            if (before < kept.ties) v += weights.of(kept.t) * (double)min(e, kept.ties - before);
+        }
+        const uint64_t any = __ballot(v > 0.0);
+        if (!any && lo > 0) continue;
+        incl = base + wave_scan64(v, lane);
+        const uint64_t past = __ballot(incl > want && v > 0.0);
+        tile = past ? __ffsll((unsigned long long)past) - 1 : any ? 63 - __clzll(any) : 0;
+        incl -= v;
+        break;
     }
-    if (kept.ties) {
-        before = a.group_ties[group] + wave_scan_u32(e) - e;
-        if (before < kept.ties) v += weights.of(kept.t) * (double)min(e, kept.ties - before);
-    }
-    const double incl = base + wave_scan64(v, lane);
-    const uint64_t past = __ballot(incl > want && v > 0.0), any = __ballot(v > 0.0);
-    const int tile = past ? __ffsll((unsigned long long)past) - 1 : any ? 63 - __clzll(any) : 0;
-    base = lane64(incl - v, tile);
+    base = lane64(incl, tile);
     before = __shfl((int)before, tile, 64);
     int64_t id = -1;
     double weight = 0.0;

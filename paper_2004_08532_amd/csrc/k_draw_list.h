@@ -14,7 +14,7 @@ struct DrawArgs {
 #ifdef __HIPCC__
 namespace {
 
-__device__ __forceinline__ double unit_number(double u) { return u > 0.0 ? u : 0.0; }  // (NaN: 0)
+__device__ __forceinline__ double unit_number(double u) { return u > 0.0 ? fmin(u, 1.0 - 0x1p-53) : 0.0; }  // (NaN: 0)
 
 template <int THREADS> __device__ __forceinline__ void write_empty(const DrawArgs& a, int64_t row) {
     for (int d = threadIdx.x; d < a.draws; d += THREADS) {
@@ -61,14 +61,17 @@ __device__ __forceinline__ void draw_from_list(const DrawArgs& a, int64_t row, u
     const double total = sums[count - 1];
     for (int d = threadIdx.x; d < a.draws; d += THREADS) {
         const double want = unit_number(a.u[row * a.draws + d]) * total;
-        int lo = 0, hi = count - 1;  // first entry whose running sum exceeds `want`, the last one where none does
+        int lo = 0, hi = count - 1;  // first entry whose running sum exceeds `want`
         while (lo < hi) {
             const int mid = (lo + hi) / 2;
             if (sums[mid] > want) hi = mid; else lo = mid + 1;
         }
-        while (lo > 0 && !(sums[lo] > sums[lo - 1])) --lo;  // (an entry without weight is never drawn)
+        // (An entry without weight is never drawn.  The running sums do not tell: they are added up in another order from lane to lane, so that one can
+        // differ from the one before it by a rounding where nothing was added.)
+        double w = weights.of(key_score((uint32_t)list[lo]));
+        while (lo > 0 && !(w > 0.0)) w = weights.of(key_score((uint32_t)list[--lo]));
         a.ids[row * a.draws + d] = (int64_t)(uint32_t)~(uint32_t)(list[lo] >> 32);
-        if (a.logp) a.logp[row * a.draws + d] = (float)log(weights.of(key_score((uint32_t)list[lo])) / total);
+        if (a.logp) a.logp[row * a.draws + d] = (float)log(w / total);
     }
 }
 

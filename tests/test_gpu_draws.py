@@ -1,11 +1,11 @@
-"""Draws by kge_sample_scores where a search or a rounding can miss."""
+"""Draws by kge_sample_scores where a search or a rounding can miss: every id has to be a candidate that is kept, with a weight of its own."""
 import math
 
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_rows import U32, kge  # noqa: F401
+from test_gpu_rows import U32, kge, normal, order, rows_of, weights  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +46,62 @@ def test_last_group_at_every_number_of_groups(kge):
     for groups in range(9, most + 1):
         n = groups * 4096 - groups % 3
         equal_scores(kge, n, buffer, np.array([0, n // 2, n - 4096, n - 1]), lambda k: k)
+
+
+# ---- tiles and entries without a weight
+
+def check_draws(kge, x, u, T=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """Each id is kept and has a weight; the number lies in the candidate's own part of the sum, to 1e-12 of the whole sum (its weights are off by 4e-14
+    and sums of up to 2^17 in 64 bits by less than that); logp is that candidate's."""
+    rows = x.shape[0]
+    ids = torch.full(u.shape, -7, dtype=torch.int64, device="cuda")
+    logp = torch.full(u.shape, 77.0, device="cuda")
+    kge.kge_sample_scores(x, torch.from_numpy(u).cuda(), T, top_k, top_p, min_p, ids, logp)
+    x, ids, logp = x.double().cpu().numpy(), ids.cpu().numpy(), logp.cpu().numpy()
+    T, top_p, min_p = (float(np.float32(v)) for v in (T, top_p, min_p))
+    for i in range(rows):
+        first = order(x[i])
+        w = weights(x[i], T)
+        w[w < 2.0 ** -1000] = 0.0
+        first = first[:top_k] if top_k else first
+        if top_p < 1:
+            sums = np.cumsum(w[first])
+            first = first[:1 + np.searchsorted(sums[:-1], top_p * sums[-1])]
+        kept = np.sort(first[w[first] >= min_p])
+        kept = kept[w[kept] > 0]
+        sums = np.cumsum(w[kept].astype(np.longdouble))
+        want = np.clip(np.nan_to_num(u[i]), 0.0, 1.0 - 2.0 ** -53) * sums[-1]
+        for d in range(u.shape[1]):
+            at = np.searchsorted(kept, ids[i, d])
+            assert at < kept.size and kept[at] == ids[i, d], (i, d, u[i, d], ids[i, d])
+            slack = 1e-12 * sums[-1] if want[d] > 0 else 0.0
+            assert sums[at] - w[kept[at]] - slack <= want[d] <= sums[at] + slack, (i, d, u[i, d], ids[i, d])
+            exact = float(np.log(w[kept[at]] / sums[-1]))
+            assert abs(logp[i, d] - exact) <= 1.01 * U32 * abs(exact) + 1e-12, (i, d, logp[i, d], exact)
+
+
+ALL_KEPT = [dict(), dict(min_p=1e-6), dict(top_p=0.97), dict(top_p=0.9, min_p=0.001, T=2.0), dict(top_k=200), dict(top_k=900, T=0.002)]
+NUMBERS = [1.0, 1.0 - 2.0 ** -53, 1.0 - 2.0 ** -52, 5.0, math.inf, 0.0, -1.0, math.nan]
+
+
+@pytest.mark.parametrize("setting", range(len(ALL_KEPT)))
+@pytest.mark.parametrize("n", [200, 700, 1300, 2000, 5000, 8000, 15_000, 30_000, 50_000, 90_000])
+def test_numbers_at_the_ends(kge, n, setting):
+    x = normal(32, n, n + setting)
+    x[8:16, n - n // 3:] = -math.inf
+    x[16:24, :n // 3] = -math.inf
+    check_draws(kge, rows_of(x), np.tile(NUMBERS, (32, 1)), **ALL_KEPT[setting])
+
+
+@pytest.mark.parametrize("setting", range(len(ALL_KEPT)))
+@pytest.mark.parametrize("n", [1300, 5000, 15_000, 30_000, 70_000])
+def test_numbers_at_the_borders_of_masked_tiles(kge, n, setting):
+    """Numbers that are the running sums in front of stretches of masked candidates."""
+    x = normal(16, n, n + setting)
+    part = max(256, n // 6 // 256 * 256)
+    for first in range(part, n, 2 * part):
+        x[:, first:first + part] = -math.inf
+    w = np.stack([weights(r, ALL_KEPT[setting].get("T", 1.0)) for r in x.double().numpy()])
+    sums = np.cumsum(w, 1)
+    u = sums[:, part - 1::part] / sums[:, -1:]
+    check_draws(kge, rows_of(x), np.concatenate([u, np.nextafter(u, 0.0)], 1), **ALL_KEPT[setting])
