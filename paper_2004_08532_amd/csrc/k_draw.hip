@@ -75,7 +75,15 @@ __device__ __forceinline__ void draw_in_tile(const Quad<DT>& x, int64_t first, i
     weight = __shfl(weight, who, 64);
 }
 
-// The draws of a row whose tile sums a workgroup has in LDS.  sums[t]: of tile t, relative to best[t] (a row's best where that is null).
+// Tiles of rows of which nothing is left out have sums relative to the best of the four tiles that a wave had at a time, and what counts beside that can
+// be too little beside the row's best: a tile with a sum whose scores are all below the row's floor.  Then one of the other three, whose best is not
+// below it, is where the number falls: the tiles behind it, j = 1, 2, ..., and where those end the ones in front of it.
+__device__ __forceinline__ int other_of_four(int tile, int j) {
+    const int r = tile & 3;
+    return r + j < 4 ? tile + j : tile - (r + j - 3);
+}
+
+// The draws of a row whose tile sums a workgroup has in LDS.  sums[t]: of tile t, relative to tile_best[t] (the row's best where that is null).
 template <int DT, int WAVES, int TILES>
 __device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, const typename Score<DT>::type* s, int tiles, double* sums,
                                                 const float* tile_best, const Kept& kept, const Weights& weights) {
@@ -124,12 +132,34 @@ __device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, 
             }
             quad[d].load(s, (int64_t)tile[d] * 256 + lane * 4, a.in.n);
         }
+        uint32_t missed = 0;  // a bit per draw
 #pragma unroll
         for (int d = 0; d < AT_ONCE; ++d) {
             if (d >= n) break;
             int64_t id = -1;
             double weight = 0.0;
             draw_in_tile<DT, false>(quad[d], (int64_t)tile[d] * 256, a.in.n, kept, weights, 0u, tile[d] > 0 ? sums[tile[d] - 1] : 0.0, lane64(own, d), lane, id, weight);
+            if (tile_best && id < 0) missed |= 1u << d;
+            if (lane == 0) {
+                a.ids[row * a.draws + d0 + d] = id;
+                if (a.logp) a.logp[row * a.draws + d0 + d] = (float)log(weight / total);
+            }
+        }
+        if (!tile_best) continue;
+        for (; missed; missed &= missed - 1) {
+            const int d = __ffs((int)missed) - 1;
+            int from = tile[0];
+#pragma unroll
+            for (int k = 1; k < AT_ONCE; ++k) from = d == k ? tile[k] : from;
+            int64_t id = -1;
+            double weight = 0.0;
+#pragma unroll 1
+            for (int j = 1; j < 4 && id < 0; ++j) {
+                const int t = other_of_four(from, j);
+                if (t >= tiles) continue;
+                quad[0].load(s, (int64_t)t * 256 + lane * 4, a.in.n);
+                draw_in_tile<DT, false>(quad[0], (int64_t)t * 256, a.in.n, kept, weights, 0u, t > 0 ? sums[t - 1] : 0.0, lane64(own, d), lane, id, weight);
+            }
             if (lane == 0) {
                 a.ids[row * a.draws + d0 + d] = id;
                 if (a.logp) a.logp[row * a.draws + d0 + d] = (float)log(weight / total);
@@ -960,13 +990,16 @@ __global__ __launch_bounds__(256) void k_draw_pick(LongArgs a) {
         incl -= v;
         break;
     }
-    base = lane64(incl, tile);
-    before = __shfl((int)before, tile, 64);
     int64_t id = -1;
     double weight = 0.0;
-    Quad<DT> x;
-    x.load(s, lo * GROUP + (int64_t)tile * 256 + lane * 4, a.d.in.n);
-    draw_in_tile<DT, true>(x, lo * GROUP + (int64_t)tile * 256, a.d.in.n, kept, weights, before, base, want, lane, id, weight);
+#pragma unroll 1
+    for (int j = 0; j < 4 && id < 0; ++j) {
+        const int t = j == 0 ? tile : other_of_four(tile, j);
+        const int64_t first = lo * GROUP + (int64_t)t * 256;
+        Quad<DT> x;
+        x.load(s, first + lane * 4, a.d.in.n);
+        draw_in_tile<DT, true>(x, first, a.d.in.n, kept, weights, (uint32_t)__shfl((int)before, t, 64), lane64(incl, t), want, lane, id, weight);
+    }
     if (lane == 0) {
         a.d.ids[d] = id;
         if (a.d.logp) a.d.logp[d] = (float)log(weight / total);

@@ -105,3 +105,24 @@ def test_numbers_at_the_borders_of_masked_tiles(kge, n, setting):
     sums = np.cumsum(w, 1)
     u = sums[:, part - 1::part] / sums[:, -1:]
     check_draws(kge, rows_of(x), np.concatenate([u, np.nextafter(u, 0.0)], 1), **ALL_KEPT[setting])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [1024, 2048, 5000, 14_000, 33_000, 80_000, 300_000])
+def test_tiles_whose_weights_are_less_than_any(kge, n, dtype):
+    """The number 0 falls on the first candidate with a weight of 2^-1000 or more, whatever lies in front of it: tiles of 256 whose weights are a
+    little less, beside tiles whose weights are a little more."""
+    x = np.full((6, n), -math.inf)
+    x[:, n - 3] = 0.0                       # the best one
+    x[0, 0:256], x[0, 256 + 9] = -695.0, -600.0    # exp(-693.15) = 2^-1000
+    x[1, 0:512], x[1, 512 + 200] = -700.0, -690.0
+    x[2, 3], x[2, 300], x[2, 600], x[2, 1000] = -695.0, -694.0, -698.0, -692.0
+    x[3, 0:1024:5] = -696.0
+    x[3, 700] = -688.0
+    x[4, 0:256] = -690.0
+    x[4, 256:1000] = -700.0
+    x[5] = -694.0
+    x[5, n // 2 - 4] = -640.0
+    x[5, n - 3:] = 0.0
+    check_draws(kge, rows_of(torch.from_numpy(x), dtype), np.tile([0.0, -1.0, 0.5, 1.0 - 2.0 ** -53, 1e-310], (6, 1)))
+    check_draws(kge, rows_of(torch.from_numpy(x / 128), dtype), np.tile([0.0, 0.5], (6, 1)), T=1 / 128)
