@@ -259,6 +259,8 @@ template <int LOG_BINS> __device__ __forceinline__ BinRule<LOG_BINS> next_bins(c
         x.hi = r.hi - ((uint32_t)b << r.shift);
         const uint32_t last = ((uint32_t)1 << r.shift) - 1;
         x.lo = x.hi >= last && x.hi - last > r.lo ? x.hi - last : r.lo;
+        // (no score has the key of -0, but an interval that ends with it would hold +0, which the bin in front has counted)
+        if (x.hi == NEGATIVE_ZERO_KEY && x.hi > x.lo) --x.hi;
     }
     x.shift = x.hi > x.lo ? max(0, 32 - __clz(x.hi - x.lo) - LOG_BINS) : 0;
     double p;

@@ -134,6 +134,7 @@ template <int DT> struct Quad {
 };
 
 constexpr uint32_t LOWEST_KEY = 0x00800000u;  // of the lowest finite number
+constexpr uint32_t NEGATIVE_ZERO_KEY = 0x7FFFFFFFu;  // below that of +0; of no score
 __device__ __forceinline__ uint32_t order_key(float s) {
     const uint32_t u = __float_as_uint(s + 0.f);  // -0 -> +0
     const uint32_t k = u >> 31 ? ~u : u | 0x80000000u;

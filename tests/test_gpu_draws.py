@@ -126,3 +126,17 @@ def test_tiles_whose_weights_are_less_than_any(kge, n, dtype):
     x[5, n - 3:] = 0.0
     check_draws(kge, rows_of(torch.from_numpy(x), dtype), np.tile([0.0, -1.0, 0.5, 1.0 - 2.0 ** -53, 1e-310], (6, 1)))
     check_draws(kge, rows_of(torch.from_numpy(x / 128), dtype), np.tile([0.0, 0.5], (6, 1)), T=1 / 128)
+
+
+@pytest.mark.parametrize("n", [1500, 2000, 6000, 15_000, 30_000, 40_000, 200_000])
+def test_top_p_that_ends_next_to_zero(kge, n):
+    """The cut lies among scores of -2^-149, just below many zeros and above a few more: whatever the first bins are, whose borders the row's best and
+    lowest score set, the zeros are counted once."""
+    g = np.random.default_rng(n)
+    for most, T in ((1 << 20, 1e-39), (1 << 23, 1e-38)):
+        x = g.choice([0, -1, 9], (64, n), p=[0.2, 0.25, 0.55])
+        x = np.where(x == 9, g.integers(-40, 31, x.shape), x).astype(np.float64)
+        x[:, 7], x[:, n // 2] = most + np.arange(64) * 3, -most - g.integers(0, 64, 64)
+        x[:, -1] = -1
+        u = np.concatenate([np.tile([1.0 - 2.0 ** -53, 0.0], (64, 1)), g.random((64, 4))], 1)
+        check_draws(kge, rows_of(torch.from_numpy(x * 2.0 ** -149).float()), u, T=T, top_p=0.6)
