@@ -310,6 +310,7 @@ int kge_top_scores(const void* scores, int32_t dtype, int64_t rows, int64_t n, i
  * u [rows x draws] (fp64: a row of millions of candidates needs more than 24 bits).  ids_out [rows x draws] receives the positions,
  * logp_out (float, same shape, or NULL) the logarithm of the candidate's share of the kept w.  A row without a candidate: id
  * -1, logarithm -inf.  Numbers outside [0, 1) count as the nearest inside, NaN as 0.
+ * draws is in [1, 2^20]; of rows of more than 32,768 values without a top_k, rows * draws is at most 2^33.
  */
 int64_t kge_sample_scores_workspace(int64_t rows, int64_t n, int32_t draws, int32_t top_k, float top_p);
 int kge_sample_scores(const void* scores, int32_t dtype, int64_t rows, int64_t n, int64_t ld,

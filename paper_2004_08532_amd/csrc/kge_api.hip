@@ -935,6 +935,9 @@ int kge_sample_scores(const void* scores, int32_t dtype, int64_t rows, int64_t n
     if (!u || !ids_out) return fail(nullptr, KGE_ERR_INVALID_ARG, "null random numbers or output%s");
     if (top_k >= n) top_k = 0;
     if (temperature == 0.f) { top_k = 1; temperature = 1.f; }  // the best candidate
+    // (a wave per draw, four to a workgroup, and workgroups are numbered in 31 bits)
+    if (n > KGE_ROW_RESIDENT && top_k == 0 && rows * draws > (1ll << 33))
+        return fail(nullptr, KGE_ERR_INVALID_ARG, "rows * draws must be at most 2^33 for rows of more than 32768 values%s");
     rc = check_workspace(workspace, workspace_bytes, kge_draw_workspace(rows, n, top_k, top_p));
     if (rc != KGE_OK) return rc;
     kge_launch_draw({scores, dtype, rows, n, ld}, u, draws, temperature, top_k, top_p, min_p, ids_out, logp_out, workspace, (hipStream_t)stream);
