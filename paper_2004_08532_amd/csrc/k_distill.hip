@@ -29,7 +29,7 @@ struct DistillArgs {
     RowScores in;
     TeacherLists t;
     double inv_t;
-    float grad_scale, loss_scale;  // grad_scale: of the call times T; loss_scale: T^2, and 1 / b in a step
+    double grad_scale, loss_scale;  // grad_scale: of the call times T; loss_scale: T^2, and 1 / b in a step
     float* loss;
     void* grad;
     int64_t ld_grad;
@@ -101,6 +101,12 @@ __device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, 
     return l;
 }
 
+// (What fp32 does not hold becomes its largest value: a weight of 0 times it is a gradient of 0.)
+__device__ __forceinline__ float coefficient(double x) {
+    const double most = 3.402823466e38;
+    return (float)(x > most ? most : x < -most ? -most : x);
+}
+
 // From the sums of a row (best score, sum of weights, of those not listed) and of its list.
 __device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, double best, double z, double z_rest, const ListSums& l) {
     double mass = l.a, scale = 1.0, rest = 0.0;
@@ -112,11 +118,11 @@ __device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, double best, d
         mass *= scale;
     }
     RowGrad g = {best, scale, 0.f, 0.f, 0.f};
-    const double c = (double)a.grad_scale;
+    const double c = a.grad_scale;
     if (z != 0.0 && mass + rest != 0.0) {
-        g.listed = (float)(c * (mass + rest) / z);
-        g.other = rest > 0.0 ? (float)(c * ((mass + rest) / z - rest / z_rest)) : g.listed;
-        g.unit = (float)c;
+        g.listed = coefficient(c * (mass + rest) / z);
+        g.other = rest > 0.0 ? coefficient(c * ((mass + rest) / z - rest / z_rest)) : g.listed;
+        g.unit = coefficient(c);
     }
     return g;
 }
@@ -131,7 +137,7 @@ __device__ __forceinline__ double row_loss(const DistillArgs& a, double z, doubl
     if (z == 0.0 || mass + rest == 0.0) return 0.0;
     double loss = cross + mass * log(z);
     if (rest > 0.0) loss += rest * log(rest * z / z_rest);
-    return loss * (double)a.loss_scale;
+    return loss * a.loss_scale;
 }
 
 // Gradients j .. j + 3 of a row of n, but those of candidates whose bit is set.
@@ -619,8 +625,8 @@ void kge_launch_distill(const RowScores& in, const TeacherLists& t, float grad_s
     DistillArgs a = {};
     a.in = in; a.t = t;
     a.inv_t = 1.0 / (double)t.temperature;
-    a.grad_scale = grad_scale * t.temperature;
-    a.loss_scale = loss_scale * t.temperature * t.temperature;
+    a.grad_scale = (double)grad_scale * (double)t.temperature;
+    a.loss_scale = (double)loss_scale * (double)t.temperature * (double)t.temperature;
     a.loss = loss; a.grad = grad; a.ld_grad = ld_grad;
     if (step) {
         a.step = *step;
