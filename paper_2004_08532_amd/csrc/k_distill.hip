@@ -5,6 +5,8 @@
 //     grad_j = c T [ P q_j - sum_{e: id_e = j} p_e ]   listed candidates, and all where the lists are all there is
 //     grad_j = c T [ P - p_r Z / Z_r ] q_j             candidates that are not listed, where there is a rest
 // p_r = 1 - sum p is the mass that the teacher has outside of the list, q_r = Z_r / Z the student's, P = sum p + p_r.
+// Z_r can be less than any number where the listed candidates lie far above the others.  So what is not listed has weights relative to its own best
+// score u, w'_j = exp(z_j - u / T) and Z'_r = sum w' >= 1, wherever that matters: the gradient of these is c T [ P exp((u - max) / T) / Z - p_r / Z'_r ] w'_j.
 //
 // A row that a workgroup holds is read once and its gradient written once: the weights stay in registers between the sum and the gradient.
 // Long rows: a pass for the sums, one workgroup per row for what their gradients have in common, a second pass for the gradient.  A weight is
@@ -19,9 +21,10 @@
 
 namespace {
 
-// What the gradients of a row have in common: grad_j = w_j * (listed or other) - p * unit, with w relative to `best`; p_e = exp(Teacher::log_p) * scale.
+// What the gradients of a row have in common: of listed candidates w_j * listed - p * unit, with w relative to the row's best score and p_e =
+// exp(Teacher::log_p) * scale; of the others w_j * other, with w relative to `from`.
 struct RowGrad {
-    double best, scale;
+    double from, scale;
     float listed, other, unit;
 };
 
@@ -36,7 +39,7 @@ struct DistillArgs {
     StepRows step;
     // long rows
     int64_t groups, per;  // groups of a row, and of a workgroup
-    double* sums;         // [rows][groups][3]: a score, the weights' sum relative to it, that of the listed ones where there is a rest
+    double* sums;         // [rows][groups][2]: a score, the weights' sum relative to it; where there is a rest of those that are not listed
     RowGrad* rows;
 };
 
@@ -84,19 +87,20 @@ struct Teacher {
     __device__ __forceinline__ double log_p(int e) const { return ((double)scores[e] - best) * inv_t - lse; }
 };
 
-struct ListSums { double a, b; };  // sum of p before it is scaled, sum of p * (log p - (s - best) / T)
+struct ListSums { double a, b, z; };  // sum of p before it is scaled, sum of p * (log p - (s - best) / T), with a rest the weights of the list's candidates
 
-// A thread's part of the list's sums.
-template <int DT, int THREADS>
-__device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, const RowAt<DT>& r, const Teacher& teacher, double best) {
-    ListSums l = {0.0, 0.0};
+// A thread's part of the list's sums.  stands(e): the first entry of its candidate.
+template <int DT, int THREADS, typename S>
+__device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, const RowAt<DT>& r, const Teacher& teacher, double best, const S& stands) {
+    ListSums l = {0.0, 0.0, 0.0};
 #pragma unroll 1
     for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
         const int64_t id = list_position<DT>(a, row, e, r.n);
         if (id < 0) continue;
-        const double lp = teacher.log_p(e), p = exp(lp);
+        const double lp = teacher.log_p(e), p = exp(lp), x = ((double)r.at(id) - best) * a.inv_t;
         l.a += p;
-        if (p > 0.0 || p != p) l.b += p * (lp - ((double)r.at(id) - best) * a.inv_t);
+        if (p > 0.0 || p != p) l.b += p * (lp - x);
+        if (a.t.lse && stands(e)) l.z += x < INFINITY ? exp(x) : __longlong_as_double(0x7FF8000000000000ll);  // (of +inf and NaN)
     }
     return l;
 }
@@ -107,36 +111,46 @@ __device__ __forceinline__ float coefficient(double x) {
     return (float)(x > most ? most : x < -most ? -most : x);
 }
 
-// From the sums of a row (best score, sum of weights, of those not listed) and of its list.
-__device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, double best, double z, double z_rest, const ListSums& l) {
+// Weights of a row: z = Z, relative to the row's best score; z_rest: of the candidates that are not listed (of all, where that makes no difference), relative
+// to the score `from`, whose own weight is `shift`.
+struct RowSums {
+    double best, from, shift, z, z_rest;
+};
+__device__ __forceinline__ RowSums row_sums(const DistillArgs& a, double best, double from, const ListSums& l, double z_rest) {
+    const double shift = from == best ? 1.0 : exp((from - best) * a.inv_t);
+    return {best, from, shift, z_rest > 0.0 ? l.z + z_rest * shift : l.z + z_rest, z_rest};
+}
+// From these and the sums of the row's list.
+__device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, const RowSums& s, const ListSums& l) {
     double mass = l.a, scale = 1.0, rest = 0.0;
     if (a.t.lse) {
         rest = fmax(1.0 - mass, 0.0);
-        if (!(z_rest > 0.0)) rest = 0.0;  // no candidate that it could go to
+        if (!(s.z_rest > 0.0)) rest = 0.0;  // no candidate that it could go to
     } else {
         scale = mass > 0.0 || mass != mass ? 1.0 / mass : 0.0;
         mass *= scale;
     }
-    RowGrad g = {best, scale, 0.f, 0.f, 0.f};
+    RowGrad g = {s.from, scale, 0.f, 0.f, 0.f};
     const double c = a.grad_scale;
-    if (z != 0.0 && mass + rest != 0.0) {
-        g.listed = coefficient(c * (mass + rest) / z);
-        g.other = rest > 0.0 ? coefficient(c * ((mass + rest) / z - rest / z_rest)) : g.listed;
+    if (s.z != 0.0 && mass + rest != 0.0) {
+        const double own = c * (mass + rest) / s.z;
+        g.listed = coefficient(own);
+        g.other = rest > 0.0 ? coefficient(own * s.shift - c * rest / s.z_rest) : s.z_rest > 0.0 ? coefficient(own * s.shift) : g.listed;
         g.unit = coefficient(c);
     }
     return g;
 }
-__device__ __forceinline__ double row_loss(const DistillArgs& a, double z, double z_rest, const ListSums& l) {
+__device__ __forceinline__ double row_loss(const DistillArgs& a, const RowSums& s, const ListSums& l) {
     double mass = l.a, cross = l.b, rest = 0.0;
     if (a.t.lse) {
-        rest = z_rest > 0.0 ? fmax(1.0 - mass, 0.0) : 0.0;
+        rest = s.z_rest > 0.0 ? fmax(1.0 - mass, 0.0) : 0.0;
     } else if (mass > 0.0 || mass != mass) {  // log p has still to lose the logarithm of the sum
         cross = cross / mass - log(mass);
         mass /= mass;
     }
-    if (z == 0.0 || mass + rest == 0.0) return 0.0;
-    double loss = cross + mass * log(z);
-    if (rest > 0.0) loss += rest * log(rest * z / z_rest);
+    if (s.z == 0.0 || mass + rest == 0.0) return 0.0;
+    double loss = cross + mass * log(s.z);
+    if (rest > 0.0) loss += rest * (log(rest * s.z / s.z_rest) - (s.from - s.best) * a.inv_t);
     return loss * a.loss_scale;
 }
 
@@ -159,12 +173,14 @@ __device__ __forceinline__ void store_unlisted(typename Score<DT>::type* row, in
     }
 }
 
-template <int DT, int WAVES, int TPW, bool STEP>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? 6 : 1) void k_distill(DistillArgs a) {
+// REST: the teacher's log-sum-exp is given.  (Rows of 16,384 with a rest: 126 registers and 4 waves per SIMD; at 6, 31 are spilled and 1024 rows of 14,951 take 54 us
+// instead of 42.)
+template <int DT, int WAVES, int TPW, bool REST, bool STEP>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? (REST ? 4 : 6) : 1) void k_distill(DistillArgs a) {
     constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64, N = TPW * 4;
     __shared__ uint32_t listed[CAP / 32];  // a bit per candidate
     __shared__ int32_t list_at[KGE_TOP_MAX];
-    __shared__ float maxima[2][WAVES];
+    __shared__ float maxima[3][WAVES];
     __shared__ double parts[4][WAVES];
     __shared__ RowGrad shared_grad;
     __shared__ int twice;  // a candidate is listed more than once
@@ -217,50 +233,66 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? 6 : 1) void k_
     }
     best = scalar(best);
     const Teacher teacher(a, row, scalar(list_best));
-    const Weight32 weight(best, a.inv_t * 1.4426950408889634);
-    // sums of the weights: with a rest, of the candidates that are not listed, and of the few others
-    double z = 0.0, z_listed = 0.0;
+    // With a rest the list's candidates have no part in the registers' weights, which are relative to the best of the others.
+    float from = best;
+    if constexpr (REST) {
+        uint32_t bits[(TPW + 7) / 8] = {};  // of the registers, in their order
+#pragma unroll
+        for (int i = 0; i < TPW; ++i) bits[i / 8] |= (listed[((i * WAVES + wave) * 256 + lane * 4) >> 5] >> (lane * 4 & 31) & 15u) << i % 8 * 4;
+        from = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            const int mask = __builtin_amdgcn_sbfe((int)bits[q / 32], q % 32, 1);  // (-1: listed)
+            v[q] = __int_as_float((mask & (int)0xFF800000) | (~mask & __float_as_int(v[q])));
+            from = fmaxf(from, v[q]);
+        }
+        from = wave_most(from);
+        if constexpr (WAVES > 1) {
+            if (lane == 0) maxima[2][wave] = from;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) from = fmaxf(from, maxima[2][w]);
+        }
+        from = scalar(from);
+    }
+    const double per = a.inv_t * 1.4426950408889634;
+    const Weight32 relative(from, per);
+    double z = 0.0;
     forget<N>(v);
 #pragma unroll
     for (int i = 0; i < TPW; ++i) {
-        const int at = (i * WAVES + wave) * 256 + lane * 4;
-        const uint32_t bits = a.t.lse ? listed[at >> 5] >> (at & 31) & 15u : 0u;
-        float four;
 #pragma unroll
-        for (int q = 4 * i; q < 4 * i + 4; ++q) v[q] = weight.of(v[q]);
-        four = (v[4 * i] + v[4 * i + 1]) + (v[4 * i + 2] + v[4 * i + 3]);
-        if (bits) {
-            four = 0.f;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (bits >> q & 1) z_listed += (double)v[4 * i + q];
-                else four += v[4 * i + q];
-            }
-        }
-        z += (double)four;
+        for (int q = 4 * i; q < 4 * i + 4; ++q) v[q] = relative.of(v[q]);
+        z += (double)((v[4 * i] + v[4 * i + 1]) + (v[4 * i + 2] + v[4 * i + 3]));
         __builtin_amdgcn_sched_barrier(0);  // (tile by tile: the 64-bit halves of all weights at once would not fit the registers)
     }
     forget<N>(v);
-    ListSums l = {0.0, 0.0};
+    auto stands = [&](int e) {
+        bool first = true;
+        if (twice) for (int x = 0; x < e; ++x) first = first && list_at[x] != list_at[e];
+        return first;
+    };
+    const Weight32 weight(best, per);
+    ListSums l = {0.0, 0.0, 0.0};
     z = wave_sum64(z);
     if (wave * 64 < a.t.m) {
-        l = sum_list<DT, THREADS>(a, row, r, teacher, weight.best);
+        l = sum_list<DT, THREADS>(a, row, r, teacher, weight.best, stands);
         l.a = wave_sum64(l.a);
         l.b = wave_sum64(l.b);
+        if constexpr (REST) l.z = wave_sum64(l.z);
     }
-    if (__ballot(z_listed != 0.0)) z_listed = wave_sum64(z_listed);
-    if (lane == 0) { parts[0][wave] = z; parts[1][wave] = z_listed; parts[2][wave] = l.a; parts[3][wave] = l.b; }
+    if (lane == 0) { parts[0][wave] = z; parts[1][wave] = l.z; parts[2][wave] = l.a; parts[3][wave] = l.b; }
     __syncthreads();
     if (wave == 0) {  // (one wave for all: the divisions and logarithms of a row are as much work as a tile)
         double sum[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum[k] = wave_sum64(lane < WAVES ? parts[k][lane] : 0.0);
-        const double z_rest = sum[0], all = best == INFINITY ? __longlong_as_double(0x7FF8000000000000ll) : sum[0] + sum[1];
-        l = {sum[2], sum[3]};
+        l = {sum[2], sum[3], sum[1]};
+        const RowSums sums = row_sums(a, weight.best, relative.best, l, best == INFINITY ? __longlong_as_double(0x7FF8000000000000ll) : sum[0]);
         if (lane == 0) {
-            if (a.loss) a.loss[row] = (float)row_loss(a, all, z_rest, l);
+            if (a.loss) a.loss[row] = (float)row_loss(a, sums, l);
             if constexpr (STEP) a.step.cpos[row] = 0.f;
-            shared_grad = row_grad(a, weight.best, all, z_rest, l);
+            shared_grad = row_grad(a, sums, l);
         }
     }
     if (!a.grad) return;
@@ -281,13 +313,11 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? 6 : 1) void k_
         const int at = list_at[e];
         if (at < 0) continue;
         auto p_of = [&](int x) { return exp(teacher.log_p(x)) * g.scale; };
+        if (!stands(e)) continue;
         double p = p_of(e);
-        bool stands = true;
         if (twice) {
-            for (int x = 0; x < e; ++x) stands = stands && list_at[x] != at;
-            for (int x = e + 1; stands && x < a.t.m; ++x) if (list_at[x] == at) p += p_of(x);
+            for (int x = e + 1; x < a.t.m; ++x) if (list_at[x] == at) p += p_of(x);
         }
-        if (!stands) continue;
         const float raw = widen<DT>(r.s[at]);
         out[at] = narrow<DT>(shape(fmaf(weight.of(r.of(raw)), g.listed, -(float)p * g.unit), raw));
     }
@@ -346,7 +376,7 @@ __device__ __forceinline__ uint32_t marks_of(const uint32_t* bits, int p) { retu
 template <int DT>
 __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
     __shared__ uint32_t listed[3][GROUP_WORDS];
-    __shared__ double parts[3][4];
+    __shared__ double parts[2][4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t blocks = a.in.rows * a.groups, start = (int64_t)flat_block() * a.per, end = min(start + a.per, blocks);
     if (start >= blocks) return;
@@ -370,7 +400,7 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
         __syncthreads();
     }
     float base = -INFINITY, limit = -INFINITY;
-    double z = 0.0, z_listed = 0.0;  // of this lane
+    double z = 0.0;  // of this lane
     Weight32 weight(base, per);
     int turn = 0;
     for (int64_t block = start; block < end; ++block) {
@@ -379,6 +409,11 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i].template values<false>(here.group * GROUP + (wave * 4 + i) * 256, a.in.n, v + 4 * i);
+            const uint32_t bits = rest ? marks_of(listed[turn], (wave * 4 + i) * 256 + lane * 4) : 0u;
+            if (bits) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) if (bits >> q & 1) v[4 * i + q] = -INFINITY;
+            }
             best = largest(largest(best, v[4 * i], v[4 * i + 1]), v[4 * i + 2], v[4 * i + 3]);
         }
         at.step(a.groups);
@@ -400,7 +435,6 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
             } else if (top > limit) {
                 const double f = base > -INFINITY ? exp2(((double)base - (double)top) * per) : 0.0;
                 z = f == 0.0 && !(z != z) ? 0.0 : z * f;
-                z_listed = f == 0.0 ? 0.0 : z_listed * f;
                 base = top;
                 limit = top + (float)fmin(40.0 / per, 3e38);
                 weight = Weight32(base, per);
@@ -408,18 +442,7 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t bits = rest ? marks_of(listed[turn], (wave * 4 + i) * 256 + lane * 4) : 0u;
-#pragma unroll
-            for (int q = 4 * i; q < 4 * i + 4; ++q) v[q] = weight.of(v[q]);
-            float four = (v[4 * i] + v[4 * i + 1]) + (v[4 * i + 2] + v[4 * i + 3]);
-            if (bits) {
-                four = 0.f;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if (bits >> q & 1) z_listed += (double)v[4 * i + q];
-                    else four += v[4 * i + q];
-                }
-            }
+            const float four = (weight.of(v[4 * i]) + weight.of(v[4 * i + 1])) + (weight.of(v[4 * i + 2]) + weight.of(v[4 * i + 3]));
             z += (double)four;
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -427,15 +450,14 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
         const bool last = block + 1 == end || at.row != here.row;
         if (last) {
             z = wave_sum64(z);
-            if (rest) z_listed = wave_sum64(z_listed);
-            if (lane == 0) { parts[0][wave] = (double)base; parts[1][wave] = z; parts[2][wave] = z_listed; }
+            if (lane == 0) { parts[0][wave] = (double)base; parts[1][wave] = z; }
             base = limit = -INFINITY;
-            z = z_listed = 0.0;
+            z = 0.0;
         }
         if (last || rest) __syncthreads();
         if (threadIdx.x == 0) {
-            double* p = a.sums + 3 * block;
-            double top = -INFINITY, s = 0.0, sl = 0.0;
+            double* p = a.sums + 2 * block;
+            double top = -INFINITY, s = 0.0;
             if (last) {
 #pragma unroll 1
                 for (int w = 0; w < 4; ++w) top = fmax(top, parts[0][w]);
@@ -443,10 +465,9 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
                 for (int w = 0; w < 4; ++w) {
                     const double b = parts[0][w], f = b == top ? 1.0 : exp2((b - top) * per);
                     if (parts[1][w] != 0.0) s += parts[1][w] * f;
-                    if (parts[2][w] != 0.0) sl += parts[2][w] * f;
                 }
             }
-            p[0] = top; p[1] = s; p[2] = sl;
+            p[0] = top; p[1] = s;
         }
         if (last) __syncthreads();
     }
@@ -467,17 +488,19 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     RowAt<DT> r;
     r.s = static_cast<const typename Score<DT>::type*>(a.in.p) + row * a.in.ld;
     r.n = a.in.n; r.is_dist = false; r.gamma = 0.f;
-    const double* p = a.sums + 3 * row * a.groups;
+    const double* p = a.sums + 2 * row * a.groups;
     const double per = a.inv_t * 1.4426950408889634;
+    const bool rest = a.t.lse != nullptr;
     constexpr uint32_t NONE = 0xFFFFFFFFu;  // (not a position: rows have fewer than 2^32 candidates)
     for (int x = threadIdx.x; x < SLOTS; x += 256) { key[x] = NONE; first[x] = NONE; times[x] = 0; }
-    float best = -INFINITY, list_best = -INFINITY;
-    for (int64_t g = threadIdx.x; g < a.groups; g += 256) best = fmaxf(best, (float)p[3 * g]);
+    float from = -INFINITY, list_best = -INFINITY, listed_best = -INFINITY;  // best of what the sums are of, of the teacher's scores, of the student's in the list
+    for (int64_t g = threadIdx.x; g < a.groups; g += 256) from = fmaxf(from, (float)p[2 * g]);
     __syncthreads();
     for (int e = threadIdx.x; e < a.t.m; e += 256) {
         const int64_t id = list_position<DT>(a, row, e, r.n);
         if (id < 0) { entry_slot[e] = 0xFFFF; continue; }
         list_best = fmaxf(list_best, a.t.scores[row * a.t.m + e]);
+        if (rest) listed_best = fmaxf(listed_best, r.at(id));
         uint32_t x = ((uint32_t)id * 2654435761u) >> 21;  // (2^11 slots for up to 2^10 candidates: there is always a free one)
         while (true) {
             const uint32_t was = atomicCAS(&key[x], NONE, (uint32_t)id);
@@ -488,25 +511,24 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
         atomicAdd(&times[x], 1u);
         entry_slot[e] = (uint16_t)x;
     }
-    best = block_max<4>(best, maxima);
+    from = block_max<4>(from, maxima);
     list_best = block_max<4>(list_best, maxima);
-    double z = 0.0, z_listed = 0.0;
-    for (int64_t g = threadIdx.x; g < a.groups; g += 256) {
-        const double b = p[3 * g], f = b == (double)best ? 1.0 : exp2((b - (double)best) * per);
-        if (p[3 * g + 1] != 0.0) z += p[3 * g + 1] * f;
-        if (p[3 * g + 2] != 0.0) z_listed += p[3 * g + 2] * f;
-    }
-    z = block_sum64<4>(z, slot);
-    z_listed = block_sum64<4>(z_listed, slot);
+    if (rest) listed_best = block_max<4>(listed_best, maxima);
+    const float best = fmaxf(from, listed_best);
+    const double b = best > -INFINITY ? (double)best : 0.0;
+    double z_rest = 0.0;
+    for (int64_t g = threadIdx.x; g < a.groups; g += 256)
+        if (p[2 * g + 1] != 0.0) z_rest += p[2 * g + 1] * (p[2 * g] == (double)from ? 1.0 : exp2((p[2 * g] - (double)from) * per));
+    z_rest = block_sum64<4>(z_rest, slot);
     const Teacher teacher(a, row, list_best);
-    const double b = best > -INFINITY ? (double)best : 0.0, z_rest = z;
-    z += z_listed;
-    ListSums l = sum_list<DT, 256>(a, row, r, teacher, b);
+    ListSums l = sum_list<DT, 256>(a, row, r, teacher, b, [&](int e) { return first[entry_slot[e]] == (uint32_t)e; });
     l.a = block_sum64<4>(l.a, slot);
     l.b = block_sum64<4>(l.b, slot);
+    if (rest) l.z = block_sum64<4>(l.z, slot);
+    const RowSums sums = row_sums(a, b, from > -INFINITY ? (double)from : b, l, z_rest);
     if (threadIdx.x == 0) {
-        if (a.loss) a.loss[row] = (float)row_loss(a, z, z_rest, l);
-        a.rows[row] = shared_grad = row_grad(a, b, z, z_rest, l);
+        if (a.loss) a.loss[row] = (float)row_loss(a, sums, l);
+        a.rows[row] = shared_grad = row_grad(a, sums, l);
     }
     __syncthreads();
     if (!a.grad) return;
@@ -549,7 +571,7 @@ __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
     __syncthreads();
     marks.set(a, at.group, listed[0]);
     __syncthreads();
-    Weight32 weight((float)a.rows[at.row].best, per);
+    Weight32 weight((float)a.rows[at.row].from, per);
     float other = a.rows[at.row].other;
     int turn = 0;
     for (int64_t block = start; block < end; ++block) {
@@ -578,7 +600,7 @@ __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
         }
         turn = next;
         if (block + 1 < end && at.row != here.row) {
-            weight = Weight32((float)a.rows[at.row].best, per);
+            weight = Weight32((float)a.rows[at.row].from, per);
             other = a.rows[at.row].other;
         }
         __syncthreads();
@@ -586,7 +608,7 @@ __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
 }
 
 // c: the context of a training step, whose launches are timed; null otherwise
-template <int DT, bool STEP>
+template <int DT, bool REST, bool STEP>
 void launch_rows(kge_ctx* c, const DistillArgs& a, hipStream_t st) {
     const int64_t n = a.in.n;
     const dim3 grid = flat_grid(a.in.rows);
@@ -594,19 +616,23 @@ void launch_rows(kge_ctx* c, const DistillArgs& a, hipStream_t st) {
         if (c) KGE_LAUNCH(c, kernel, grid, dim3(threads), 0, st, a);
         else hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a);
     };
-    if (n <= 256) go(k_distill<DT, 1, 1, STEP>, 64);
-    else if (n <= 1024) go(k_distill<DT, 4, 1, STEP>, 256);
-    else if (n <= 4096) go(k_distill<DT, 4, 4, STEP>, 256);
+    if (n <= 256) go(k_distill<DT, 1, 1, REST, STEP>, 64);
+    else if (n <= 1024) go(k_distill<DT, 4, 1, REST, STEP>, 256);
+    else if (n <= 4096) go(k_distill<DT, 4, 4, REST, STEP>, 256);
     // (us, 16 / 1024 / 4096 rows of 5000, by the kernel for 16,384 -> by this: 9.0 -> 7.5 / 23.9 -> 17.6 / 71 -> 55)
-    else if (n <= 8192) go(k_distill<DT, 8, 4, STEP>, 512);
+    else if (n <= 8192) go(k_distill<DT, 8, 4, REST, STEP>, 512);
     // (us, 16 / 256 / 4096 rows of 15,000, 1024 threads -> these 512: 9.4 -> 9.3 / 13.5 -> 11.9 / 168 -> 132)
-    else if (n <= 16384) go(k_distill<DT, 8, 8, STEP>, 512);
-    else go(k_distill<DT, 16, 8, STEP>, 1024);
+    else if (n <= 16384) go(k_distill<DT, 8, 8, REST, STEP>, 512);
+    else go(k_distill<DT, 16, 8, REST, STEP>, 1024);
 }
 
 template <int DT>
 void launch(const DistillArgs& a, hipStream_t st) {
-    if (a.groups == 0) { launch_rows<DT, false>(nullptr, a, st); return; }
+    if (a.groups == 0) {
+        if (a.t.lse) launch_rows<DT, true, false>(nullptr, a, st);
+        else launch_rows<DT, false, false>(nullptr, a, st);
+        return;
+    }
     const dim3 grid = flat_grid(pieces(a.in.rows * a.groups, a.per));
     k_distill_sums<DT><<<grid, 256, 0, st>>>(a);
     k_distill_finish<DT><<<flat_grid(a.in.rows), 256, 0, st>>>(a);
@@ -617,7 +643,7 @@ void launch(const DistillArgs& a, hipStream_t st) {
 
 int64_t kge_distill_workspace(int64_t rows, int64_t n) {
     if (n <= KGE_ROW_RESIDENT) return 0;
-    return up256(rows * pieces(n, GROUP) * 24) + up256(rows * (int64_t)sizeof(RowGrad));
+    return up256(rows * pieces(n, GROUP) * 16) + up256(rows * (int64_t)sizeof(RowGrad));
 }
 
 void kge_launch_distill(const RowScores& in, const TeacherLists& t, float grad_scale, float loss_scale, float* loss, void* grad, int64_t ld_grad,
@@ -630,14 +656,15 @@ void kge_launch_distill(const RowScores& in, const TeacherLists& t, float grad_s
     a.loss = loss; a.grad = grad; a.ld_grad = ld_grad;
     if (step) {
         a.step = *step;
-        launch_rows<KGE_F32, true>(step->c, a, st);
+        if (t.lse) launch_rows<KGE_F32, true, true>(step->c, a, st);
+        else launch_rows<KGE_F32, false, true>(step->c, a, st);
         return;
     }
     if (in.n > KGE_ROW_RESIDENT) {
         a.groups = pieces(in.n, GROUP);
         a.per = groups_per_workgroup(in.rows * a.groups);
         a.sums = static_cast<double*>(workspace);
-        a.rows = reinterpret_cast<RowGrad*>(static_cast<char*>(workspace) + up256(in.rows * a.groups * 24));
+        a.rows = reinterpret_cast<RowGrad*>(static_cast<char*>(workspace) + up256(in.rows * a.groups * 16));
     }
     if (in.dtype == KGE_F32) launch<KGE_F32>(a, st);
     else if (in.dtype == KGE_BF16) launch<KGE_BF16>(a, st);
