@@ -9,9 +9,9 @@
 // score u, w'_j = exp(z_j - u / T) and Z'_r = sum w' >= 1, wherever that matters: the gradient of these is c T [ P exp((u - max) / T) / Z - p_r / Z'_r ] w'_j.
 //
 // A row that a workgroup holds is read once and its gradient written once: the weights stay in registers between the sum and the gradient.
-// Long rows: a pass for the sums, one workgroup per row for what their gradients have in common, a second pass for the gradient.  A weight is
-// formed in 32 bits from an argument in 64; what is a difference of near values (logarithms of the loss, the rest) and all sums of weights are
-// in 64.
+// Long rows: a pass for the sums, one workgroup per row for what their gradients have in common, a second pass for the gradient.  Up to T = 4 a
+// weight is formed in 32 bits from an argument in 64, and four of them are added in 32; sums of these, weights of listed candidates where there is a rest,
+// logarithms and the rest are in 64.  Above that sums are of weights in 64 bits (see WIDE_TEMPERATURE).
 //
 // 1024 rows of 14,951 fp32, lists of 64 and a rest: 36 us, 3.4 TB/s read and written (a large copy: 24 us); the vector units work for 19, and the
 // phases of a row (reads, sums, list, writes) overlap only with those of two other rows on the CU.  16 rows of 2.5 M bf16, lists of 256 and a
@@ -87,10 +87,10 @@ struct Teacher {
     __device__ __forceinline__ double log_p(int e) const { return ((double)scores[e] - best) * inv_t - lse; }
 };
 
-struct ListSums { double a, b, z; };  // sum of p before it is scaled, sum of p * (log p - (s - best) / T), with a rest the weights of the list's candidates
+struct ListSums { double a, b, z; };  // sum of p before it is scaled, sum of p * (log p - (s - best) / T), MARKED: the weights of the list's candidates
 
 // A thread's part of the list's sums.  stands(e): the first entry of its candidate.
-template <int DT, int THREADS, typename S>
+template <int DT, int THREADS, bool MARKED, typename S>
 __device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, const RowAt<DT>& r, const Teacher& teacher, double best, const S& stands) {
     ListSums l = {0.0, 0.0, 0.0};
 #pragma unroll 1
@@ -100,7 +100,7 @@ __device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, 
         const double lp = teacher.log_p(e), p = exp(lp), x = ((double)r.at(id) - best) * a.inv_t;
         l.a += p;
         if (p > 0.0 || p != p) l.b += p * (lp - x);
-        if (a.t.lse && stands(e)) l.z += x < INFINITY ? exp(x) : __longlong_as_double(0x7FF8000000000000ll);  // (of +inf and NaN)
+        if (MARKED && stands(e)) l.z += x < INFINITY ? exp(x) : __longlong_as_double(0x7FF8000000000000ll);  // (of +inf and NaN)
     }
     return l;
 }
@@ -154,6 +154,81 @@ __device__ __forceinline__ double row_loss(const DistillArgs& a, const RowSums& 
     return loss * a.loss_scale;
 }
 
+// Above T = 4 weights are formed in 64 bits.  T^2 multiplies a divergence that is of the size of 1 / T^2 where student and teacher are near each other, and an error
+// in the logarithm of the sum of 32-bit weights, some 1e-8, with it.  The sums of p log(p / q), which are near 0, and of what is near 1 lose as much, so with delta_e =
+// log(p_e / q_e), the same for the rest, and sums of p and of q that are both 1:
+//     sum p delta = sum (p delta - p + q) = sum p (delta + expm1(-delta)),    P q - p = p expm1(-delta) + (P - 1) q
+// whose terms are all small of themselves: an error of delta, 2^-53 times the size of the logarithms in it, is multiplied with |p - q|.
+// Largest error of a loss beside the loss, 256 candidates all listed / 14,952 with lists of 64 and a rest, 32 bits -> 64: T = 4 2e-6 / 7e-8, T = 8 7e-6 / 4e-6 -> 6e-8
+// (half a step of fp32), T = 100 7e-4 -> 6e-8, T = 1000 8e-2 -> 6e-8.  us, 1024 rows of 256 / 14,951 with their gradient 7.8 -> 8.3 / 34 -> 45, 64 rows of 100,000 30 -> 33.
+constexpr float WIDE_TEMPERATURE = 4.f;
+struct WideRow {
+    double log_z, log_mass;  // of the student's weights, of the list's p before they are scaled
+    double excess, rest;     // P - 1; what the candidates that are not listed add to the loss / T^2
+    int live;
+};
+// p log(p / q) - p + q
+__device__ __forceinline__ double wide_term(double p, double delta, double q) {
+    return fabs(delta) < 1.0 ? p * (delta + expm1(-delta)) : (p > 0.0 || p != p ? p * delta : 0.0) - p + q;
+}
+__device__ __forceinline__ WideRow wide_row(const DistillArgs& a, const RowSums& s, const ListSums& l, RowGrad& g) {
+    WideRow w = {log(s.z), 0.0, 0.0, 0.0, 0};
+    double rest = 0.0;
+    if (a.t.lse) {
+        if (s.z_rest > 0.0) rest = fmax(1.0 - l.a, 0.0);
+        if (!(rest > 0.0)) w.excess = l.a - 1.0;
+    } else {
+        w.log_mass = log(l.a);
+    }
+    w.live = s.z != 0.0 && l.a + rest != 0.0;
+    const double q = s.z_rest > 0.0 ? s.z_rest * s.shift / s.z : s.z_rest, c = a.grad_scale;
+    g = {s.from, 1.0, 0.f, 0.f, 0.f};
+    if (rest > 0.0) {
+        const double delta = log(rest * s.z / s.z_rest) - (s.from - s.best) * a.inv_t;
+        w.rest = wide_term(rest, delta, q);
+        g.other = coefficient(fabs(delta) < 1.0 ? c * (rest / s.z_rest) * expm1(-delta) : c * (s.shift / s.z - rest / s.z_rest));
+    } else {
+        w.rest = w.excess + q;
+        if (w.live) g.other = coefficient(c * (1.0 + w.excess) * s.shift / s.z);
+    }
+    return w;
+}
+struct WideEntry {
+    double p, delta, q;
+    __device__ __forceinline__ WideEntry(const Teacher& teacher, const WideRow& w, int e, double x /* (s - best) / T */) {
+        const double lp = teacher.log_p(e) - w.log_mass;
+        delta = lp - x + w.log_z;
+        p = exp(lp);
+        q = exp(x - w.log_z);
+    }
+    __device__ __forceinline__ double grad(double excess) const {
+        return fabs(delta) < 1.0 ? p * expm1(-delta) + excess * q : (1.0 + excess) * q - p;
+    }
+};
+// What a list adds to the loss / T^2: a thread's part.  position(e): of an entry's candidate, -1 if it is not used.  (The q of a candidate is counted once.)
+template <int THREADS, typename R, typename P, typename S>
+__device__ __forceinline__ double wide_list(const DistillArgs& a, const R& r, const Teacher& teacher, double best, const WideRow& w, const P& position, const S& stands) {
+    double sum = 0.0;
+#pragma unroll 1
+    for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
+        const int64_t at = position(e);
+        if (at < 0) continue;
+        const WideEntry x(teacher, w, e, ((double)r.at(at) - best) * a.inv_t);
+        sum += wide_term(x.p, x.delta, x.q) - (stands(e) ? 0.0 : x.q);
+    }
+    return sum;
+}
+// A listed candidate's gradient by its first entry e; repeated: there are more of them.
+template <typename R, typename P>
+__device__ __forceinline__ double wide_grad(const DistillArgs& a, const R& r, const Teacher& teacher, double best, const WideRow& w, const P& position, int e, int64_t at, bool repeated) {
+    if (!w.live) return 0.0;
+    const WideEntry x(teacher, w, e, ((double)r.at(at) - best) * a.inv_t);
+    double sum = x.grad(w.excess);
+    if (repeated)
+        for (int y = e + 1; y < a.t.m; ++y) if (position(y) == at) sum -= exp(teacher.log_p(y) - w.log_mass);
+    return a.grad_scale * sum;
+}
+
 // Gradients j .. j + 3 of a row of n, but those of candidates whose bit is set.
 template <int DT>
 __device__ __forceinline__ void store_unlisted(typename Score<DT>::type* row, int64_t j, int64_t n, const float v[4], uint32_t bits) {
@@ -173,16 +248,21 @@ __device__ __forceinline__ void store_unlisted(typename Score<DT>::type* row, in
     }
 }
 
-// REST: the teacher's log-sum-exp is given.  (Rows of 16,384 with a rest: 126 registers and 4 waves per SIMD; at 6, 31 are spilled and 1024 rows of 14,951 take 54 us
-// instead of 42.)
-template <int DT, int WAVES, int TPW, bool REST, bool STEP>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? (REST ? 4 : 6) : 1) void k_distill(DistillArgs a) {
+enum { LISTS, REST, WIDE };  // the lists are all there is; the teacher's log-sum-exp is given; either, T > WIDE_TEMPERATURE
+// Waves per SIMD that the registers are cut to.  (Rows of 16,384 with a rest: 126 registers at 4; at 6, 31 are spilled and 1024 rows of 14,951 take 54 us instead
+// of 42.  Of lists alone 80 at 6, for three rows on a CU instead of two.)
+constexpr int distill_waves(int waves, int tpw, int mode, bool step) { return waves != 8 ? 1 : tpw == 8 ? (mode == LISTS ? 6 : 4) : mode == LISTS && !step ? 6 : 1; }
+
+template <int DT, int WAVES, int TPW, int MODE, bool STEP>
+__global__ __launch_bounds__(WAVES * 64, distill_waves(WAVES, TPW, MODE, STEP)) void k_distill(DistillArgs a) {
     constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64, N = TPW * 4;
+    constexpr bool MARKED = MODE != LISTS;  // the list's candidates have no part in the sum over the row
     __shared__ uint32_t listed[CAP / 32];  // a bit per candidate
     __shared__ int32_t list_at[KGE_TOP_MAX];
     __shared__ float maxima[3][WAVES];
     __shared__ double parts[4][WAVES];
     __shared__ RowGrad shared_grad;
+    __shared__ WideRow shared_wide;
     __shared__ int twice;  // a candidate is listed more than once
     const int64_t row = flat_block();
     if (row >= a.in.rows) return;
@@ -233,9 +313,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? (REST ? 4 : 6)
     }
     best = scalar(best);
     const Teacher teacher(a, row, scalar(list_best));
-    // With a rest the list's candidates have no part in the registers' weights, which are relative to the best of the others.
+    // The registers' weights are relative to the best of what has a part in their sum.
     float from = best;
-    if constexpr (REST) {
+    if constexpr (MARKED) {
         uint32_t bits[(TPW + 7) / 8] = {};  // of the registers, in their order
 #pragma unroll
         for (int i = 0; i < TPW; ++i) bits[i / 8] |= (listed[((i * WAVES + wave) * 256 + lane * 4) >> 5] >> (lane * 4 & 31) & 15u) << i % 8 * 4;
@@ -259,12 +339,22 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? (REST ? 4 : 6)
     const Weight32 relative(from, per);
     double z = 0.0;
     forget<N>(v);
+    if constexpr (MODE == WIDE) {  // (the registers keep the scores)
+        const Scale scale(a.inv_t);
+        const Weights wide(from, scale);
 #pragma unroll
-    for (int i = 0; i < TPW; ++i) {
+        for (int q = 0; q < N; ++q) {
+            z += wide.of(v[q]);
+            if (q % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
 #pragma unroll
-        for (int q = 4 * i; q < 4 * i + 4; ++q) v[q] = relative.of(v[q]);
-        z += (double)((v[4 * i] + v[4 * i + 1]) + (v[4 * i + 2] + v[4 * i + 3]));
-        __builtin_amdgcn_sched_barrier(0);  // (tile by tile: the 64-bit halves of all weights at once would not fit the registers)
+        for (int i = 0; i < TPW; ++i) {
+#pragma unroll
+            for (int q = 4 * i; q < 4 * i + 4; ++q) v[q] = relative.of(v[q]);
+            z += (double)((v[4 * i] + v[4 * i + 1]) + (v[4 * i + 2] + v[4 * i + 3]));
+            __builtin_amdgcn_sched_barrier(0);  // (tile by tile: the 64-bit halves of all weights at once would not fit the registers)
+        }
     }
     forget<N>(v);
     auto stands = [&](int e) {
@@ -276,10 +366,10 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? (REST ? 4 : 6)
     ListSums l = {0.0, 0.0, 0.0};
     z = wave_sum64(z);
     if (wave * 64 < a.t.m) {
-        l = sum_list<DT, THREADS>(a, row, r, teacher, weight.best, stands);
+        l = sum_list<DT, THREADS, MARKED>(a, row, r, teacher, weight.best, stands);
         l.a = wave_sum64(l.a);
         l.b = wave_sum64(l.b);
-        if constexpr (REST) l.z = wave_sum64(l.z);
+        if constexpr (MARKED) l.z = wave_sum64(l.z);
     }
     if (lane == 0) { parts[0][wave] = z; parts[1][wave] = l.z; parts[2][wave] = l.a; parts[3][wave] = l.b; }
     __syncthreads();
@@ -290,10 +380,20 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? (REST ? 4 : 6)
         l = {sum[2], sum[3], sum[1]};
         const RowSums sums = row_sums(a, weight.best, relative.best, l, best == INFINITY ? __longlong_as_double(0x7FF8000000000000ll) : sum[0]);
         if (lane == 0) {
-            if (a.loss) a.loss[row] = (float)row_loss(a, sums, l);
+            if constexpr (MODE == WIDE) {
+                shared_wide = wide_row(a, sums, l, shared_grad);
+            } else {
+                if (a.loss) a.loss[row] = (float)row_loss(a, sums, l);
+                shared_grad = row_grad(a, sums, l);
+            }
             if constexpr (STEP) a.step.cpos[row] = 0.f;
-            shared_grad = row_grad(a, sums, l);
         }
+    }
+    auto position = [&](int e) { return (int64_t)list_at[e]; };
+    if (MODE == WIDE && a.loss) {
+        __syncthreads();
+        const double sum = block_sum64<WAVES>(wide_list<THREADS>(a, r, teacher, weight.best, shared_wide, position, stands), parts[0]);
+        if (threadIdx.x == 0) a.loss[row] = shared_wide.live ? (float)((sum + shared_wide.rest) * a.loss_scale) : 0.f;
     }
     if (!a.grad) return;
     __syncthreads();
@@ -312,14 +412,20 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? (REST ? 4 : 6)
     for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
         const int at = list_at[e];
         if (at < 0) continue;
-        auto p_of = [&](int x) { return exp(teacher.log_p(x)) * g.scale; };
         if (!stands(e)) continue;
-        double p = p_of(e);
-        if (twice) {
-            for (int x = e + 1; x < a.t.m; ++x) if (list_at[x] == at) p += p_of(x);
-        }
         const float raw = widen<DT>(r.s[at]);
-        out[at] = narrow<DT>(shape(fmaf(weight.of(r.of(raw)), g.listed, -(float)p * g.unit), raw));
+        float x;
+        if constexpr (MODE == WIDE) {
+            x = (float)wide_grad(a, r, teacher, weight.best, shared_wide, position, e, at, twice != 0);
+        } else {
+            auto p_of = [&](int x) { return exp(teacher.log_p(x)) * g.scale; };
+            double p = p_of(e);
+            if (twice) {
+                for (int y = e + 1; y < a.t.m; ++y) if (list_at[y] == at) p += p_of(y);
+            }
+            x = fmaf(weight.of(r.of(raw)), g.listed, -(float)p * g.unit);
+        }
+        out[at] = narrow<DT>(shape(x, raw));
     }
 #pragma unroll
     for (int i = 0; i < TPW; ++i) {
@@ -331,7 +437,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? (REST ? 4 : 6)
             again.template values<false>(tile, r.n, raw);
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) x[q] = shape(v[4 * i + q] * g.other, raw[q]);
+        for (int q = 0; q < 4; ++q) x[q] = shape((MODE == WIDE ? relative.of(v[4 * i + q]) : v[4 * i + q]) * g.other, raw[q]);
         if (at < r.n) store_unlisted<DT>(out, at, r.n, x, listed[at >> 5] >> (at & 31) & 15u);
         if constexpr (STEP) __builtin_amdgcn_sched_barrier(0);
     }
@@ -373,7 +479,7 @@ __device__ __forceinline__ uint32_t marks_of(const uint32_t* bits, int p) { retu
 
 // Sums of the weights of a workgroup's part of a row, noted with its last group; its other groups note none.  A wave adds up relative to a score of
 // its own, the best of the first scores it meets, and takes another one only when a score lies 2^40 above (in weights).
-template <int DT>
+template <int DT, bool WIDE_SUMS>
 __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
     __shared__ uint32_t listed[3][GROUP_WORDS];
     __shared__ double parts[2][4];
@@ -384,7 +490,8 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
     at.group = start - at.row * a.groups;
     const auto* scores = static_cast<const typename Score<DT>::type*>(a.in.p);
     const double per = a.inv_t * 1.4426950408889634;
-    const bool rest = a.t.lse != nullptr;
+    const bool rest = WIDE_SUMS || a.t.lse;
+    const Scale scale(a.inv_t);
     Quad<DT> x[4];
     auto load = [&](const GroupWalk& w) {
 #pragma unroll
@@ -440,11 +547,20 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
                 weight = Weight32(base, per);
             }
         }
+        if constexpr (WIDE_SUMS) {
+            const Weights wide(base, scale);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float four = (weight.of(v[4 * i]) + weight.of(v[4 * i + 1])) + (weight.of(v[4 * i + 2]) + weight.of(v[4 * i + 3]));
-            z += (double)four;
-            __builtin_amdgcn_sched_barrier(0);
+            for (int q = 0; q < 16; ++q) {
+                z += wide.of(v[q]);
+                if (q % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float four = (weight.of(v[4 * i]) + weight.of(v[4 * i + 1])) + (weight.of(v[4 * i + 2]) + weight.of(v[4 * i + 3]));
+                z += (double)four;
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         turn = next;
         const bool last = block + 1 == end || at.row != here.row;
@@ -475,7 +591,7 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
 
 // A row's loss, what its gradients have in common, and the gradients of its listed candidates: k_distill_grad leaves these out, and what it reads in
 // their place (where gradients replace the scores) does not matter to it.
-template <int DT>
+template <int DT, bool WIDE_SUMS>
 __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     constexpr int SLOTS = 2 * KGE_TOP_MAX;
     __shared__ double slot[4];
@@ -483,6 +599,7 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     __shared__ uint32_t key[SLOTS], first[SLOTS], times[SLOTS];  // candidates of the list, its first entry and their number
     __shared__ uint16_t entry_slot[KGE_TOP_MAX];
     __shared__ RowGrad shared_grad;
+    __shared__ WideRow shared_wide;
     const int64_t row = flat_block();
     if (row >= a.in.rows) return;
     RowAt<DT> r;
@@ -490,7 +607,7 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     r.n = a.in.n; r.is_dist = false; r.gamma = 0.f;
     const double* p = a.sums + 2 * row * a.groups;
     const double per = a.inv_t * 1.4426950408889634;
-    const bool rest = a.t.lse != nullptr;
+    const bool rest = WIDE_SUMS || a.t.lse;
     constexpr uint32_t NONE = 0xFFFFFFFFu;  // (not a position: rows have fewer than 2^32 candidates)
     for (int x = threadIdx.x; x < SLOTS; x += 256) { key[x] = NONE; first[x] = NONE; times[x] = 0; }
     float from = -INFINITY, list_best = -INFINITY, listed_best = -INFINITY;  // best of what the sums are of, of the teacher's scores, of the student's in the list
@@ -521,14 +638,26 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
         if (p[2 * g + 1] != 0.0) z_rest += p[2 * g + 1] * (p[2 * g] == (double)from ? 1.0 : exp2((p[2 * g] - (double)from) * per));
     z_rest = block_sum64<4>(z_rest, slot);
     const Teacher teacher(a, row, list_best);
-    ListSums l = sum_list<DT, 256>(a, row, r, teacher, b, [&](int e) { return first[entry_slot[e]] == (uint32_t)e; });
+    auto stands = [&](int e) { return first[entry_slot[e]] == (uint32_t)e; };
+    ListSums l = rest ? sum_list<DT, 256, true>(a, row, r, teacher, b, stands) : sum_list<DT, 256, false>(a, row, r, teacher, b, stands);
     l.a = block_sum64<4>(l.a, slot);
     l.b = block_sum64<4>(l.b, slot);
     if (rest) l.z = block_sum64<4>(l.z, slot);
     const RowSums sums = row_sums(a, b, from > -INFINITY ? (double)from : b, l, z_rest);
     if (threadIdx.x == 0) {
-        if (a.loss) a.loss[row] = (float)row_loss(a, sums, l);
-        a.rows[row] = shared_grad = row_grad(a, sums, l);
+        if constexpr (WIDE_SUMS) {
+            shared_wide = wide_row(a, sums, l, shared_grad);
+        } else {
+            if (a.loss) a.loss[row] = (float)row_loss(a, sums, l);
+            shared_grad = row_grad(a, sums, l);
+        }
+        a.rows[row] = shared_grad;
+    }
+    auto position = [&](int e) { return entry_slot[e] == 0xFFFF ? (int64_t)-1 : (int64_t)key[entry_slot[e]]; };
+    if (WIDE_SUMS && a.loss) {
+        __syncthreads();
+        const double sum = block_sum64<4>(wide_list<256>(a, r, teacher, b, shared_wide, position, stands), slot);
+        if (threadIdx.x == 0) a.loss[row] = shared_wide.live ? (float)((sum + shared_wide.rest) * a.loss_scale) : 0.f;
     }
     __syncthreads();
     if (!a.grad) return;
@@ -538,14 +667,18 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     for (int e = threadIdx.x; e < a.t.m; e += 256) {
         const uint32_t x = entry_slot[e];
         if (x == 0xFFFF || first[x] != (uint32_t)e) continue;
-        double sum = exp(teacher.log_p(e));
-        uint32_t left = times[x] - 1;
-        for (int y = e + 1; left; ++y) {
-            if (entry_slot[y] != x) continue;
-            sum += exp(teacher.log_p(y));
-            --left;
+        if constexpr (WIDE_SUMS) {
+            out[key[x]] = narrow<DT>((float)wide_grad(a, r, teacher, b, shared_wide, position, e, key[x], times[x] > 1));
+        } else {
+            double sum = exp(teacher.log_p(e));
+            uint32_t left = times[x] - 1;
+            for (int y = e + 1; left; ++y) {
+                if (entry_slot[y] != x) continue;
+                sum += exp(teacher.log_p(y));
+                --left;
+            }
+            out[key[x]] = narrow<DT>(fmaf(weight.of(r.at(key[x])), g.listed, -(float)(sum * g.scale) * g.unit));
         }
-        out[key[x]] = narrow<DT>(fmaf(weight.of(r.at(key[x])), g.listed, -(float)(sum * g.scale) * g.unit));
     }
 }
 
@@ -608,7 +741,7 @@ __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
 }
 
 // c: the context of a training step, whose launches are timed; null otherwise
-template <int DT, bool REST, bool STEP>
+template <int DT, int MODE, bool STEP>
 void launch_rows(kge_ctx* c, const DistillArgs& a, hipStream_t st) {
     const int64_t n = a.in.n;
     const dim3 grid = flat_grid(a.in.rows);
@@ -616,26 +749,33 @@ void launch_rows(kge_ctx* c, const DistillArgs& a, hipStream_t st) {
         if (c) KGE_LAUNCH(c, kernel, grid, dim3(threads), 0, st, a);
         else hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a);
     };
-    if (n <= 256) go(k_distill<DT, 1, 1, REST, STEP>, 64);
-    else if (n <= 1024) go(k_distill<DT, 4, 1, REST, STEP>, 256);
-    else if (n <= 4096) go(k_distill<DT, 4, 4, REST, STEP>, 256);
+    if (n <= 256) go(k_distill<DT, 1, 1, MODE, STEP>, 64);
+    else if (n <= 1024) go(k_distill<DT, 4, 1, MODE, STEP>, 256);
+    else if (n <= 4096) go(k_distill<DT, 4, 4, MODE, STEP>, 256);
     // (us, 16 / 1024 / 4096 rows of 5000, by the kernel for 16,384 -> by this: 9.0 -> 7.5 / 23.9 -> 17.6 / 71 -> 55)
-    else if (n <= 8192) go(k_distill<DT, 8, 4, REST, STEP>, 512);
+    else if (n <= 8192) go(k_distill<DT, 8, 4, MODE, STEP>, 512);
     // (us, 16 / 256 / 4096 rows of 15,000, 1024 threads -> these 512: 9.4 -> 9.3 / 13.5 -> 11.9 / 168 -> 132)
-    else if (n <= 16384) go(k_distill<DT, 8, 8, REST, STEP>, 512);
-    else go(k_distill<DT, 16, 8, REST, STEP>, 1024);
+    else if (n <= 16384) go(k_distill<DT, 8, 8, MODE, STEP>, 512);
+    else go(k_distill<DT, 16, 8, MODE, STEP>, 1024);
 }
 
 template <int DT>
 void launch(const DistillArgs& a, hipStream_t st) {
+    const bool wide = a.t.temperature > WIDE_TEMPERATURE;
     if (a.groups == 0) {
-        if (a.t.lse) launch_rows<DT, true, false>(nullptr, a, st);
-        else launch_rows<DT, false, false>(nullptr, a, st);
+        if (wide) launch_rows<DT, WIDE, false>(nullptr, a, st);
+        else if (a.t.lse) launch_rows<DT, REST, false>(nullptr, a, st);
+        else launch_rows<DT, LISTS, false>(nullptr, a, st);
         return;
     }
-    const dim3 grid = flat_grid(pieces(a.in.rows * a.groups, a.per));
-    k_distill_sums<DT><<<grid, 256, 0, st>>>(a);
-    k_distill_finish<DT><<<flat_grid(a.in.rows), 256, 0, st>>>(a);
+    const dim3 grid = flat_grid(pieces(a.in.rows * a.groups, a.per)), rows = flat_grid(a.in.rows);
+    if (wide) {
+        k_distill_sums<DT, true><<<grid, 256, 0, st>>>(a);
+        k_distill_finish<DT, true><<<rows, 256, 0, st>>>(a);
+    } else {
+        k_distill_sums<DT, false><<<grid, 256, 0, st>>>(a);
+        k_distill_finish<DT, false><<<rows, 256, 0, st>>>(a);
+    }
     if (a.grad) k_distill_grad<DT><<<grid, 256, 0, st>>>(a);
 }
 
@@ -656,8 +796,9 @@ void kge_launch_distill(const RowScores& in, const TeacherLists& t, float grad_s
     a.loss = loss; a.grad = grad; a.ld_grad = ld_grad;
     if (step) {
         a.step = *step;
-        if (t.lse) launch_rows<KGE_F32, true, true>(step->c, a, st);
-        else launch_rows<KGE_F32, false, true>(step->c, a, st);
+        if (t.temperature > WIDE_TEMPERATURE) launch_rows<KGE_F32, WIDE, true>(step->c, a, st);
+        else if (t.lse) launch_rows<KGE_F32, REST, true>(step->c, a, st);
+        else launch_rows<KGE_F32, LISTS, true>(step->c, a, st);
         return;
     }
     if (in.n > KGE_ROW_RESIDENT) {
