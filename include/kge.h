@@ -330,7 +330,8 @@ int kge_sample_scores(const void* scores, int32_t dtype, int64_t rows, int64_t n
  * (with the same pitch) and must not overlap it otherwise.  -inf marks a candidate that is masked: q = 0, gradient 0 unless it is
  * listed.  A row with no candidate, or with no entry in use, has loss 0 and gradient 0; so has a rest without a candidate it could
  * belong to.  NaN and +inf make the row's loss and gradient NaN.
- * Up to T = 4 the weights exp(s / T) are formed in 32 bits: a loss is off by some 1e-8 T^2 beside its rounding.  Above that in 64 bits: by some 1e-13 T.
+ * Up to T = 4 the weights of candidates that are not listed are formed in 32 bits, which moves a loss by some 1e-8 of itself and of T
+ * beside its rounding; above that in 64 bits: by some 1e-13.
  */
 int64_t kge_distill_loss_workspace(int64_t rows, int64_t n);
 int kge_distill_loss(const void* scores, int32_t dtype, int64_t rows, int64_t n, int64_t ld,

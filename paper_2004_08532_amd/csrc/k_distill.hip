@@ -6,12 +6,12 @@
 //     grad_j = c T [ P - p_r Z / Z_r ] q_j             candidates that are not listed, where there is a rest
 // p_r = 1 - sum p is the mass that the teacher has outside of the list, q_r = Z_r / Z the student's, P = sum p + p_r.
 // Z_r can be less than any number where the listed candidates lie far above the others.  So what is not listed has weights relative to its own best
-// score u, w'_j = exp(z_j - u / T) and Z'_r = sum w' >= 1, wherever that matters: the gradient of these is c T [ P exp((u - max) / T) / Z - p_r / Z'_r ] w'_j.
+// score u, w'_j = exp(z_j - u / T) and Z'_r = sum w' >= 1: the gradient of these is c T [ P exp((u - max) / T) / Z - p_r / Z'_r ] w'_j.
 //
 // A row that a workgroup holds is read once and its gradient written once: the weights stay in registers between the sum and the gradient.
-// Long rows: a pass for the sums, one workgroup per row for what their gradients have in common, a second pass for the gradient.  Up to T = 4 a
-// weight is formed in 32 bits from an argument in 64, and four of them are added in 32; sums of these, weights of listed candidates where there is a rest,
-// logarithms and the rest are in 64.  Above that sums are of weights in 64 bits (see WIDE_TEMPERATURE).
+// Long rows: a pass for the sums, one workgroup per row for what their gradients have in common, a second pass for the gradient.  Weights of listed
+// candidates are formed in 64 bits (but for the sum of a long row without a rest); up to T = 4 those of the others in 32 bits from an argument in 64, four of them
+// added in 32.  All other sums and logarithms are in 64.
 //
 // 1024 rows of 14,951 fp32, lists of 64 and a rest: 36 us, 3.4 TB/s read and written (a large copy: 24 us); the vector units work for 19, and the
 // phases of a row (reads, sums, list, writes) overlap only with those of two other rows on the CU.  16 rows of 2.5 M bf16, lists of 256 and a
@@ -24,8 +24,8 @@ namespace {
 // What the gradients of a row have in common: of listed candidates w_j * listed - p * unit, with w relative to the row's best score and p_e =
 // exp(Teacher::log_p) * scale; of the others w_j * other, with w relative to `from`.
 struct RowGrad {
-    double from, scale;
-    float listed, other, unit;
+    double from, scale, listed, unit;
+    float other;
 };
 
 struct DistillArgs {
@@ -87,7 +87,7 @@ struct Teacher {
     __device__ __forceinline__ double log_p(int e) const { return ((double)scores[e] - best) * inv_t - lse; }
 };
 
-struct ListSums { double a, b, z; };  // sum of p before it is scaled, sum of p * (log p - (s - best) / T), MARKED: the weights of the list's candidates
+struct ListSums { double a, b, z; };  // sum of p before it is scaled, sum of p * (log p - (s - best) / T), MARKED: of the weights of the list's candidates
 
 // A thread's part of the list's sums.  stands(e): the first entry of its candidate.
 template <int DT, int THREADS, bool MARKED, typename S>
@@ -130,13 +130,13 @@ __device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, const RowSums&
         scale = mass > 0.0 || mass != mass ? 1.0 / mass : 0.0;
         mass *= scale;
     }
-    RowGrad g = {s.from, scale, 0.f, 0.f, 0.f};
+    RowGrad g = {s.from, scale, 0.0, 0.0, 0.f};
     const double c = a.grad_scale;
     if (s.z != 0.0 && mass + rest != 0.0) {
         const double own = c * (mass + rest) / s.z;
-        g.listed = coefficient(own);
-        g.other = rest > 0.0 ? coefficient(own * s.shift - c * rest / s.z_rest) : s.z_rest > 0.0 ? coefficient(own * s.shift) : g.listed;
-        g.unit = coefficient(c);
+        g.listed = own;
+        g.other = rest > 0.0 ? coefficient(own * s.shift - c * rest / s.z_rest) : s.z_rest > 0.0 ? coefficient(own * s.shift) : coefficient(own);
+        g.unit = c;
     }
     return g;
 }
@@ -154,13 +154,14 @@ __device__ __forceinline__ double row_loss(const DistillArgs& a, const RowSums& 
     return loss * a.loss_scale;
 }
 
-// Above T = 4 weights are formed in 64 bits.  T^2 multiplies a divergence that is of the size of 1 / T^2 where student and teacher are near each other, and an error
-// in the logarithm of the sum of 32-bit weights, some 1e-8, with it.  The sums of p log(p / q), which are near 0, and of what is near 1 lose as much, so with delta_e =
-// log(p_e / q_e), the same for the rest, and sums of p and of q that are both 1:
+// Above T = 4 the weights of candidates that are not listed are formed in 64 bits, too.  An error e of their sum's logarithm is multiplied with |p_r - q_r|, which falls as
+// 1 / T, and the divergence that T^2 multiplies falls as 1 / T^2 where student and teacher are near each other: the loss is off by e T of itself, and e is some 1e-8 in
+// 32 bits.  The sums of p log(p / q), which are near 0, and of what is near 1 lose bits in the same way, so with delta_e = log(p_e / q_e), the same for the rest,
+// and sums of p and of q that are both 1:
 //     sum p delta = sum (p delta - p + q) = sum p (delta + expm1(-delta)),    P q - p = p expm1(-delta) + (P - 1) q
 // whose terms are all small of themselves: an error of delta, 2^-53 times the size of the logarithms in it, is multiplied with |p - q|.
-// Largest error of a loss beside the loss, 256 candidates all listed / 14,952 with lists of 64 and a rest, 32 bits -> 64: T = 4 2e-6 / 7e-8, T = 8 7e-6 / 4e-6 -> 6e-8
-// (half a step of fp32), T = 100 7e-4 -> 6e-8, T = 1000 8e-2 -> 6e-8.  us, 1024 rows of 256 / 14,951 with their gradient 7.8 -> 8.3 / 34 -> 45, 64 rows of 100,000 30 -> 33.
+// Largest error of a loss beside the loss, 14,952 candidates, lists of 64 and a rest, 32 bits -> 64: T = 4 7e-8 (half a step of fp32 is 6e-8), T = 8 9e-8 -> 5e-8, T = 100
+// 5e-7 -> 5e-8, T = 1000 8e-6 -> 5e-8.  us, 1024 rows of 256 / 14,951 with their gradient 7.8 -> 8.3 / 34 -> 45, 64 rows of 100,000 30 -> 33.
 constexpr float WIDE_TEMPERATURE = 4.f;
 struct WideRow {
     double log_z, log_mass;  // of the student's weights, of the list's p before they are scaled
@@ -182,7 +183,7 @@ __device__ __forceinline__ WideRow wide_row(const DistillArgs& a, const RowSums&
     }
     w.live = s.z != 0.0 && l.a + rest != 0.0;
     const double q = s.z_rest > 0.0 ? s.z_rest * s.shift / s.z : s.z_rest, c = a.grad_scale;
-    g = {s.from, 1.0, 0.f, 0.f, 0.f};
+    g = {s.from, 1.0, 0.0, 0.0, 0.f};
     if (rest > 0.0) {
         const double delta = log(rest * s.z / s.z_rest) - (s.from - s.best) * a.inv_t;
         w.rest = wide_term(rest, delta, q);
@@ -248,15 +249,10 @@ __device__ __forceinline__ void store_unlisted(typename Score<DT>::type* row, in
     }
 }
 
-enum { LISTS, REST, WIDE };  // the lists are all there is; the teacher's log-sum-exp is given; either, T > WIDE_TEMPERATURE
-// Waves per SIMD that the registers are cut to.  (Rows of 16,384 with a rest: 126 registers at 4; at 6, 31 are spilled and 1024 rows of 14,951 take 54 us instead
-// of 42.  Of lists alone 80 at 6, for three rows on a CU instead of two.)
-constexpr int distill_waves(int waves, int tpw, int mode, bool step) { return waves != 8 ? 1 : tpw == 8 ? (mode == LISTS ? 6 : 4) : mode == LISTS && !step ? 6 : 1; }
-
-template <int DT, int WAVES, int TPW, int MODE, bool STEP>
-__global__ __launch_bounds__(WAVES * 64, distill_waves(WAVES, TPW, MODE, STEP)) void k_distill(DistillArgs a) {
+// (Rows of 16,384: 123 registers at 4 waves per SIMD; at 6, 31 are spilled and 1024 rows of 14,951 take 54 us instead of 42.)
+template <int DT, int WAVES, int TPW, bool WIDE, bool STEP>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? 4 : 1) void k_distill(DistillArgs a) {
     constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64, N = TPW * 4;
-    constexpr bool MARKED = MODE != LISTS;  // the list's candidates have no part in the sum over the row
     __shared__ uint32_t listed[CAP / 32];  // a bit per candidate
     __shared__ int32_t list_at[KGE_TOP_MAX];
     __shared__ float maxima[3][WAVES];
@@ -313,13 +309,12 @@ __global__ __launch_bounds__(WAVES * 64, distill_waves(WAVES, TPW, MODE, STEP)) 
     }
     best = scalar(best);
     const Teacher teacher(a, row, scalar(list_best));
-    // The registers' weights are relative to the best of what has a part in their sum.
-    float from = best;
-    if constexpr (MARKED) {
+    // The list's candidates have no part in the registers' weights, which are relative to the best of the others.
+    float from = -INFINITY;
+    {
         uint32_t bits[(TPW + 7) / 8] = {};  // of the registers, in their order
 #pragma unroll
         for (int i = 0; i < TPW; ++i) bits[i / 8] |= (listed[((i * WAVES + wave) * 256 + lane * 4) >> 5] >> (lane * 4 & 31) & 15u) << i % 8 * 4;
-        from = -INFINITY;
 #pragma unroll
         for (int q = 0; q < N; ++q) {
             const int mask = __builtin_amdgcn_sbfe((int)bits[q / 32], q % 32, 1);  // (-1: listed)
@@ -339,7 +334,7 @@ __global__ __launch_bounds__(WAVES * 64, distill_waves(WAVES, TPW, MODE, STEP)) 
     const Weight32 relative(from, per);
     double z = 0.0;
     forget<N>(v);
-    if constexpr (MODE == WIDE) {  // (the registers keep the scores)
+    if constexpr (WIDE) {  // (the registers keep the scores)
         const Scale scale(a.inv_t);
         const Weights wide(from, scale);
 #pragma unroll
@@ -362,14 +357,14 @@ __global__ __launch_bounds__(WAVES * 64, distill_waves(WAVES, TPW, MODE, STEP)) 
         if (twice) for (int x = 0; x < e; ++x) first = first && list_at[x] != list_at[e];
         return first;
     };
-    const Weight32 weight(best, per);
+    const double top = fabsf(best) < INFINITY ? (double)best : 0.0;
     ListSums l = {0.0, 0.0, 0.0};
     z = wave_sum64(z);
     if (wave * 64 < a.t.m) {
-        l = sum_list<DT, THREADS, MARKED>(a, row, r, teacher, weight.best, stands);
+        l = sum_list<DT, THREADS, true>(a, row, r, teacher, top, stands);
         l.a = wave_sum64(l.a);
         l.b = wave_sum64(l.b);
-        if constexpr (MARKED) l.z = wave_sum64(l.z);
+        l.z = wave_sum64(l.z);
     }
     if (lane == 0) { parts[0][wave] = z; parts[1][wave] = l.z; parts[2][wave] = l.a; parts[3][wave] = l.b; }
     __syncthreads();
@@ -378,9 +373,9 @@ __global__ __launch_bounds__(WAVES * 64, distill_waves(WAVES, TPW, MODE, STEP)) 
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum[k] = wave_sum64(lane < WAVES ? parts[k][lane] : 0.0);
         l = {sum[2], sum[3], sum[1]};
-        const RowSums sums = row_sums(a, weight.best, relative.best, l, best == INFINITY ? __longlong_as_double(0x7FF8000000000000ll) : sum[0]);
+        const RowSums sums = row_sums(a, top, relative.best, l, best == INFINITY ? __longlong_as_double(0x7FF8000000000000ll) : sum[0]);
         if (lane == 0) {
-            if constexpr (MODE == WIDE) {
+            if constexpr (WIDE) {
                 shared_wide = wide_row(a, sums, l, shared_grad);
             } else {
                 if (a.loss) a.loss[row] = (float)row_loss(a, sums, l);
@@ -390,9 +385,9 @@ __global__ __launch_bounds__(WAVES * 64, distill_waves(WAVES, TPW, MODE, STEP)) 
         }
     }
     auto position = [&](int e) { return (int64_t)list_at[e]; };
-    if (MODE == WIDE && a.loss) {
+    if (WIDE && a.loss) {
         __syncthreads();
-        const double sum = block_sum64<WAVES>(wide_list<THREADS>(a, r, teacher, weight.best, shared_wide, position, stands), parts[0]);
+        const double sum = block_sum64<WAVES>(wide_list<THREADS>(a, r, teacher, top, shared_wide, position, stands), parts[0]);
         if (threadIdx.x == 0) a.loss[row] = shared_wide.live ? (float)((sum + shared_wide.rest) * a.loss_scale) : 0.f;
     }
     if (!a.grad) return;
@@ -415,15 +410,15 @@ __global__ __launch_bounds__(WAVES * 64, distill_waves(WAVES, TPW, MODE, STEP)) 
         if (!stands(e)) continue;
         const float raw = widen<DT>(r.s[at]);
         float x;
-        if constexpr (MODE == WIDE) {
-            x = (float)wide_grad(a, r, teacher, weight.best, shared_wide, position, e, at, twice != 0);
+        if constexpr (WIDE) {
+            x = (float)wide_grad(a, r, teacher, top, shared_wide, position, e, at, twice != 0);
         } else {
             auto p_of = [&](int x) { return exp(teacher.log_p(x)) * g.scale; };
             double p = p_of(e);
             if (twice) {
                 for (int y = e + 1; y < a.t.m; ++y) if (list_at[y] == at) p += p_of(y);
             }
-            x = fmaf(weight.of(r.of(raw)), g.listed, -(float)p * g.unit);
+            x = (float)(exp(((double)r.of(raw) - top) * a.inv_t) * g.listed - p * g.unit);
         }
         out[at] = narrow<DT>(shape(x, raw));
     }
@@ -437,7 +432,7 @@ __global__ __launch_bounds__(WAVES * 64, distill_waves(WAVES, TPW, MODE, STEP)) 
             again.template values<false>(tile, r.n, raw);
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) x[q] = shape((MODE == WIDE ? relative.of(v[4 * i + q]) : v[4 * i + q]) * g.other, raw[q]);
+        for (int q = 0; q < 4; ++q) x[q] = shape((WIDE ? relative.of(v[4 * i + q]) : v[4 * i + q]) * g.other, raw[q]);
         if (at < r.n) store_unlisted<DT>(out, at, r.n, x, listed[at >> 5] >> (at & 31) & 15u);
         if constexpr (STEP) __builtin_amdgcn_sched_barrier(0);
     }
@@ -479,7 +474,7 @@ __device__ __forceinline__ uint32_t marks_of(const uint32_t* bits, int p) { retu
 
 // Sums of the weights of a workgroup's part of a row, noted with its last group; its other groups note none.  A wave adds up relative to a score of
 // its own, the best of the first scores it meets, and takes another one only when a score lies 2^40 above (in weights).
-template <int DT, bool WIDE_SUMS>
+template <int DT, bool WIDE>
 __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
     __shared__ uint32_t listed[3][GROUP_WORDS];
     __shared__ double parts[2][4];
@@ -490,7 +485,7 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
     at.group = start - at.row * a.groups;
     const auto* scores = static_cast<const typename Score<DT>::type*>(a.in.p);
     const double per = a.inv_t * 1.4426950408889634;
-    const bool rest = WIDE_SUMS || a.t.lse;
+    const bool rest = WIDE || a.t.lse;
     const Scale scale(a.inv_t);
     Quad<DT> x[4];
     auto load = [&](const GroupWalk& w) {
@@ -547,7 +542,7 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
                 weight = Weight32(base, per);
             }
         }
-        if constexpr (WIDE_SUMS) {
+        if constexpr (WIDE) {
             const Weights wide(base, scale);
 #pragma unroll
             for (int q = 0; q < 16; ++q) {
@@ -591,7 +586,7 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
 
 // A row's loss, what its gradients have in common, and the gradients of its listed candidates: k_distill_grad leaves these out, and what it reads in
 // their place (where gradients replace the scores) does not matter to it.
-template <int DT, bool WIDE_SUMS>
+template <int DT, bool WIDE>
 __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     constexpr int SLOTS = 2 * KGE_TOP_MAX;
     __shared__ double slot[4];
@@ -607,7 +602,7 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     r.n = a.in.n; r.is_dist = false; r.gamma = 0.f;
     const double* p = a.sums + 2 * row * a.groups;
     const double per = a.inv_t * 1.4426950408889634;
-    const bool rest = WIDE_SUMS || a.t.lse;
+    const bool rest = WIDE || a.t.lse;
     constexpr uint32_t NONE = 0xFFFFFFFFu;  // (not a position: rows have fewer than 2^32 candidates)
     for (int x = threadIdx.x; x < SLOTS; x += 256) { key[x] = NONE; first[x] = NONE; times[x] = 0; }
     float from = -INFINITY, list_best = -INFINITY, listed_best = -INFINITY;  // best of what the sums are of, of the teacher's scores, of the student's in the list
@@ -645,7 +640,7 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     if (rest) l.z = block_sum64<4>(l.z, slot);
     const RowSums sums = row_sums(a, b, from > -INFINITY ? (double)from : b, l, z_rest);
     if (threadIdx.x == 0) {
-        if constexpr (WIDE_SUMS) {
+        if constexpr (WIDE) {
             shared_wide = wide_row(a, sums, l, shared_grad);
         } else {
             if (a.loss) a.loss[row] = (float)row_loss(a, sums, l);
@@ -654,7 +649,7 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
         a.rows[row] = shared_grad;
     }
     auto position = [&](int e) { return entry_slot[e] == 0xFFFF ? (int64_t)-1 : (int64_t)key[entry_slot[e]]; };
-    if (WIDE_SUMS && a.loss) {
+    if (WIDE && a.loss) {
         __syncthreads();
         const double sum = block_sum64<4>(wide_list<256>(a, r, teacher, b, shared_wide, position, stands), slot);
         if (threadIdx.x == 0) a.loss[row] = shared_wide.live ? (float)((sum + shared_wide.rest) * a.loss_scale) : 0.f;
@@ -662,12 +657,11 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     __syncthreads();
     if (!a.grad) return;
     const RowGrad g = shared_grad;
-    const Weight32 weight(best, per);
     auto* out = static_cast<typename Score<DT>::type*>(a.grad) + row * a.ld_grad;
     for (int e = threadIdx.x; e < a.t.m; e += 256) {
         const uint32_t x = entry_slot[e];
         if (x == 0xFFFF || first[x] != (uint32_t)e) continue;
-        if constexpr (WIDE_SUMS) {
+        if constexpr (WIDE) {
             out[key[x]] = narrow<DT>((float)wide_grad(a, r, teacher, b, shared_wide, position, e, key[x], times[x] > 1));
         } else {
             double sum = exp(teacher.log_p(e));
@@ -677,7 +671,7 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
                 sum += exp(teacher.log_p(y));
                 --left;
             }
-            out[key[x]] = narrow<DT>(fmaf(weight.of(r.at(key[x])), g.listed, -(float)(sum * g.scale) * g.unit));
+            out[key[x]] = narrow<DT>((float)(exp(((double)r.at(key[x]) - b) * a.inv_t) * g.listed - sum * g.scale * g.unit));
         }
     }
 }
@@ -741,7 +735,7 @@ __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
 }
 
 // c: the context of a training step, whose launches are timed; null otherwise
-template <int DT, int MODE, bool STEP>
+template <int DT, bool WIDE, bool STEP>
 void launch_rows(kge_ctx* c, const DistillArgs& a, hipStream_t st) {
     const int64_t n = a.in.n;
     const dim3 grid = flat_grid(a.in.rows);
@@ -749,23 +743,22 @@ void launch_rows(kge_ctx* c, const DistillArgs& a, hipStream_t st) {
         if (c) KGE_LAUNCH(c, kernel, grid, dim3(threads), 0, st, a);
         else hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a);
     };
-    if (n <= 256) go(k_distill<DT, 1, 1, MODE, STEP>, 64);
-    else if (n <= 1024) go(k_distill<DT, 4, 1, MODE, STEP>, 256);
-    else if (n <= 4096) go(k_distill<DT, 4, 4, MODE, STEP>, 256);
+    if (n <= 256) go(k_distill<DT, 1, 1, WIDE, STEP>, 64);
+    else if (n <= 1024) go(k_distill<DT, 4, 1, WIDE, STEP>, 256);
+    else if (n <= 4096) go(k_distill<DT, 4, 4, WIDE, STEP>, 256);
     // (us, 16 / 1024 / 4096 rows of 5000, by the kernel for 16,384 -> by this: 9.0 -> 7.5 / 23.9 -> 17.6 / 71 -> 55)
-    else if (n <= 8192) go(k_distill<DT, 8, 4, MODE, STEP>, 512);
+    else if (n <= 8192) go(k_distill<DT, 8, 4, WIDE, STEP>, 512);
     // (us, 16 / 256 / 4096 rows of 15,000, 1024 threads -> these 512: 9.4 -> 9.3 / 13.5 -> 11.9 / 168 -> 132)
-    else if (n <= 16384) go(k_distill<DT, 8, 8, MODE, STEP>, 512);
-    else go(k_distill<DT, 16, 8, MODE, STEP>, 1024);
+    else if (n <= 16384) go(k_distill<DT, 8, 8, WIDE, STEP>, 512);
+    else go(k_distill<DT, 16, 8, WIDE, STEP>, 1024);
 }
 
 template <int DT>
 void launch(const DistillArgs& a, hipStream_t st) {
     const bool wide = a.t.temperature > WIDE_TEMPERATURE;
     if (a.groups == 0) {
-        if (wide) launch_rows<DT, WIDE, false>(nullptr, a, st);
-        else if (a.t.lse) launch_rows<DT, REST, false>(nullptr, a, st);
-        else launch_rows<DT, LISTS, false>(nullptr, a, st);
+        if (wide) launch_rows<DT, true, false>(nullptr, a, st);
+        else launch_rows<DT, false, false>(nullptr, a, st);
         return;
     }
     const dim3 grid = flat_grid(pieces(a.in.rows * a.groups, a.per)), rows = flat_grid(a.in.rows);
@@ -796,9 +789,8 @@ void kge_launch_distill(const RowScores& in, const TeacherLists& t, float grad_s
     a.loss = loss; a.grad = grad; a.ld_grad = ld_grad;
     if (step) {
         a.step = *step;
-        if (t.temperature > WIDE_TEMPERATURE) launch_rows<KGE_F32, WIDE, true>(step->c, a, st);
-        else if (t.lse) launch_rows<KGE_F32, REST, true>(step->c, a, st);
-        else launch_rows<KGE_F32, LISTS, true>(step->c, a, st);
+        if (t.temperature > WIDE_TEMPERATURE) launch_rows<KGE_F32, true, true>(step->c, a, st);
+        else launch_rows<KGE_F32, false, true>(step->c, a, st);
         return;
     }
     if (in.n > KGE_ROW_RESIDENT) {

@@ -244,3 +244,25 @@ def test_repeated_entries_at_large_temperatures(kge):
             # and the two losses themselves, of up to 45,000, are rounded to fp32: by 2^-24 of each
             assert ((one[0] - two[0] - less).abs() <= T * 2.0 ** -17 + 1.01 * U32 * (one[0].abs() + two[0].abs())).all()
             assert (one[1] - two[1]).abs().max() <= 2.0 ** -17
+
+
+# ---- listed candidates
+
+@pytest.mark.parametrize("T", [0.5, 1.0, 4.0])
+@pytest.mark.parametrize("n", [1, 5, 60, 256, 700, 1024])
+def test_lists_of_all_candidates(kge, n, T):
+    """Weights of listed candidates are formed in 64 bits at every temperature: where all are listed, loss and gradient are off by their rounding, and by the
+    2^-53 of each of some 30 steps, the logarithms' of their size."""
+    x = normal(4, n, n)
+    ids, t, lse = teacher_lists(x.double().numpy(), n, n, T, unused=False)
+    for given in (None, lse, lse + 0.3):
+        loss, grad = torch.empty(4, device="cuda"), torch.empty(4, n, device="cuda")
+        d_lse = None if given is None else torch.from_numpy(given).float().cuda()
+        kge.kge_distill_loss(rows_of(x), torch.from_numpy(ids).cuda(), torch.from_numpy(t).float().cuda(), d_lse, T, 1.0, loss, grad)
+        t32 = t.astype(np.float32).astype(np.float64)
+        for i in range(4):
+            want, g, scale, _, of_sum = exact(x[i].double().numpy(), ids[i], t32[i], None if given is None else d_lse[i].item(), T)
+            size = 2.0 + math.log(n) + (np.abs(x[i].double().numpy()).max() + np.abs(t[i]).max()) / T
+            assert abs(loss[i].item() - float(want)) <= 1.01 * U32 * abs(float(want)) + T * T * (30 * size + 4 * of_sum) * 2.0 ** -53
+            off = 1.01 * U32 * np.abs(g.astype(float)) + 30 * size * 2.0 ** -53 * scale.astype(float) + 2.0 ** -149
+            assert (np.abs(grad[i].double().cpu().numpy() - g.astype(float)) <= off).all()
