@@ -511,12 +511,18 @@ __global__ __launch_bounds__(256) void k_distill_sums(DistillArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i].template values<false>(here.group * GROUP + (wave * 4 + i) * 256, a.in.n, v + 4 * i);
-            const uint32_t bits = rest ? marks_of(listed[turn], (wave * 4 + i) * 256 + lane * 4) : 0u;
-            if (bits) {
+            if (!rest) best = largest(largest(best, v[4 * i], v[4 * i + 1]), v[4 * i + 2], v[4 * i + 3]);
+        }
+        if (rest) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) if (bits >> q & 1) v[4 * i + q] = -INFINITY;
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t bits = marks_of(listed[turn], (wave * 4 + i) * 256 + lane * 4);
+                if (bits) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) if (bits >> q & 1) v[4 * i + q] = -INFINITY;
+                }
+                best = largest(largest(best, v[4 * i], v[4 * i + 1]), v[4 * i + 2], v[4 * i + 3]);
             }
-            best = largest(largest(best, v[4 * i], v[4 * i + 1]), v[4 * i + 2], v[4 * i + 3]);
         }
         at.step(a.groups);
         const int next = turn == 2 ? 0 : turn + 1;
