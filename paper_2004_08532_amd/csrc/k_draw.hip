@@ -9,7 +9,7 @@
 //
 // What bounds them (fp32; a large copy takes 12 us for the first and 16 us for the last of these):
 //     1024 rows of 14,951, 16 draws, nothing cut   k_draw_whole 30 us: a weight in 64 bits per score, 13 M wave instructions, 26 us of the vector units
-//     the same, top-p 0.9, 1 draw                  k_draw_rows 62 us: bins, then weights in 64 bits, 23 M wave instructions, 47 us of the vector units
+//     the same, top-p 0.9, 1 draw                  k_draw_rows 63 us: bins, then weights in 64 bits, 22 M wave instructions, 45 us of the vector units
 //     one such row                                 k_draw_rows 22 us: a chain of some twenty steps between barriers, on one CU
 //     2 rows of 10 M, top-p 0.95, 64 draws         143 us in 9 launches: best and lowest score 16, bins 43, 29, 13 and 6, the cut 5, sums of what is
 //                                                  kept 26, running sums 8, draws 6; the first bins and the sums are bound by their weights
