@@ -72,6 +72,24 @@ template <int DT> struct RowAt {
     __device__ __forceinline__ float at(int64_t j) const { return of(widen<DT>(s[j])); }
 };
 
+// exp in 64 bits.  WIDE: the library's.  Else the polynomial of the draws' weights (k_rows.h), off by 4e-14: its coefficients are in scalar registers, those of
+// the library's in vector registers for all the loops over a list together (rows of 8192: 88 registers instead of 73).
+template <bool WIDE> struct Exp64 {
+    __device__ __forceinline__ double operator()(double x) const { return exp(x); }
+};
+template <> struct Exp64<false> {
+    Scale scale;
+    __device__ __forceinline__ Exp64() : scale(1.0) {}
+    __device__ __forceinline__ double operator()(double x) const {
+        x = x < -800.0 ? -800.0 : x > 800.0 ? 800.0 : x;  // (NaN stays)
+        const double shifted = fma(x, scale.per, 0x1.8p52), f = fma(x, scale.per, -(shifted - 0x1.8p52));
+        double p = scale.c[8];
+#pragma unroll
+        for (int i = 7; i >= 0; --i) p = fma(p, f, scale.c[i]);
+        return __builtin_ldexp(fma(p, f, 1.0), __double2loint(shifted));
+    }
+};
+
 // An entry of a list: the candidate's position, -1 if the entry is not used.
 template <int DT> __device__ __forceinline__ int64_t list_position(const DistillArgs& a, int64_t row, int e, int64_t n) {
     const int64_t id = a.t.ids[row * a.t.m + e];
@@ -89,18 +107,23 @@ struct Teacher {
 
 struct ListSums { double a, b, z; };  // sum of p before it is scaled, sum of p * (log p - (s - best) / T), MARKED: of the weights of the list's candidates
 
-// A thread's part of the list's sums.  stands(e): the first entry of its candidate.
-template <int DT, int THREADS, bool MARKED, typename S>
-__device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, const RowAt<DT>& r, const Teacher& teacher, double best, const S& stands) {
+struct Entry { double p, w; };  // before p is scaled; the student's weight
+
+// A thread's part of the list's sums.  stands(e): the first entry of its candidate.  `own` becomes the thread's first entry.
+template <int DT, int THREADS, bool MARKED, typename X, typename S>
+__device__ __forceinline__ ListSums sum_list(const DistillArgs& a, int64_t row, const RowAt<DT>& r, const Teacher& teacher, double best, const X& exp_of, const S& stands, Entry& own) {
     ListSums l = {0.0, 0.0, 0.0};
 #pragma unroll 1
     for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
         const int64_t id = list_position<DT>(a, row, e, r.n);
         if (id < 0) continue;
-        const double lp = teacher.log_p(e), p = exp(lp), x = ((double)r.at(id) - best) * a.inv_t;
+        const double lp = teacher.log_p(e), p = exp_of(lp), x = ((double)r.at(id) - best) * a.inv_t;
         l.a += p;
         if (p > 0.0 || p != p) l.b += p * (lp - x);
-        if (MARKED && stands(e)) l.z += x < INFINITY ? exp(x) : __longlong_as_double(0x7FF8000000000000ll);  // (of +inf and NaN)
+        if (!MARKED && !a.grad) continue;
+        const double w = x < INFINITY ? exp_of(x) : __longlong_as_double(0x7FF8000000000000ll);  // (of +inf and NaN)
+        if (MARKED && stands(e)) l.z += w;
+        if (e == (int)threadIdx.x) own = {p, w};
     }
     return l;
 }
@@ -116,8 +139,9 @@ __device__ __forceinline__ float coefficient(double x) {
 struct RowSums {
     double best, from, shift, z, z_rest;
 };
-__device__ __forceinline__ RowSums row_sums(const DistillArgs& a, double best, double from, const ListSums& l, double z_rest) {
-    const double shift = from == best ? 1.0 : exp((from - best) * a.inv_t);
+template <typename X>
+__device__ __forceinline__ RowSums row_sums(const DistillArgs& a, double best, double from, const ListSums& l, double z_rest, const X& exp_of) {
+    const double shift = from == best ? 1.0 : exp_of((from - best) * a.inv_t);
     return {best, from, shift, z_rest > 0.0 ? l.z + z_rest * shift : l.z + z_rest, z_rest};
 }
 // From these and the sums of the row's list.
@@ -161,7 +185,7 @@ __device__ __forceinline__ double row_loss(const DistillArgs& a, const RowSums& 
 //     sum p delta = sum (p delta - p + q) = sum p (delta + expm1(-delta)),    P q - p = p expm1(-delta) + (P - 1) q
 // whose terms are all small of themselves: an error of delta, 2^-53 times the size of the logarithms in it, is multiplied with |p - q|.
 // Largest error of a loss beside the loss, 14,952 candidates, lists of 64 and a rest, 32 bits -> 64: T = 4 7e-8 (half a step of fp32 is 6e-8), T = 8 9e-8 -> 5e-8, T = 100
-// 5e-7 -> 5e-8, T = 1000 8e-6 -> 5e-8.  us, 1024 rows of 256 / 14,951 with their gradient 7.8 -> 8.3 / 34 -> 45, 64 rows of 100,000 30 -> 33.
+// 5e-7 -> 5e-8, T = 1000 8e-6 -> 5e-8.  us, 1024 rows of 256 / 14,951 with their gradient 8.0 -> 8.4 / 34 -> 43, 64 rows of 100,000 30 -> 33.
 constexpr float WIDE_TEMPERATURE = 4.f;
 struct WideRow {
     double log_z, log_mass;  // of the student's weights, of the list's p before they are scaled
@@ -249,9 +273,10 @@ __device__ __forceinline__ void store_unlisted(typename Score<DT>::type* row, in
     }
 }
 
-// (Rows of 16,384: 123 registers at 4 waves per SIMD; at 6, 31 are spilled and 1024 rows of 14,951 take 54 us instead of 42.)
+// (Workgroups of 512: 80 registers for three rows on a CU; of rows of 16,384, 9 are spilled.  us, 4096 rows of 15,000 at two rows -> at three 147 -> 116; of 5000,
+// where nothing is spilled, 73 -> 58.)
 template <int DT, int WAVES, int TPW, bool WIDE, bool STEP>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? 4 : 1) void k_distill(DistillArgs a) {
+__global__ __launch_bounds__(WAVES * 64, WAVES != 8 ? 1 : !WIDE ? 6 : 4) void k_distill(DistillArgs a) {
     constexpr int CAP = WAVES * TPW * 256, THREADS = WAVES * 64, N = TPW * 4;
     __shared__ uint32_t listed[CAP / 32];  // a bit per candidate
     __shared__ int32_t list_at[KGE_TOP_MAX];
@@ -270,24 +295,11 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? 4 : 1) void k_
 
     for (int x = threadIdx.x; x < CAP / 32; x += THREADS) listed[x] = 0;
     if (threadIdx.x == 0) twice = 0;
-    float v[N], best = -INFINITY, list_best = -INFINITY;
-    {
-        Quad<DT> x[TPW];
+    Quad<DT> x[TPW];
 #pragma unroll
-        for (int i = 0; i < TPW; ++i) x[i].load(r.s, (i * WAVES + wave) * 256 + lane * 4, r.n);
-#pragma unroll
-        for (int i = 0; i < TPW; ++i) {
-            const int tile = (i * WAVES + wave) * 256;
-            x[i].template values<false>(tile, r.n, v + 4 * i);
-            if constexpr (STEP) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) if (tile + lane * 4 + q < r.n) v[4 * i + q] = r.of(v[4 * i + q]);
-            }
-            best = largest(largest(best, v[4 * i], v[4 * i + 1]), v[4 * i + 2], v[4 * i + 3]);
-        }
-    }
-    const bool bad = __ballot(!(best < INFINITY)) != 0;  // NaN or +inf: the row's sums are NaN
+    for (int i = 0; i < TPW; ++i) x[i].load(r.s, (i * WAVES + wave) * 256 + lane * 4, r.n);
     __syncthreads();
+    float list_best = -INFINITY, listed_best = -INFINITY;  // of the teacher's scores, of the student's
 #pragma unroll 1
     for (int e = threadIdx.x; e < a.t.m; e += THREADS) {
         const int at = (int)list_position<DT>(a, row, e, r.n);
@@ -296,40 +308,40 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? 4 : 1) void k_
             const uint32_t bit = 1u << (at & 31);
             if (atomicOr(&listed[at >> 5], bit) & bit) twice = 1;
             list_best = fmaxf(list_best, a.t.scores[row * a.t.m + e]);
+            listed_best = fmaxf(listed_best, r.at(at));
         }
     }
-    best = bad ? INFINITY : wave_most(best);
+    __syncthreads();
+    // The list's candidates have no part in the registers' weights, which are relative to the best of the others.
+    float v[N], from = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+        const int tile = (i * WAVES + wave) * 256, at = tile + lane * 4;
+        const uint32_t bits = listed[at >> 5] >> (at & 31);
+        x[i].template values<false>(tile, r.n, v + 4 * i);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (STEP) if (at + q < r.n) v[4 * i + q] = r.of(v[4 * i + q]);
+            const int mask = __builtin_amdgcn_sbfe((int)bits, q, 1);  // (-1: listed)
+            v[4 * i + q] = __int_as_float((mask & (int)0xFF800000) | (~mask & __float_as_int(v[4 * i + q])));
+        }
+        from = largest(largest(from, v[4 * i], v[4 * i + 1]), v[4 * i + 2], v[4 * i + 3]);
+    }
+    const bool bad = __ballot(!(from < INFINITY)) != 0;  // NaN or +inf: the row's sums are NaN
+    from = bad ? INFINITY : wave_most(from);
     list_best = wave_most(list_best);
-    if (lane == 0) { maxima[0][wave] = best; maxima[1][wave] = list_best; }
+    listed_best = wave_most(listed_best);
+    if (lane == 0) { maxima[0][wave] = from; maxima[1][wave] = list_best; maxima[2][wave] = listed_best; }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-        best = fmaxf(best, maxima[0][w]);
+        from = fmaxf(from, maxima[0][w]);
         list_best = fmaxf(list_best, maxima[1][w]);
+        listed_best = fmaxf(listed_best, maxima[2][w]);
     }
-    best = scalar(best);
+    from = scalar(from);
+    const float best = scalar(fmaxf(from, listed_best));
     const Teacher teacher(a, row, scalar(list_best));
-    // The list's candidates have no part in the registers' weights, which are relative to the best of the others.
-    float from = -INFINITY;
-    {
-        uint32_t bits[(TPW + 7) / 8] = {};  // of the registers, in their order
-#pragma unroll
-        for (int i = 0; i < TPW; ++i) bits[i / 8] |= (listed[((i * WAVES + wave) * 256 + lane * 4) >> 5] >> (lane * 4 & 31) & 15u) << i % 8 * 4;
-#pragma unroll
-        for (int q = 0; q < N; ++q) {
-            const int mask = __builtin_amdgcn_sbfe((int)bits[q / 32], q % 32, 1);  // (-1: listed)
-            v[q] = __int_as_float((mask & (int)0xFF800000) | (~mask & __float_as_int(v[q])));
-            from = fmaxf(from, v[q]);
-        }
-        from = wave_most(from);
-        if constexpr (WAVES > 1) {
-            if (lane == 0) maxima[2][wave] = from;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) from = fmaxf(from, maxima[2][w]);
-        }
-        from = scalar(from);
-    }
     const double per = a.inv_t * 1.4426950408889634;
     const Weight32 relative(from, per);
     double z = 0.0;
@@ -359,9 +371,11 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? 4 : 1) void k_
     };
     const double top = fabsf(best) < INFINITY ? (double)best : 0.0;
     ListSums l = {0.0, 0.0, 0.0};
+    const Exp64<WIDE> exp_of;
+    Entry own = {0.0, 0.0};  // (most lists have at most an entry per thread: nothing is formed twice)
     z = wave_sum64(z);
     if (wave * 64 < a.t.m) {
-        l = sum_list<DT, THREADS, true>(a, row, r, teacher, top, stands);
+        l = sum_list<DT, THREADS, true>(a, row, r, teacher, top, exp_of, stands, own);
         l.a = wave_sum64(l.a);
         l.b = wave_sum64(l.b);
         l.z = wave_sum64(l.z);
@@ -373,7 +387,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? 4 : 1) void k_
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum[k] = wave_sum64(lane < WAVES ? parts[k][lane] : 0.0);
         l = {sum[2], sum[3], sum[1]};
-        const RowSums sums = row_sums(a, top, relative.best, l, best == INFINITY ? __longlong_as_double(0x7FF8000000000000ll) : sum[0]);
+        const RowSums sums = row_sums(a, top, relative.best, l, best == INFINITY ? __longlong_as_double(0x7FF8000000000000ll) : sum[0], exp_of);
         if (lane == 0) {
             if constexpr (WIDE) {
                 shared_wide = wide_row(a, sums, l, shared_grad);
@@ -413,12 +427,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 && TPW == 8 ? 4 : 1) void k_
         if constexpr (WIDE) {
             x = (float)wide_grad(a, r, teacher, top, shared_wide, position, e, at, twice != 0);
         } else {
-            auto p_of = [&](int x) { return exp(teacher.log_p(x)) * g.scale; };
-            double p = p_of(e);
+            if (e >= THREADS) own = {exp_of(teacher.log_p(e)), exp_of(((double)r.of(raw) - top) * a.inv_t)};
+            double p = own.p;
             if (twice) {
-                for (int y = e + 1; y < a.t.m; ++y) if (list_at[y] == at) p += p_of(y);
+                for (int y = e + 1; y < a.t.m; ++y) if (list_at[y] == at) p += exp_of(teacher.log_p(y));
             }
-            x = (float)(exp(((double)r.of(raw) - top) * a.inv_t) * g.listed - p * g.unit);
+            x = (float)(own.w * g.listed - p * g.scale * g.unit);
         }
         out[at] = narrow<DT>(shape(x, raw));
     }
@@ -640,11 +654,13 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
     z_rest = block_sum64<4>(z_rest, slot);
     const Teacher teacher(a, row, list_best);
     auto stands = [&](int e) { return first[entry_slot[e]] == (uint32_t)e; };
-    ListSums l = rest ? sum_list<DT, 256, true>(a, row, r, teacher, b, stands) : sum_list<DT, 256, false>(a, row, r, teacher, b, stands);
+    const Exp64<WIDE> exp_of;
+    Entry own = {0.0, 0.0};
+    ListSums l = rest ? sum_list<DT, 256, true>(a, row, r, teacher, b, exp_of, stands, own) : sum_list<DT, 256, false>(a, row, r, teacher, b, exp_of, stands, own);
     l.a = block_sum64<4>(l.a, slot);
     l.b = block_sum64<4>(l.b, slot);
     if (rest) l.z = block_sum64<4>(l.z, slot);
-    const RowSums sums = row_sums(a, b, from > -INFINITY ? (double)from : b, l, z_rest);
+    const RowSums sums = row_sums(a, b, from > -INFINITY ? (double)from : b, l, z_rest, exp_of);
     if (threadIdx.x == 0) {
         if constexpr (WIDE) {
             shared_wide = wide_row(a, sums, l, shared_grad);
@@ -670,14 +686,15 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs a) {
         if constexpr (WIDE) {
             out[key[x]] = narrow<DT>((float)wide_grad(a, r, teacher, b, shared_wide, position, e, key[x], times[x] > 1));
         } else {
-            double sum = exp(teacher.log_p(e));
+            if (e >= 256) own = {exp_of(teacher.log_p(e)), exp_of(((double)r.at(key[x]) - b) * a.inv_t)};
+            double sum = own.p;
             uint32_t left = times[x] - 1;
             for (int y = e + 1; left; ++y) {
                 if (entry_slot[y] != x) continue;
-                sum += exp(teacher.log_p(y));
+                sum += exp_of(teacher.log_p(y));
                 --left;
             }
-            out[key[x]] = narrow<DT>((float)(exp(((double)r.at(key[x]) - b) * a.inv_t) * g.listed - sum * g.scale * g.unit));
+            out[key[x]] = narrow<DT>((float)(own.w * g.listed - sum * g.scale * g.unit));
         }
     }
 }
@@ -752,9 +769,9 @@ void launch_rows(kge_ctx* c, const DistillArgs& a, hipStream_t st) {
     if (n <= 256) go(k_distill<DT, 1, 1, WIDE, STEP>, 64);
     else if (n <= 1024) go(k_distill<DT, 4, 1, WIDE, STEP>, 256);
     else if (n <= 4096) go(k_distill<DT, 4, 4, WIDE, STEP>, 256);
-    // (us, 16 / 1024 / 4096 rows of 5000, by the kernel for 16,384 -> by this: 9.0 -> 7.5 / 23.9 -> 17.6 / 71 -> 55)
+    // (us, 16 / 1024 / 4096 rows of 5000, by the kernel for 16,384 -> by this: 9.6 -> 8.1 / 24 -> 19 / 76 -> 58)
     else if (n <= 8192) go(k_distill<DT, 8, 4, WIDE, STEP>, 512);
-    // (us, 16 / 256 / 4096 rows of 15,000, 1024 threads -> these 512: 9.4 -> 9.3 / 13.5 -> 11.9 / 168 -> 132)
+    // (us, 16 / 256 / 4096 rows of 15,000, 1024 threads -> these 512: 9.2 -> 9.8 / 11.7 -> 12.0 / 198 -> 116)
     else if (n <= 16384) go(k_distill<DT, 8, 8, WIDE, STEP>, 512);
     else go(k_distill<DT, 16, 8, WIDE, STEP>, 1024);
 }
