@@ -111,7 +111,8 @@ __device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, 
     int last = 0;  // tile with a weight
 #pragma unroll
     for (int k = 0; k < WORDS; ++k) {
-        const uint64_t some = weighted[k];
+        const uint64_t word = weighted[k];  // (the same for the wave: in scalar registers, and with it the tiles' numbers)
+        const uint64_t some = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(word >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)word);
         x[k] = some >> lane & 1 ? sums[k * 64 + lane] : -INFINITY;
         if (some) last = k * 64 + 63 - __clzll(some);
     }
@@ -124,12 +125,13 @@ __device__ __forceinline__ void draw_from_tiles(const DrawArgs& a, int64_t row, 
 #pragma unroll
         for (int d = 0; d < AT_ONCE; ++d) {
             const double want = lane64(own, d);
-            tile[d] = last;  // the first tile with a weight whose running sum exceeds `want`
+            int at = 0;  // the first tile with a weight whose running sum exceeds `want`, the last one with a weight where none does
 #pragma unroll
             for (int k = WORDS - 1; k >= 0; --k) {
-                const uint64_t past = __ballot(x[k] > want);
-                if (past) tile[d] = k * 64 + __ffsll((unsigned long long)past) - 1;
+                const uint64_t past = __ballot(x[k] > want) | (last / 64 == k ? (uint64_t)1 << (last & 63) : 0);
+                at = past ? k * 64 + __builtin_ctzll(past) : at;
             }
+            tile[d] = at;
             quad[d].load(s, (int64_t)tile[d] * 256 + lane * 4, a.in.n);
         }
         uint32_t missed = 0;  // a bit per draw
