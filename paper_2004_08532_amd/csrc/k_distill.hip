@@ -13,10 +13,10 @@
 // candidates are formed in 64 bits (but for the sum of a long row without a rest); up to T = 4 those of the others in 32 bits from an argument in 64, four of them
 // added in 32.  All other sums and logarithms are in 64.
 //
-// 1024 rows of 14,951 fp32, lists of 64 and a rest: 36 us, 3.4 TB/s read and written (a large copy: 24 us); the vector units work for 21, and the
-// phases of a row (reads, sums, list, writes) overlap only with those of one other row on the CU.  16 rows of 2.5 M bf16, lists of 256 and a
+// 1024 rows of 14,951 fp32, lists of 64 and a rest: 37 us, 3.3 TB/s read and written (a large copy: 24 us); the vector units work for 19, and the
+// phases of a row (reads, sums, list, writes) overlap only with those of two other rows on the CU.  16 rows of 2.5 M bf16, lists of 256 and a
 // rest: sums 33 us (2.4 TB/s; 11.9 M wave instructions, 25 us of the vector units), lists 10, gradient 32 (5 TB/s).  690 rows of 40,943 fp16, loss
-// alone: sums 25, lists 7.  1024 rows of 256, lists of 16: 7.7 us.
+// alone: sums 24, lists 7.  1024 rows of 256, lists of 16: 7.4 us.
 #include "k_rows.h"
 
 namespace {
